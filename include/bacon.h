@@ -348,6 +348,174 @@ typedef struct {
 bacon_status bacon_profile_enable(bacon_ctx *ctx, int32_t enable);
 int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
 
+/* ---- Decoding over the kept rows: a cache held in 8 bits -----------------
+ *
+ * The rows that a prompt's compression keeps (bacon_select_topk, the fused
+ * calls) move into blocks of block_tokens tokens of one (layer, sequence, KV
+ * head) -- a pair below -- each with K and V in e4m3 and one scale for its K
+ * and one for its V.  New tokens are appended there, and decoding attends over them.
+ *
+ *   scale of a block of rows X:  2^e, e the smallest integer with
+ *       max |X| <= 448 2^e, held to -100 <= e <= 120 (max |X| = 0: e = -100)
+ *   code of x:   x 2^-e rounded to the nearest e4m3 value, ties to even
+ *   value held:  code 2^e
+ *
+ * A power of two changes no value's relative precision (e4m3 keeps 4 bits
+ * whatever the scale, down to 2^-6 of it), its products are exact, the value
+ * held is exact in bfloat16 and float32, and a scale that has to grow moves
+ * codes by whole binades.  Values are finite with |x| <= 2^127.
+ *
+ * Every pair has a length (rows held), a row of the block table (max_blocks
+ * block ids, -1 where it has none) and the offset of its entries in the
+ * layer's idx.  They lie in device memory with the codes: lengths that only the
+ * device knows (BACON_ALLOC_ADAPTIVE) never pass through the host.  Row p of a
+ * pair is row p % block_tokens of block table[p / block_tokens].
+ *
+ * Memory of a cache, at the byte offsets of bacon_cache_layout:
+ *   lens, starts  [num_layers, max_batch, Hkv] int32
+ *   table         [num_layers, max_batch, Hkv, max_blocks] int32
+ *   scales        [num_blocks, 2] float32, K then V
+ *   codes         [num_blocks, 2, block_tokens * d] e4m3 bytes: K as
+ *                 [block_tokens, d], V transposed as [d, block_tokens]
+ *   errors        one uint32 word
+ *
+ * Calls name the sequences first_seq .. first_seq + num_seqs - 1 (or + batch
+ * - 1) of the cache, so that a prompt can join a batch that is decoding.
+ * The same rules as above: checks on the host before anything is enqueued,
+ * no allocation, no synchronisation, the caller's buffers, all work on the
+ * given stream.  Calls on one cache run one after the other (one stream, or
+ * events between streams), but attends and loads of one cache may run beside
+ * each other, each attend with a work buffer of its own.  What only the device can see is
+ * bounded there and noted in the error word: a pair that finds no blocks, an
+ * append beyond the table, an id outside the pool (its rows count as absent),
+ * an idx entry outside the candidates (its row is zero). */
+
+typedef struct {
+  int32_t num_layers;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;      /* num_q_heads % num_kv_heads == 0              */
+  int32_t head_dim;          /* 64 or 128                                    */
+  int32_t window;            /* W >= 1 of the prompt's compression           */
+  int32_t block_tokens;      /* 16, 32 or 64                                 */
+  int32_t max_batch;         /* sequences, 1..64                             */
+  int32_t max_blocks;        /* table entries of a pair, >= 1                */
+  int64_t num_blocks;        /* blocks of the pool, 1..2^31 - 1              */
+  bacon_dtype dtype;         /* of K and V rows, queries and outputs         */
+} bacon_cache_shape;
+
+typedef struct {
+  size_t lens, starts, table, scales, codes, errors;   /* byte offsets       */
+  size_t total;                                        /* bytes of the cache */
+} bacon_cache_offsets;
+
+typedef struct bacon_cache bacon_cache;
+
+/* Bits of the error word. */
+enum {
+  BACON_CACHE_NO_BLOCKS = 1,  /* a pair found no blocks, or an append no room */
+  BACON_CACHE_BAD_BLOCK = 2,  /* a block id outside [0, num_blocks)           */
+  BACON_CACHE_BAD_INDEX = 4   /* an idx entry outside the candidates          */
+};
+
+/* Where the parts of a cache of this shape lie in its memory. */
+bacon_status bacon_cache_layout(const bacon_cache_shape *shape, bacon_cache_offsets *out);
+
+/* Creates a cache over the caller's device memory (bytes >= total above,
+ * 256-byte aligned).  Host work only; bacon_cache_clear comes first. */
+bacon_status bacon_cache_init(bacon_cache **cache, const bacon_cache_shape *shape, void *d_mem, size_t bytes);
+
+/* Destroys the host object (the memory stays the caller's). */
+bacon_status bacon_cache_free(bacon_cache *cache);
+
+/* Empties sequences: lengths 0, tables -1.  Every sequence is cleared once
+ * before another call names it (ORDER otherwise).  A clear of all max_batch
+ * sequences, and a cache's first clear, also clears the error word. */
+bacon_status bacon_cache_clear(bacon_cache *cache, int32_t first_seq, int32_t num_seqs, void *stream);
+
+/* Block tables of a prompt's pairs, built on the device.  Sequence b of the
+ * batch becomes sequence first_seq + b; its pair (l, h) holds
+ *   rows = min(K_{l,b,h}, N_b - W) + W
+ * and takes need = ceil((rows + reserve) / block_tokens) ids, in (layer,
+ * sequence, head) order, from d_free [num_free] (int32, device; each once), or
+ * from 0, 1, 2, .. num_blocks - 1 where d_free is NULL.  K_{l,b,h} is entry
+ * (l * budgets_batch + b) * Hkv + h of d_budgets (int32, device; what
+ * bacon_alloc_output receives, with budgets_batch its max_batch), or, where d_budgets is
+ * NULL, budgets[b] of the batch at every layer.  head_budgets must be NULL
+ * (INVALID): head-wise budgets are given in d_budgets.
+ * A pair whose ids pass the end of the list, or that needs more than
+ * max_blocks, gets no blocks and length 0 (NO_BLOCKS); the ids of later pairs
+ * do not move.  d_used (int64, device, optional) receives the sum of need. */
+bacon_status bacon_cache_tables(bacon_cache *cache, const bacon_batch *batch, int32_t first_seq,
+                                const int32_t *d_budgets, int32_t budgets_batch, int32_t reserve,
+                                const int32_t *d_free, int64_t num_free, int64_t *d_used, void *stream);
+
+/* The kept rows of num_layers layers of a prompt, quantised into the blocks
+ * that bacon_cache_tables gave (the same batch and first_seq).  d_k, d_v: host
+ * arrays of num_layers device pointers to the layers' K and V [T, Hkv, d], as
+ * bacon_compact reads them; d_idx: such an array of their idx.  The pair's rows are its kept positions in
+ * ascending order, then the window's; d_idx NULL stands for idx entries 0, 1, 2, ...
+ * (every row, where the budget is N_b - W). */
+bacon_status bacon_cache_store(bacon_cache *cache, const bacon_batch *batch, int32_t first_seq,
+                               int32_t first_layer, int32_t num_layers, const void *const *d_k,
+                               const void *const *d_v, const int32_t *const *d_idx, void *stream);
+
+/* The values held: rows first_token .. first_token + count - 1 of every pair
+ * of the named layers and sequences to d_k_out, d_v_out [num_layers, num_seqs,
+ * Hkv, count, d] (the cache's dtype); zero where the pair has no such row.
+ * first_token < 0 counts from each pair's end: -count is its last count rows. */
+bacon_status bacon_cache_load(bacon_cache *cache, int32_t first_layer, int32_t num_layers,
+                              int32_t first_seq, int32_t num_seqs, int32_t first_token, int32_t count,
+                              void *d_k_out, void *d_v_out, void *stream);
+
+/* Appends new tokens of one layer: token j of sequence b is row b * tokens + j
+ * of d_k and d_v, rows of Hkv x d elements k_stride and v_stride elements
+ * apart (>= Hkv d, 16 bytes a multiple; a view of a fused projection's output will do).  d_counts [num_seqs] (int32,
+ * device, optional; held to 0..tokens) gives each sequence's own number of new tokens.  Every pair's length
+ * grows by that number.  In each block touched, e is the larger of the old
+ * rows' (if the block has any) and of the one the new rows need; where it
+ * grows the old codes are rounded again at it.  A pair without room (in its
+ * table's blocks) is left as it is (NO_BLOCKS).  1 <= tokens <= 64. */
+bacon_status bacon_cache_append(bacon_cache *cache, int32_t layer, int32_t first_seq, int32_t num_seqs,
+                                int32_t tokens, const int32_t *d_counts, const void *d_k, int64_t k_stride,
+                                const void *d_v, int64_t v_stride, void *stream);
+
+/* Attention of the last tokens of every sequence over one layer's cache:
+ * query j of c = d_counts[b] (or tokens) sees the rows p < len - (c - 1 - j)
+ * of its KV head, out = softmax(q . k / sqrt(d)) v in 32 bits.  d_q rows as
+ * d_k above, with Hq heads; d_out [num_seqs, tokens, Hq, d] in the cache's
+ * dtype; d_lse (optional) [num_seqs, tokens, Hq] float32, the natural log of
+ * the normaliser.  A query that sees no row, and a query j >= c (a padded
+ * batch), gives zeros and -infinity.  G * tokens <= 64, G = Hq / Hkv.
+ * max_tokens: the longest length to expect (0: the table's), which settles how the work is
+ * divided; longer pairs are right, only slower.  d_work: scratch of
+ * bacon_cache_work_bytes (0: may be NULL), 256-byte aligned, of this call
+ * alone until its work is done. */
+bacon_status bacon_cache_attend(bacon_cache *cache, int32_t layer, int32_t first_seq, int32_t num_seqs,
+                                int32_t tokens, const int32_t *d_counts, const void *d_q, int64_t q_stride,
+                                int32_t max_tokens, void *d_out, float *d_lse, void *d_work,
+                                size_t work_bytes, void *stream);
+size_t bacon_cache_work_bytes(const bacon_cache *cache, int32_t num_seqs, int32_t tokens,
+                              int32_t max_tokens);
+
+/* A decode step of one layer: bacon_cache_append, then bacon_cache_attend over
+ * the grown cache, with the same results. */
+bacon_status bacon_cache_step(bacon_cache *cache, int32_t layer, int32_t first_seq, int32_t num_seqs,
+                              int32_t tokens, const int32_t *d_counts, const void *d_q, int64_t q_stride,
+                              const void *d_k, int64_t k_stride, const void *d_v, int64_t v_stride,
+                              int32_t max_tokens, void *d_out, float *d_lse, void *d_work,
+                              size_t work_bytes, void *stream);
+
+/* Moves lengths: every pair of the named layers and sequences by d_delta[b]
+ * (int32, device, optional) or by delta, held to 0 .. max_blocks *
+ * block_tokens.  A negative move takes back drafted tokens that were rejected
+ * (a scale that grew for them stays). */
+bacon_status bacon_cache_advance(bacon_cache *cache, int32_t first_layer, int32_t num_layers,
+                                 int32_t first_seq, int32_t num_seqs, int32_t delta, const int32_t *d_delta,
+                                 void *stream);
+
+/* Waits for the device and returns the error word (-1 if it cannot be read). */
+int32_t bacon_cache_errors(bacon_cache *cache);
+
 const char *bacon_status_string(bacon_status s);
 const char *bacon_last_error(void);
 

@@ -27,6 +27,10 @@ ENTRY_POINTS = [
     "bacon_idx_count",
     "bacon_kept_rows",
     "bacon_profile_enable", "bacon_profile_read", "bacon_status_string", "bacon_last_error",
+    "bacon_cache_layout", "bacon_cache_init", "bacon_cache_free", "bacon_cache_clear",
+    "bacon_cache_tables", "bacon_cache_store", "bacon_cache_load", "bacon_cache_append",
+    "bacon_cache_attend", "bacon_cache_work_bytes", "bacon_cache_step", "bacon_cache_advance",
+    "bacon_cache_errors",
 ]
 
 
@@ -56,6 +60,23 @@ class Batch(C.Structure):
 
 class KernelTime(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("launches", C.c_int64), ("total_ms", C.c_double)]
+
+
+class CacheShape(C.Structure):
+    _fields_ = [("num_layers", C.c_int32), ("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("window", C.c_int32), ("block_tokens", C.c_int32),
+                ("max_batch", C.c_int32), ("max_blocks", C.c_int32), ("num_blocks", C.c_int64),
+                ("dtype", C.c_int)]
+
+
+class CacheOffsets(C.Structure):
+    _fields_ = [("lens", C.c_size_t), ("starts", C.c_size_t), ("table", C.c_size_t),
+                ("scales", C.c_size_t), ("codes", C.c_size_t), ("errors", C.c_size_t),
+                ("total", C.c_size_t)]
+
+
+# bits of a cache's error word
+CACHE_NO_BLOCKS, CACHE_BAD_BLOCK, CACHE_BAD_INDEX = 1, 2, 4
 
 
 class BaconError(RuntimeError):
@@ -106,6 +127,26 @@ def lib() -> C.CDLL:
         L.bacon_profile_enable.argtypes = [vp, C.c_int32]
         L.bacon_profile_read.argtypes = [vp, C.POINTER(KernelTime), C.c_int32]
         L.bacon_profile_read.restype = C.c_int32
+        i32, i64, cap = C.c_int32, C.c_int64, C.POINTER(Batch)
+        L.bacon_cache_layout.argtypes = [C.POINTER(CacheShape), C.POINTER(CacheOffsets)]
+        L.bacon_cache_init.argtypes = [ctxp, C.POINTER(CacheShape), vp, sz]
+        L.bacon_cache_free.argtypes = [vp]
+        L.bacon_cache_clear.argtypes = [vp, i32, i32, vp]
+        L.bacon_cache_tables.argtypes = [vp, cap, i32, vp, i32, i32, vp, i64, vp, vp]
+        L.bacon_cache_store.argtypes = [vp, cap, i32, i32, i32, vp, vp, vp, vp]
+        L.bacon_cache_load.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]
+        L.bacon_cache_append.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp]
+        L.bacon_cache_attend.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, i32, vp, vp, vp, sz, vp]
+        L.bacon_cache_work_bytes.argtypes = [vp, i32, i32, i32]
+        L.bacon_cache_work_bytes.restype = sz
+        L.bacon_cache_step.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, i32, vp, vp,
+                                       vp, sz, vp]
+        L.bacon_cache_advance.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp]
+        L.bacon_cache_errors.argtypes = [vp]
+        L.bacon_cache_errors.restype = i32
+        for name in ("layout", "init", "free", "clear", "tables", "store", "load", "append", "attend",
+                     "step", "advance"):
+            getattr(L, "bacon_cache_" + name).restype = C.c_int
         L.bacon_status_string.argtypes = [C.c_int]
         L.bacon_status_string.restype = C.c_char_p
         L.bacon_last_error.restype = C.c_char_p
@@ -388,3 +429,220 @@ def bacon_debug_capture(ctx: Context, B=None, V=None, lam=None):
 
 def bacon_window_lse(ctx: Context, batch, q_win, k, out=None):
     return ctx.bacon_window_lse(batch, q_win, k, out)
+
+
+class Cache:
+    """A bacon_cache: the kept rows of a model's layers in 8 bits, with its
+    memory on `device`.
+
+    lens, starts [num_layers, max_batch, Hkv] and table [.., max_blocks]
+    (int32), scales [num_blocks, 2] (float32) and codes [num_blocks, 2,
+    block_tokens * d] (uint8, e4m3) are views of that memory.  max_tokens: the
+    longest a pair may become.  Tensors given to the calls are on the cache's
+    device; every call runs on that device's current stream.  New tokens and
+    queries may be views of one projection's output: only the heads of a token have
+    to lie together, tokens evenly spaced.
+    """
+
+    def __init__(self, num_layers, num_q_heads, num_kv_heads, head_dim, window, block_tokens, max_batch,
+                 max_tokens, num_blocks, dtype, device="cuda"):
+        import torch
+        if block_tokens < 1:
+            raise BaconError(ERR_INVALID, "block_tokens must be >= 1")
+        blocks = (max_tokens + block_tokens - 1) // block_tokens
+        self.shape = CacheShape(num_layers, num_q_heads, num_kv_heads, head_dim, window, block_tokens,
+                                max_batch, blocks, num_blocks, BF16 if dtype in ("bf16", BF16) else FP32)
+        off = CacheOffsets()
+        _check(lib().bacon_cache_layout(C.byref(self.shape), C.byref(off)))
+        dev = torch.device(device)
+        self.device = dev if dev.index is not None else torch.device(dev.type, torch.cuda.current_device())
+        self.torch_dtype = torch.bfloat16 if self.shape.dtype == BF16 else torch.float32
+        self.memory = torch.empty(off.total + 256, dtype=torch.uint8, device=self.device)
+        skip = -self.memory.data_ptr() % 256
+        self._h = C.c_void_p()
+        _check(lib().bacon_cache_init(C.byref(self._h), C.byref(self.shape),
+                                      C.c_void_p(self.memory.data_ptr() + skip), off.total))
+
+        def part(at, dtype, *shape):
+            n = int(np.prod(shape)) * dtype.itemsize
+            return self.memory[skip + at:skip + at + n].view(dtype).view(shape)
+
+        pairs = (num_layers, max_batch, num_kv_heads)
+        self.lens = part(off.lens, torch.int32, *pairs)
+        self.starts = part(off.starts, torch.int32, *pairs)
+        self.table = part(off.table, torch.int32, *pairs, blocks)
+        self.scales = part(off.scales, torch.float32, num_blocks, 2)
+        self.codes = part(off.codes, torch.uint8, num_blocks, 2, block_tokens * head_dim)
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h and h.value and _lib is not None:
+            _lib.bacon_cache_free(h)
+            self._h = C.c_void_p()
+
+    # ---- checks and marshalling
+    def _stream(self):
+        import torch
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _call(self, fn, *args):
+        """fn on the cache's device and that device's current stream."""
+        import torch
+        if torch.cuda.current_device() == self.device.index:
+            _check(fn(self._h, *args, self._stream()))
+        else:
+            with torch.cuda.device(self.device):
+                _check(fn(self._h, *args, self._stream()))
+
+    def _whole(self, t, name, dtype, shape=None):
+        """The pointer of a contiguous tensor of this dtype (and shape)."""
+        if t is None:
+            return None
+        if t.device != self.device or t.dtype != dtype or not t.is_contiguous():
+            raise BaconError(ERR_INVALID, f"{name} must be a contiguous {dtype} tensor on {self.device}")
+        if shape is not None and tuple(t.shape) != shape:
+            raise BaconError(ERR_INVALID, f"{name} has shape {tuple(t.shape)}, {shape} expected")
+        return t.data_ptr()
+
+    def _tokens(self, t, name, heads, like=None):
+        """Pointer and token distance of rows [num_seqs, tokens, heads, d]."""
+        if t.device != self.device or t.dtype != self.torch_dtype or t.dim() != 4:
+            raise BaconError(ERR_INVALID, f"{name} must be a 4-d {self.torch_dtype} tensor on {self.device}")
+        (b, n, h, d), (sb, sn, sh, sd) = t.shape, t.stride()
+        if h != heads or d != self.shape.head_dim or b < 1 or n < 1 or like is not None and like != (b, n):
+            raise BaconError(ERR_INVALID, f"{name} has shape {tuple(t.shape)}")
+        step = sn if n > 1 else sb if b > 1 else h * d
+        if sd != 1 or h > 1 and sh != d or n > 1 and b > 1 and sb != n * sn:
+            raise BaconError(ERR_INVALID, f"{name} has strides {t.stride()}: a token's heads lie together, "
+                                          "tokens evenly spaced")
+        return t.data_ptr(), step
+
+    def _counts(self, counts, b, name="counts"):
+        import torch
+        return self._whole(counts, name, torch.int32, (b,))
+
+    # ---- entry points (same names as the C ABI)
+    def bacon_cache_clear(self, first_seq=0, num_seqs=None):
+        n = self.shape.max_batch - first_seq if num_seqs is None else num_seqs
+        self._call(lib().bacon_cache_clear, first_seq, n)
+
+    def bacon_cache_tables(self, batch: BatchLayout, budgets=None, reserve=0, free=None, first_seq=0, used=None):
+        """Lengths, tables and idx offsets of a prompt; budgets: None (the
+        batch's) or int32 [num_layers, >= batch, Hkv] on the device; free: None
+        or the int32 ids to take.  Returns the number of ids needed, int64 [1]
+        on the device (more than given: some pairs found no blocks)."""
+        import torch
+        s = self.shape
+        if used is None:
+            used = torch.empty(1, dtype=torch.int64, device=self.device)
+        nb = 0
+        if budgets is not None:
+            if budgets.dim() != 3 or budgets.shape[0] != s.num_layers or budgets.shape[2] != s.num_kv_heads:
+                raise BaconError(ERR_INVALID, f"budgets have shape {tuple(budgets.shape)}")
+            nb = budgets.shape[1]
+        self._call(lib().bacon_cache_tables, C.byref(batch.c), first_seq,
+                   self._whole(budgets, "budgets", torch.int32), nb, reserve,
+                   self._whole(free, "free", torch.int32), 0 if free is None else free.numel(),
+                   self._whole(used, "used", torch.int64, (1,)))
+        return used
+
+    def _layers(self, xs, name, dtype, shape):
+        """Host array of per-layer pointers: a list of tensors, or one with the layers first."""
+        import torch
+        if isinstance(xs, torch.Tensor):
+            if xs.dim() < 1 or shape is not None and tuple(xs.shape[1:]) != shape:
+                raise BaconError(ERR_INVALID, f"{name} has shape {tuple(xs.shape)}")
+            base = self._whole(xs, name, dtype)
+            step = xs.stride(0) * xs.element_size()
+            return (C.c_void_p * len(xs))(*[base + step * i for i in range(len(xs))])
+        return (C.c_void_p * len(xs))(*[self._whole(x, name, dtype, shape) for x in xs])
+
+    def bacon_cache_store(self, batch: BatchLayout, ks, vs, idxs=None, first_seq=0, first_layer=0):
+        """The kept rows of the layers first_layer, ..: ks, vs per-layer [T, Hkv,
+        d] (lists, or stacked), idxs per-layer idx, or None (rows 0, 1, 2, ..)."""
+        import torch
+        s = self.shape
+        n = len(ks)
+        if len(vs) != n or idxs is not None and len(idxs) != n or n < 1:
+            raise BaconError(ERR_INVALID, f"{n} layers of K, {len(vs)} of V")
+        rows = (batch.total, s.num_kv_heads, s.head_dim)
+        self._call(lib().bacon_cache_store, C.byref(batch.c), first_seq, first_layer, n,
+                   self._layers(ks, "k", self.torch_dtype, rows), self._layers(vs, "v", self.torch_dtype, rows),
+                   None if idxs is None else self._layers(idxs, "idx", torch.int32, None))
+
+    def bacon_cache_load(self, count, first_token=0, first_layer=0, num_layers=None, first_seq=0, num_seqs=None,
+                         out=None):
+        """The values held, rows first_token .. first_token + count - 1 of every
+        pair (first_token < 0: from its end): K, V [layers, seqs, Hkv, count, d]."""
+        import torch
+        s = self.shape
+        nl = s.num_layers - first_layer if num_layers is None else num_layers
+        ns = s.max_batch - first_seq if num_seqs is None else num_seqs
+        shape = (nl, ns, s.num_kv_heads, count, s.head_dim)
+        if out is None:
+            if min(shape) < 1:
+                raise BaconError(ERR_INVALID, f"a load of shape {shape}")
+            out = torch.empty((2, *shape), dtype=self.torch_dtype, device=self.device).unbind(0)
+        k, v = out
+        self._call(lib().bacon_cache_load, first_layer, nl, first_seq, ns, first_token, count,
+                   self._whole(k, "k_out", self.torch_dtype, shape), self._whole(v, "v_out", self.torch_dtype, shape))
+        return k, v
+
+    def bacon_cache_append(self, layer, k, v, counts=None, first_seq=0):
+        """Appends new tokens' rows k, v [num_seqs, tokens, Hkv, d]; counts
+        (int32 [num_seqs], device): each sequence's own number of them."""
+        hkv = self.shape.num_kv_heads
+        kp, ks = self._tokens(k, "k", hkv)
+        b, n = k.shape[:2]
+        vp, vs = self._tokens(v, "v", hkv, (b, n))
+        self._call(lib().bacon_cache_append, layer, first_seq, b, n, self._counts(counts, b), kp, ks, vp, vs)
+
+    def _attend_out(self, q, max_tokens, out, lse, want_lse, work):
+        import torch
+        b, n, hq, d = q.shape
+        if out is None:
+            out = torch.empty((b, n, hq, d), dtype=self.torch_dtype, device=self.device)
+        if lse is None and want_lse:
+            lse = torch.empty((b, n, hq), dtype=torch.float32, device=self.device)
+        need = lib().bacon_cache_work_bytes(self._h, b, n, max_tokens)
+        if need and work is None:
+            work = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return (out, lse, self._whole(out, "out", self.torch_dtype, (b, n, hq, d)),
+                self._whole(lse, "lse", torch.float32, (b, n, hq)),
+                self._whole(work, "work", torch.uint8), work.numel() if need else 0)
+
+    def bacon_cache_attend(self, layer, q, counts=None, max_tokens=None, first_seq=0, out=None, lse=None,
+                           want_lse=False, work=None):
+        """Attention of q [num_seqs, tokens, Hq, d] over the layer's cache:
+        out, or (out, lse [num_seqs, tokens, Hq]) with want_lse or lse given.
+        max_tokens: the longest length to expect (None: the table's)."""
+        qp, qs = self._tokens(q, "q", self.shape.num_q_heads)
+        b, n = q.shape[:2]
+        most = max_tokens or 0
+        out, lse, *ptrs = self._attend_out(q, most, out, lse, want_lse, work)
+        self._call(lib().bacon_cache_attend, layer, first_seq, b, n, self._counts(counts, b), qp, qs, most, *ptrs)
+        return out if lse is None else (out, lse)
+
+    def bacon_cache_step(self, layer, q, k, v, counts=None, max_tokens=None, first_seq=0, out=None, lse=None,
+                         want_lse=False, work=None):
+        """bacon_cache_append(k, v), then bacon_cache_attend(q) over the grown cache."""
+        s = self.shape
+        qp, qs = self._tokens(q, "q", s.num_q_heads)
+        b, n = q.shape[:2]
+        kp, ks = self._tokens(k, "k", s.num_kv_heads, (b, n))
+        vp, vs = self._tokens(v, "v", s.num_kv_heads, (b, n))
+        most = max_tokens or 0
+        out, lse, *ptrs = self._attend_out(q, most, out, lse, want_lse, work)
+        self._call(lib().bacon_cache_step, layer, first_seq, b, n, self._counts(counts, b), qp, qs, kp, ks, vp, vs,
+                   most, *ptrs)
+        return out if lse is None else (out, lse)
+
+    def bacon_cache_advance(self, delta=0, counts=None, first_layer=0, num_layers=None, first_seq=0, num_seqs=None):
+        """Moves the lengths by delta, or by counts (int32 [num_seqs], device; may be negative)."""
+        nl = self.shape.num_layers - first_layer if num_layers is None else num_layers
+        ns = self.shape.max_batch - first_seq if num_seqs is None else num_seqs
+        self._call(lib().bacon_cache_advance, first_layer, nl, first_seq, ns, delta, self._counts(counts, ns))
+
+    def bacon_cache_errors(self) -> int:
+        """The error word (CACHE_* bits); waits for the device."""
+        return int(lib().bacon_cache_errors(self._h))

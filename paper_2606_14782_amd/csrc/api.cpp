@@ -11,16 +11,17 @@
 #include <vector>
 
 #include "../../include/bacon.h"
+#include "error.h"
 #include "internal.h"
 #include "schedule.h"
 
 using namespace bacon;
 
 namespace {
-
 thread_local std::string g_err;
+}  // namespace
 
-bacon_status fail(bacon_status s, const char *fmt, ...) {
+bacon_status bacon::fail(bacon_status s, const char *fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -29,6 +30,8 @@ bacon_status fail(bacon_status s, const char *fmt, ...) {
   g_err = buf;
   return s;
 }
+
+namespace {
 
 bacon_status hip_fail(hipError_t e, const char *what) {
   return fail(BACON_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
