@@ -376,7 +376,8 @@ int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
  *   table         [num_layers, max_batch, Hkv, max_blocks] int32
  *   scales        [num_blocks, 2] float32, K then V
  *   codes         [num_blocks, 2, block_tokens * d] e4m3 bytes: K as
- *                 [block_tokens, d], V transposed as [d, block_tokens]
+ *                 [block_tokens, d], V in groups of 16 tokens, each
+ *                 transposed: [block_tokens / 16, d, 16]
  *   errors        one uint32 word
  *
  * Calls name the sequences first_seq .. first_seq + num_seqs - 1 (or + batch

@@ -8,7 +8,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbacon.so")
-SOURCES = ["kernels.hip", "noalloc.hip", "cache.hip", "api.cpp", "cache_api.cpp"]
+SOURCES = ["kernels.hip", "noalloc.hip", "cache.hip", "cache_attend.hip", "api.cpp", "cache_api.cpp"]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -71,7 +71,19 @@ struct CacheStepArgs {
   void *out;
   float *lse;              // optional
   float scale_log2;        // log2(e) / sqrt(d)
+  // Division of a pair's rows: `splits` workgroups of `chunk` rows (more where
+  // the pair is longer); with several, each leaves its part in work.
+  int splits, chunk;
+  float2 *part_ml;         // [pairs, splits, R] maximum (log2 units) and sum
+  float *part_o;           // [pairs, splits, R, d] sums weighted by 2^(logit - maximum)
 };
+
+// How an attend of q_rows query rows per pair is divided.
+struct CachePlan {
+  int splits, chunk;
+  size_t ml_bytes, bytes;  // of the work buffer: part_ml, then part_o
+};
+CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens);
 
 struct CacheMoveArgs {
   CacheDev c;

@@ -1,130 +1,14 @@
 // gfx950 kernels of the 8-bit cache: block tables from the budgets, the kept
-// rows quantised into blocks and read back, new tokens' rows, and attention
-// over a layer's cache.  include/bacon.h states the layouts and the numbers.
+// rows quantised into blocks and read back, and new tokens' rows.
+// include/bacon.h states the layouts and the numbers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <math.h>
-#include <stdint.h>
 
-#include "../../include/bacon.h"
-#include "cache.h"
+#include "cache_dev.h"
 
 namespace bacon {
 namespace {
-
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr float kTop = 448.f;          // largest e4m3 value
-constexpr float kLn2f = 0.69314718055994531f;
-
-__device__ __forceinline__ float bf16_float(unsigned bits) { return __uint_as_float(bits << 16); }
-
-// bfloat16 bits of x, rounded to nearest, ties to even (x finite).
-__device__ __forceinline__ unsigned float_bf16(float x) {
-  const unsigned u = __float_as_uint(x);
-  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-}
-
-// 2^e as a float, -126 <= e <= 127.
-__device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
-
-// The scale of a block whose largest magnitude is a: 2^e, e the smallest
-// integer with a <= 448 2^e = 1.75 2^(e+8), within the bounds.
-__device__ __forceinline__ float block_scale(float a) {
-  const unsigned u = __float_as_uint(a);
-  int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-  e = e < kCacheLow ? kCacheLow : e > kCacheHigh ? kCacheHigh : e;
-  return two_to(e);
-}
-
-// Four values, already divided by their scale, as e4m3 bytes.
-__device__ __forceinline__ unsigned pack4(float a, float b, float c, float d) {
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
-  return (unsigned)r;
-}
-
-__device__ __forceinline__ void unpack4(unsigned w, float (&x)[4]) {
-  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
-  const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-  x[0] = lo[0];
-  x[1] = lo[1];
-  x[2] = hi[0];
-  x[3] = hi[1];
-}
-
-__device__ __forceinline__ int64_t pair_of(const CacheDev &c, int layer, int seq, int h) {
-  return ((int64_t)layer * c.B + seq) * c.Hkv + h;
-}
-
-// A pair's length, held to its table.
-__device__ __forceinline__ int pair_len(const CacheDev &c, int64_t pair) {
-  const int n = c.lens[pair], cap = c.max_blocks << c.bt_log;
-  return n < 0 ? 0 : n > cap ? cap : n;
-}
-
-// Id of the pair's block i, or -1 where the table holds none of the pool's.
-__device__ __forceinline__ int block_id(const CacheDev &c, int64_t pair, int i) {
-  const int id = i < c.max_blocks ? c.table[pair * c.max_blocks + i] : -1;
-  return (unsigned)id < (unsigned)c.num_blocks ? id : -1;
-}
-
-template <int D>
-__device__ __forceinline__ uint8_t *block_codes(const CacheDev &c, int id, int kv) {
-  return c.codes + (((int64_t)id * 2 + kv) << c.bt_log) * D;
-}
-
-__device__ __forceinline__ float wave_max(float v) {
-  for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-  return v;
-}
-__device__ __forceinline__ float wave_add(float v) {
-  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-  return v;
-}
-
-// The largest v of a 256-thread workgroup; red holds 4 floats, free again
-// after the next barrier.
-__device__ __forceinline__ float block_max(float v, float *red) {
-  v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-}
-
-template <bool BF16>
-__device__ __forceinline__ float load_elem(const void *p, int64_t i) {
-  if constexpr (BF16) return bf16_float(static_cast<const uint16_t *>(p)[i]);
-  return static_cast<const float *>(p)[i];
-}
-template <bool BF16>
-__device__ __forceinline__ void store_elem(void *p, int64_t i, float x) {
-  if constexpr (BF16)
-    static_cast<uint16_t *>(p)[i] = (uint16_t)float_bf16(x);
-  else
-    static_cast<float *>(p)[i] = x;
-}
-
-// Eight consecutive elements as floats (i a multiple of 8).
-template <bool BF16>
-__device__ __forceinline__ void load8(const void *p, int64_t i, float (&x)[8]) {
-  if constexpr (BF16) {
-    const u32x4 w = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + i);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = bf16_float(w[j] & 0xFFFFu);
-      x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-    }
-  } else {
-    const float4 a = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i);
-    const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  }
-}
 
 // ------------------------------------------------------------------- clear
 
@@ -297,7 +181,7 @@ __global__ __launch_bounds__(256) void k_cache_store(CacheStoreArgs a, int per_p
         *reinterpret_cast<u32x2 *>(dst + r * D + (t % TR) * 8) = w;
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) tile[((t % TR) * 8 + j) * bt + r] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+        for (int j = 0; j < 8; ++j) tile[v_at<D>(r, (t % TR) * 8 + j)] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
       }
     }
     if (kv == 1) {
@@ -328,7 +212,7 @@ __global__ __launch_bounds__(256) void k_cache_load(CacheLoadArgs a, int64_t row
     if (pos >= 0 && pos < len) {
       const int id = block_id(c, pair, (int)(pos >> c.bt_log)), at = (int)pos & ((1 << c.bt_log) - 1);
       if (id >= 0) {
-        const unsigned kc = block_codes<D>(c, id, 0)[at * D + dim], vc = block_codes<D>(c, id, 1)[(dim << c.bt_log) + at];
+        const unsigned kc = block_codes<D>(c, id, 0)[at * D + dim], vc = block_codes<D>(c, id, 1)[v_at<D>(at, dim)];
         k = __builtin_amdgcn_cvt_f32_fp8((int)kc, 0) * c.scales[(int64_t)id * 2];
         v = __builtin_amdgcn_cvt_f32_fp8((int)vc, 0) * c.scales[(int64_t)id * 2 + 1];
       } else if (dim == 0) {
@@ -389,70 +273,11 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheStepArgs a) {
         const int r = e / D, dim = e % D;
         const float x = load_elem<BF16>(src, (row0 + r) * stride + h * D + dim) * inv;
         const unsigned w = pack4(x, 0.f, 0.f, 0.f);
-        dst[kv ? (dim << c.bt_log) + old + r : (old + r) * D + dim] = (uint8_t)w;
+        dst[kv ? v_at<D>(old + r, dim) : (old + r) * D + dim] = (uint8_t)w;
       }
     }
   }
   if (t == 0) c.lens[pair] = len + count;
-}
-
-// ------------------------------------------------------------------ attend
-// One workgroup per query row: logits of 256 rows at a time, the running
-// maximum and sum of the softmax, a thread per dimension for the output.
-template <bool BF16, int D>
-__global__ __launch_bounds__(256) void k_cache_attend(CacheStepArgs a) {
-  constexpr int PARTS = 256 / D;
-  __shared__ float red[4], q[D], p[256], part[256];
-  const CacheDev &c = a.c;
-  const int t = threadIdx.x, G = c.Hq / c.Hkv, bt = 1 << c.bt_log;
-  const int hq = blockIdx.x % c.Hq, j = blockIdx.x / c.Hq % a.tokens, b = blockIdx.x / c.Hq / a.tokens;
-  const int64_t pair = pair_of(c, a.layer, a.first_seq + b, hq / G), row = (int64_t)b * a.tokens + j;
-  int count = a.tokens;
-  if (a.counts) count = min(max(a.counts[b], 0), a.tokens);
-  const int end = j < count ? pair_len(c, pair) - (count - 1 - j) : 0;
-  if (t < D) q[t] = load_elem<BF16>(a.q, row * a.q_stride + hq * D + t) * a.scale_log2;
-  __syncthreads();
-  float top = -1e30f, sum = 0.f, acc = 0.f;
-  for (int base = 0; base < end; base += 256) {
-    const int pos = base + t;
-    const int id = pos < end ? block_id(c, pair, pos >> c.bt_log) : -1;
-    if (pos < end && id < 0) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
-    float s = -INFINITY;
-    if (id >= 0) {
-      const unsigned *w = reinterpret_cast<const unsigned *>(block_codes<D>(c, id, 0) + (pos & (bt - 1)) * D);
-      s = 0.f;
-      for (int i = 0; i < D / 4; ++i) {
-        float x[4];
-        unpack4(w[i], x);
-        for (int e = 0; e < 4; ++e) s = fmaf(x[e], q[4 * i + e], s);
-      }
-      s *= c.scales[(int64_t)id * 2];
-    }
-    const float most = fmaxf(top, block_max(s, red)), f = exp2f(top - most);
-    top = most;
-    p[t] = exp2f(s - top);
-    sum = sum * f + p[t];
-    acc *= f;
-    __syncthreads();
-    const int dim = t % D;
-    for (int i = t / D; i < 256 && base + i < end; i += PARTS) {
-      const int at = base + i, vid = block_id(c, pair, at >> c.bt_log);
-      if (vid < 0) continue;
-      const unsigned code = block_codes<D>(c, vid, 1)[(dim << c.bt_log) + (at & (bt - 1))];
-      acc = fmaf(p[i] * c.scales[(int64_t)vid * 2 + 1], __builtin_amdgcn_cvt_f32_fp8((int)code, 0), acc);
-    }
-    __syncthreads();
-  }
-  part[t] = acc;
-  sum = wave_add(sum);
-  if ((t & 63) == 0) red[t >> 6] = sum;
-  __syncthreads();
-  sum = red[0] + red[1] + red[2] + red[3];
-  if (t < D) {
-    for (int i = 1; i < PARTS; ++i) acc += part[i * D + t];
-    store_elem<BF16>(a.out, (row * c.Hq + hq) * D + t, sum > 0.f ? acc / sum : 0.f);
-  }
-  if (t == 0 && a.lse) a.lse[row * c.Hq + hq] = sum > 0.f ? (top + log2f(sum)) * kLn2f : -INFINITY;
 }
 
 // ----------------------------------------------------------------- advance
@@ -517,12 +342,6 @@ hipError_t launch_cache_load(const CacheLoadArgs &a, bool bf16, int head_dim, hi
 hipError_t launch_cache_append(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s) {
   const dim3 grid((unsigned)(a.num_seqs * a.c.Hkv));
   CACHE_LAUNCH(k_cache_append, grid, s, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_cache_attend(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s) {
-  const dim3 grid((unsigned)(a.num_seqs * a.tokens * a.c.Hq));
-  CACHE_LAUNCH(k_cache_attend, grid, s, a);
   return hipGetLastError();
 }
 

@@ -218,6 +218,26 @@ bacon_status check_attend(const bacon_cache *c, int layer, int first, int n, int
   return check_cleared(c, first, n);
 }
 
+CachePlan plan_of(const bacon_cache *c, int num_seqs, int tokens, int max_tokens) {
+  const int most = max_tokens ? std::min(max_tokens, capacity(c)) : capacity(c);
+  return cache_plan(num_seqs * c->shape.num_kv_heads, c->shape.num_q_heads / c->shape.num_kv_heads * tokens,
+                    c->shape.head_dim, most);
+}
+
+// The query side of an attend.
+void set_query(CacheStepArgs *a, const bacon_cache *c, const void *q, int64_t q_stride, int max_tokens, void *out,
+               float *lse, void *work) {
+  const CachePlan p = plan_of(c, a->num_seqs, a->tokens, max_tokens);
+  a->q = q;
+  a->q_stride = q_stride;
+  a->out = out;
+  a->lse = lse;
+  a->splits = p.splits;
+  a->chunk = p.chunk;
+  a->part_ml = static_cast<float2 *>(work);
+  a->part_o = reinterpret_cast<float *>(static_cast<char *>(work) + p.ml_bytes);
+}
+
 CacheStepArgs step_args(const bacon_cache *c, int layer, int first, int n, int tokens, const int32_t *d_counts) {
   CacheStepArgs a{};
   a.c = device_of(c);
@@ -380,7 +400,12 @@ bacon_status bacon_cache_append(bacon_cache *c, int32_t layer, int32_t first_seq
                   "cache_append");
 }
 
-size_t bacon_cache_work_bytes(const bacon_cache *, int32_t, int32_t, int32_t) { return 0; }
+size_t bacon_cache_work_bytes(const bacon_cache *c, int32_t num_seqs, int32_t tokens, int32_t max_tokens) {
+  if (!c || num_seqs < 1 || num_seqs > c->shape.max_batch || tokens < 1 || tokens > kCacheMaxTokens ||
+      max_tokens < 0 || c->shape.num_q_heads / c->shape.num_kv_heads * tokens > kCacheMaxQRows)
+    return 0;
+  return plan_of(c, num_seqs, tokens, max_tokens).bytes;
+}
 
 bacon_status bacon_cache_attend(bacon_cache *c, int32_t layer, int32_t first_seq, int32_t num_seqs, int32_t tokens,
                                 const int32_t *d_counts, const void *d_q, int64_t q_stride, int32_t max_tokens,
@@ -388,10 +413,7 @@ bacon_status bacon_cache_attend(bacon_cache *c, int32_t layer, int32_t first_seq
   TRY(check_attend(c, layer, first_seq, num_seqs, tokens, d_counts, d_q, q_stride, max_tokens, d_out, d_lse, d_work,
                    work_bytes));
   CacheStepArgs a = step_args(c, layer, first_seq, num_seqs, tokens, d_counts);
-  a.q = d_q;
-  a.q_stride = q_stride;
-  a.out = d_out;
-  a.lse = d_lse;
+  set_query(&a, c, d_q, q_stride, max_tokens, d_out, d_lse, d_work);
   return launched(launch_cache_attend(a, c->shape.dtype == BACON_BF16, c->shape.head_dim,
                                       static_cast<hipStream_t>(stream)),
                   "cache_attend");

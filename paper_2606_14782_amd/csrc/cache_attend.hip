@@ -1,0 +1,408 @@
+// Attention over the 8-bit cache on gfx950.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "cache_dev.h"
+
+namespace bacon {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// A wave takes tiles of 64 rows.  Both products are 16x16x32 bf16 MFMAs with
+// the rows of K, then the dimensions of V, along M and 16 query rows along N:
+//
+//   S^T = K Q^T    lane (n = lane & 15, g = lane >> 4) holds, of query n, the
+//                  logits of four rows of each of the four steps t
+//   O^T = V^T P^T  lane (n, g) gives 8 rows' weights of query n to a step
+//
+// Row 16 g + 4 t + i of the tile is M index 4 g + i of step t, so a lane's 16 weights belong to rows
+// 16 g .. 16 g + 15, which are what it gives to the second product, without an
+// exchange between lanes, and V's 16-byte groups are read in that order.
+// The codes become bf16 in registers, exactly, with the block's scale applied by the
+// conversion.
+template <int D>
+struct KvTile {
+  u32x4 k[4][D / 64], v[D / 16];
+  float ks, vs;
+};
+
+// Block ids of a tile: of the rows this lane loads K of (group (lane & 15) >> 2)
+// and of those it loads V of (group lane >> 4); -1 where there is none.
+struct TileIds {
+  int k, v;
+};
+
+__device__ __forceinline__ TileIds tile_ids(const CacheDev &c, const int32_t *row, int base, int total) {
+  const int lane = threadIdx.x & 63;
+  const int pk = base + 16 * ((lane & 15) >> 2), pv = base + 16 * (lane >> 4);
+  TileIds t;
+  t.k = pk < total ? row[pk >> c.bt_log] : -1;
+  t.v = pv < total ? row[pv >> c.bt_log] : -1;
+  return t;
+}
+
+template <int D>
+__device__ __forceinline__ void load_tile(const CacheDev &c, TileIds ids, int base, KvTile<D> &x) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, in = (1 << c.bt_log) - 1;
+  // an absent block's rows are masked: any address of the pool will do
+  const int ik = (unsigned)ids.k < (unsigned)c.num_blocks ? ids.k : 0;
+  const int iv = (unsigned)ids.v < (unsigned)c.num_blocks ? ids.v : 0;
+  const int rk = ((base + 16 * (m >> 2)) & in) + (m & 3), rv = (base + 16 * g) & in;
+  const uint8_t *k = block_codes<D>(c, ik, 0) + rk * D + 16 * g;
+  const uint8_t *v = block_codes<D>(c, iv, 1) + rv * D + 16 * m;
+  x.ks = c.scales[(int64_t)ik * 2];
+  x.vs = c.scales[(int64_t)iv * 2 + 1];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) x.k[t][j] = *reinterpret_cast<const u32x4 *>(k + 4 * t * D + 64 * j);
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) x.v[e] = *reinterpret_cast<const u32x4 *>(v + 256 * e);
+}
+
+// Eight codes as bf16 values times the scale (exact).
+__device__ __forceinline__ bf16x8 dequant(unsigned lo, unsigned hi, float scale) {
+  bf16x8 r;
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1];
+  r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
+  return r;
+}
+
+// Eight floats as NP bf16 parts whose sum they are, to 8 bits more a part.
+template <int NP>
+__device__ __forceinline__ void split8(float (&x)[8], bf16x8 (&part)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      part[p][i] = (__bf16)x[i];
+      if (p + 1 < NP) x[i] -= (float)part[p][i];
+    }
+}
+
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float xor16_32_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+
+// Waves of a workgroup: 8 fill a compute unit at 256 registers a lane; more
+// query rows hold more outputs and take 4 waves of up to 512.
+constexpr int max_waves(int nt) { return nt == 1 ? 8 : 4; }
+
+constexpr float kFloor = -1e30f;       // maximum of no logits
+
+template <int D>
+constexpr int o_pitch() { return D + 4; }
+
+template <bool BF16, int D, int NT>
+__global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepArgs a) {
+  constexpr int QP = BF16 ? 1 : 3;     // parts of a query: bf16 is one; fp32 needs three for its 24 bits
+  constexpr int PP = BF16 ? 2 : 3;     // parts of a weight: one would add 2^-9 to a bf16 output's own 2^-9
+  constexpr int KS = D / 32;
+  extern __shared__ __align__(16) char lds[];
+  bf16x8 *q_lds = reinterpret_cast<bf16x8 *>(lds);           // [NT][KS][QP][64]
+  const CacheDev &c = a.c;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, waves = blockDim.x >> 6;
+  const int m = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x % a.splits, bh = blockIdx.x / a.splits;
+  const int b = bh / c.Hkv, h = bh - b * c.Hkv;
+  const int G = c.Hq / c.Hkv, R = G * a.tokens;
+  const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
+  const int32_t *row = c.table + pair * c.max_blocks;
+  const int total = pair_len(c, pair);
+  int count = a.tokens;
+  if (a.counts) count = min(max(a.counts[b], 0), a.tokens);
+  // this workgroup's rows
+  const int chunk = max(a.chunk, ((total + a.splits - 1) / a.splits + 63) & ~63);
+  const int from = split * chunk, to = min(total, from + chunk);
+  const int first_end = total - (count - 1);                 // of the first query: below it nothing is masked
+
+  // queries: lane (n, g) holds 8 dimensions of query n for each step of 32
+  for (int i = wave; i < NT * KS; i += waves) {
+    const int nt = i / KS, s = i - nt * KS, r = nt * 16 + m;
+    float x[8] = {};
+    const int j = r / G, hq = h * G + (r - j * G);
+    if (r < R)
+      load8<BF16>(a.q, ((int64_t)b * a.tokens + j) * a.q_stride + hq * D + 64 * (s >> 1) + 16 * g + 8 * (s & 1), x);
+    bf16x8 part[QP];
+    split8<QP>(x, part);
+#pragma unroll
+    for (int p = 0; p < QP; ++p) q_lds[(i * QP + p) * 64 + lane] = part[p];
+  }
+  int end[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = nt * 16 + m, j = r / G;
+    end[nt] = r < R && j < count ? max(0, total - (count - 1 - j)) : 0;
+  }
+  __syncthreads();
+
+  f32x4 o[NT][D / 16];
+  float mx[NT], sum[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    mx[nt] = kFloor;
+    sum[nt] = 0.f;
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) o[nt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const auto work = [&](KvTile<D> &x, TileIds ids, int base) {
+    const bool here = (unsigned)ids.v < (unsigned)c.num_blocks;
+    const bool masked = base + 64 > first_end || !__all(here);
+    if (masked) {
+      // rows that hold nothing: their codes may be any bytes
+      const int n = here ? total - (base + 16 * g) : 0;
+      if (!here && base + 16 * g < total) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
+      if (n < 16) {
+        if (n <= 0) x.vs = 1.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int left = n - 4 * w;
+          const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+          for (int e = 0; e < D / 16; ++e) x.v[e][w] &= keep;
+        }
+      }
+    }
+    f32x4 s[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[nt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      bf16x8 kk[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kk[i] = dequant(x.k[i][k >> 1][2 * (k & 1)], x.k[i][k >> 1][2 * (k & 1) + 1], x.ks);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int p = 0; p < QP; ++p) {
+          const bf16x8 qq = q_lds[((nt * KS + k) * QP + p) * 64 + lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[nt][i] = mfma(kk[i], qq, s[nt][i]);
+        }
+    }
+    bf16x8 w[NT][2][PP];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (masked) {
+        const int n = here ? end[nt] - (base + 16 * g) : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (4 * i + e >= n) s[nt][i][e] = -INFINITY;
+      }
+      float top = s[nt][0][0];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[nt][i][e]);
+      top = fmaxf(mx[nt], xor16_32_max(top) * a.scale_log2);
+      if (__any(top > mx[nt])) {
+        const float f = __builtin_amdgcn_exp2f(mx[nt] - top);
+        mx[nt] = top;
+        sum[nt] *= f;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) o[nt][e] *= f;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float x8[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x8[e] = __builtin_amdgcn_exp2f(fmaf(s[nt][2 * u + (e >> 2)][e & 3], a.scale_log2, -mx[nt]));
+          sum[nt] += x8[e];
+        }
+        split8<PP>(x8, w[nt][u]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 vv = dequant(x.v[e][2 * u], x.v[e][2 * u + 1], x.vs);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int p = 0; p < PP; ++p) o[nt][e] = mfma(vv, w[nt][u][p], o[nt][e]);
+      }
+  };
+
+  // tiles of this wave, the next one's codes and the one after's ids on their way
+  const int step = 64 * waves;
+  int base = from + 64 * wave;
+  if (base < to) {
+    KvTile<D> x, y;
+    TileIds ix = tile_ids(c, row, base, to), iy = tile_ids(c, row, base + step, to);
+    load_tile<D>(c, ix, base, x);
+    for (;;) {
+      if (base + step < to) load_tile<D>(c, iy, base + step, y);
+      const TileIds ix2 = tile_ids(c, row, base + 2 * step, to);
+      work(x, ix, base);
+      base += step;
+      if (base >= to) break;
+      ix = ix2;
+      if (base + step < to) load_tile<D>(c, ix, base + step, x);
+      const TileIds iy2 = tile_ids(c, row, base + 2 * step, to);
+      work(y, iy, base);
+      base += step;
+      if (base >= to) break;
+      iy = iy2;
+    }
+  }
+
+  // join the waves, 16 query rows at a time
+  float *ml = reinterpret_cast<float *>(lds);                // [waves][16][2]
+  float *oo = ml + waves * 32;                               // [waves][16][o_pitch]
+  constexpr int P = o_pitch<D>();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float l = sum[nt] + __shfl_xor(sum[nt], 16);
+    l += __shfl_xor(l, 32);
+    __syncthreads();                                         // the queries, or the last rows, are done with
+    if (g == 0) {
+      ml[(wave * 16 + m) * 2] = mx[nt];
+      ml[(wave * 16 + m) * 2 + 1] = l;
+    }
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e)
+      *reinterpret_cast<f32x4 *>(oo + (wave * 16 + m) * P + 16 * e + 4 * g) = o[nt][e];
+    __syncthreads();
+    for (int i = t; i < 16 * (D / 4); i += blockDim.x) {
+      const int n = i / (D / 4), dim = i % (D / 4) * 4, r = nt * 16 + n;
+      if (r >= R) continue;
+      float top = kFloor;
+      for (int w = 0; w < waves; ++w) top = fmaxf(top, ml[(w * 16 + n) * 2]);
+      float l = 0.f;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < waves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + n) * 2] - top);
+        l += f * ml[(w * 16 + n) * 2 + 1];
+        acc += f * *reinterpret_cast<const f32x4 *>(oo + (w * 16 + n) * P + dim);
+      }
+      const int j = r / G;
+      const bool none = j >= count || !(l > 0.f);
+      if (a.splits > 1) {
+        const int64_t at = ((int64_t)bh * a.splits + split) * R + r;
+        if (dim == 0) a.part_ml[at] = make_float2(top, none ? 0.f : l);
+        *reinterpret_cast<f32x4 *>(a.part_o + at * D + dim) = acc;
+      } else {
+        const int64_t at = ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G);
+        const float inv = none ? 0.f : 1.f / l;
+        f32x4 y = acc * inv;
+        if (none) y = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (BF16) {
+          const u32x2 u = {float_bf16(y[0]) | float_bf16(y[1]) << 16, float_bf16(y[2]) | float_bf16(y[3]) << 16};
+          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + at * D + dim) = u;
+        } else {
+          *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at * D + dim) = y;
+        }
+        if (dim == 0 && a.lse) a.lse[at] = none ? -INFINITY : (top + __log2f(l)) * kLn2f;
+      }
+    }
+  }
+}
+
+// Joins the parts of one query row: 256 threads, D / 4 of them a part, the
+// parts divided among the others.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
+  constexpr int TR = D / 4, SP = 256 / TR;
+  __shared__ float red[4];
+  __shared__ f32x4 acc_lds[256];
+  const CacheDev &c = a.c;
+  const int t = threadIdx.x, G = c.Hq / c.Hkv, R = G * a.tokens;
+  const int r = blockIdx.x % R, bh = blockIdx.x / R;
+  const int b = bh / c.Hkv, h = bh - b * c.Hkv, j = r / G;
+  const float2 *ml = a.part_ml + (int64_t)bh * a.splits * R + r;
+  float top = kFloor;
+  for (int i = t; i < a.splits; i += 256) top = fmaxf(top, ml[(int64_t)i * R].x);
+  top = block_max(top, red);
+  float l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i = t / TR; i < a.splits; i += SP) {
+    const float2 x = ml[(int64_t)i * R];
+    if (!(x.y > 0.f)) continue;
+    const float f = __builtin_amdgcn_exp2f(x.x - top);
+    l += f * x.y;
+    acc += f * *reinterpret_cast<const f32x4 *>(a.part_o + (((int64_t)bh * a.splits + i) * R + r) * D + t % TR * 4);
+  }
+  __shared__ float l_lds[SP];
+  acc_lds[t] = acc;
+  if (t % TR == 0) l_lds[t / TR] = l;
+  __syncthreads();
+  if (t >= TR) return;
+  l = l_lds[0];
+  for (int i = 1; i < SP; ++i) {
+    l += l_lds[i];
+    acc += acc_lds[i * TR + t];
+  }
+  const bool none = !(l > 0.f);
+  const int64_t at = ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G);
+  f32x4 y = acc * (none ? 0.f : 1.f / l);
+  if constexpr (BF16) {
+    const u32x2 u = {float_bf16(y[0]) | float_bf16(y[1]) << 16, float_bf16(y[2]) | float_bf16(y[3]) << 16};
+    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + at * D + t * 4) = u;
+  } else {
+    *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at * D + t * 4) = y;
+  }
+  if (t == 0 && a.lse) a.lse[at] = none ? -INFINITY : (top + __log2f(l)) * kLn2f;
+}
+
+template <bool BF16, int D, int NT>
+hipError_t attend(const CacheStepArgs &a, int most, hipStream_t s) {
+  const int pairs = a.num_seqs * a.c.Hkv;
+  const int waves = NT == 1 && most > 256 && a.splits == 1 ? 8 : 4;
+  const int q = NT * (D / 32) * (BF16 ? 1 : 3) * 1024, o = waves * (128 + 64 * o_pitch<D>());
+  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(pairs * a.splits), dim3(64 * waves), std::max(q, o), s, a);
+  if (a.splits > 1) {
+    const int R = a.c.Hq / a.c.Hkv * a.tokens;
+    hipLaunchKernelGGL((k_cache_join<BF16, D>), dim3(pairs * R), dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens) {
+  CachePlan p{};
+  // two workgroups a compute unit, each of at least 512 rows
+  const int64_t want = std::max<int64_t>(1, 1024 / pairs);
+  const int64_t by_rows = std::max<int64_t>(1, max_tokens / 512);
+  p.splits = (int)std::min(want, by_rows);
+  p.chunk = (int)((((int64_t)max_tokens + p.splits - 1) / p.splits + 63) / 64 * 64);
+  if (p.splits > 1) {
+    const size_t parts = (size_t)pairs * p.splits * q_rows;
+    p.ml_bytes = (parts * sizeof(float2) + 255) / 256 * 256;
+    p.bytes = p.ml_bytes + parts * head_dim * sizeof(float);
+  }
+  return p;
+}
+
+hipError_t launch_cache_attend(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s) {
+  const int R = a.c.Hq / a.c.Hkv * a.tokens, most = a.chunk * a.splits;
+#define ATTEND(nt)                                                                   \
+  return bf16 ? (head_dim == 128 ? attend<true, 128, nt>(a, most, s) : attend<true, 64, nt>(a, most, s)) \
+              : (head_dim == 128 ? attend<false, 128, nt>(a, most, s) : attend<false, 64, nt>(a, most, s))
+  if (R <= 16) ATTEND(1);
+  if (R <= 32) ATTEND(2);
+  ATTEND(4);
+#undef ATTEND
+}
+
+}  // namespace bacon

@@ -1,0 +1,136 @@
+// Device helpers shared by the kernels of the 8-bit cache.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/bacon.h"
+#include "cache.h"
+
+namespace bacon {
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kTop = 448.f;          // largest e4m3 value
+constexpr float kLn2f = 0.69314718055994531f;
+
+__device__ __forceinline__ float bf16_float(unsigned bits) { return __uint_as_float(bits << 16); }
+
+// bfloat16 bits of x, rounded to nearest, ties to even (x finite).
+__device__ __forceinline__ unsigned float_bf16(float x) {
+  const unsigned u = __float_as_uint(x);
+  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+}
+
+// 2^e as a float, -126 <= e <= 127.
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+
+// The scale of a block whose largest magnitude is a: 2^e, e the smallest
+// integer with a <= 448 2^e = 1.75 2^(e+8), within the bounds.
+__device__ __forceinline__ float block_scale(float a) {
+  const unsigned u = __float_as_uint(a);
+  int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  e = e < kCacheLow ? kCacheLow : e > kCacheHigh ? kCacheHigh : e;
+  return two_to(e);
+}
+
+// Four values, already divided by their scale, as e4m3 bytes.
+__device__ __forceinline__ unsigned pack4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+  return (unsigned)r;
+}
+
+__device__ __forceinline__ void unpack4(unsigned w, float (&x)[4]) {
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+  const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  x[0] = lo[0];
+  x[1] = lo[1];
+  x[2] = hi[0];
+  x[3] = hi[1];
+}
+
+__device__ __forceinline__ int64_t pair_of(const CacheDev &c, int layer, int seq, int h) {
+  return ((int64_t)layer * c.B + seq) * c.Hkv + h;
+}
+
+// A pair's length, held to its table.
+__device__ __forceinline__ int pair_len(const CacheDev &c, int64_t pair) {
+  const int n = c.lens[pair], cap = c.max_blocks << c.bt_log;
+  return n < 0 ? 0 : n > cap ? cap : n;
+}
+
+// Id of the pair's block i, or -1 where the table holds none of the pool's.
+__device__ __forceinline__ int block_id(const CacheDev &c, int64_t pair, int i) {
+  const int id = i < c.max_blocks ? c.table[pair * c.max_blocks + i] : -1;
+  return (unsigned)id < (unsigned)c.num_blocks ? id : -1;
+}
+
+template <int D>
+__device__ __forceinline__ uint8_t *block_codes(const CacheDev &c, int id, int kv) {
+  return c.codes + (((int64_t)id * 2 + kv) << c.bt_log) * D;
+}
+
+// Byte of V's code (row r of its block, dimension dim): groups of 16 rows,
+// each transposed, so that one lane's 16-byte load holds 16 rows of a dimension
+// and the lanes of a wave read whole lines whatever the block's size.
+template <int D>
+__device__ __forceinline__ int v_at(int r, int dim) {
+  return ((r >> 4) * D + dim) * 16 + (r & 15);
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+  for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
+  return v;
+}
+__device__ __forceinline__ float wave_add(float v) {
+  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+  return v;
+}
+
+// The largest v of a 256-thread workgroup; red holds 4 floats, free again
+// after the next barrier.
+__device__ __forceinline__ float block_max(float v, float *red) {
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
+
+template <bool BF16>
+__device__ __forceinline__ float load_elem(const void *p, int64_t i) {
+  if constexpr (BF16) return bf16_float(static_cast<const uint16_t *>(p)[i]);
+  return static_cast<const float *>(p)[i];
+}
+template <bool BF16>
+__device__ __forceinline__ void store_elem(void *p, int64_t i, float x) {
+  if constexpr (BF16)
+    static_cast<uint16_t *>(p)[i] = (uint16_t)float_bf16(x);
+  else
+    static_cast<float *>(p)[i] = x;
+}
+
+// Eight consecutive elements as floats (i a multiple of 8).
+template <bool BF16>
+__device__ __forceinline__ void load8(const void *p, int64_t i, float (&x)[8]) {
+  if constexpr (BF16) {
+    const u32x4 w = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = bf16_float(w[j] & 0xFFFFu);
+      x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+    }
+  } else {
+    const float4 a = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i);
+    const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+}
+
+}  // namespace
+}  // namespace bacon
