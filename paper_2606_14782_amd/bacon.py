@@ -481,18 +481,18 @@ class Cache:
             self._h = C.c_void_p()
 
     # ---- checks and marshalling
-    def _stream(self):
-        import torch
-        return torch.cuda.current_stream(self.device).cuda_stream
-
     def _call(self, fn, *args):
         """fn on the cache's device and that device's current stream."""
         import torch
-        if torch.cuda.current_device() == self.device.index:
-            _check(fn(self._h, *args, self._stream()))
+        at = self.device.index
+        stream = torch._C._cuda_getCurrentRawStream(at)
+        if torch._C._cuda_getDevice() == at:
+            status = fn(self._h, *args, stream)
         else:
             with torch.cuda.device(self.device):
-                _check(fn(self._h, *args, self._stream()))
+                status = fn(self._h, *args, stream)
+        if status:
+            _check(status)
 
     def _whole(self, t, name, dtype, shape=None):
         """The pointer of a contiguous tensor of this dtype (and shape)."""

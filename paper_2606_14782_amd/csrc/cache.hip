@@ -225,59 +225,20 @@ __global__ __launch_bounds__(256) void k_cache_load(CacheLoadArgs a, int64_t row
 }
 
 // ------------------------------------------------------------------ append
-// One workgroup per pair, K then V, one touched block after the other.
+// One wave per pair, one touched block after the other.
 template <bool BF16, int D>
-__global__ __launch_bounds__(256) void k_cache_append(CacheStepArgs a) {
-  __shared__ float red[4];
+__global__ __launch_bounds__(64) void k_cache_append(CacheStepArgs a) {
   const CacheDev &c = a.c;
-  const int t = threadIdx.x, bt = 1 << c.bt_log, h = blockIdx.x % c.Hkv, b = blockIdx.x / c.Hkv;
+  const int h = blockIdx.x % c.Hkv, b = blockIdx.x / c.Hkv;
   const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
-  const int len = pair_len(c, pair);
-  int count = a.tokens;
-  if (a.counts) count = min(max(a.counts[b], 0), a.tokens);
-  if (count == 0) return;
-  const int b0 = len >> c.bt_log, b1 = (len + count - 1) >> c.bt_log;
-  for (int i = b0; i <= b1; ++i)
-    if (block_id(c, pair, i) < 0) {
-      if (t == 0) atomicOr(c.err, (unsigned)BACON_CACHE_NO_BLOCKS);
-      return;
-    }
-  for (int kv = 0; kv < 2; ++kv) {
-    const void *src = kv ? a.v : a.k;
-    const int64_t stride = kv ? a.v_stride : a.k_stride;
-    for (int i = b0; i <= b1; ++i) {
-      const int id = block_id(c, pair, i), base = i << c.bt_log;
-      const int from = max(len, base), m = min(len + count, base + bt) - from, old = from - base;
-      const int64_t row0 = (int64_t)b * a.tokens + (from - len);
-      uint8_t *dst = block_codes<D>(c, id, kv);
-      float top = 0.f;
-      for (int e = t; e < m * D; e += 256)
-        top = fmaxf(top, fabsf(load_elem<BF16>(src, (row0 + e / D) * stride + h * D + e % D)));
-      const float was = c.scales[(int64_t)id * 2 + kv];
-      __syncthreads();
-      float scale = block_scale(block_max(top, red));
-      if (old && scale < was) scale = was;
-      if (old && scale > was) {
-        const float f = was / scale;                         // a power of two: the product is exact
-        for (int e = t; e < bt * D / 4; e += 256) {
-          float x[4];
-          unsigned *w = reinterpret_cast<unsigned *>(dst) + e;
-          unpack4(*w, x);
-          *w = pack4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-        }
-      }
-      __syncthreads();                                       // the old codes are in place, the scale was read
-      if (t == 0) c.scales[(int64_t)id * 2 + kv] = scale;
-      const float inv = 1.f / scale;
-      for (int e = t; e < m * D; e += 256) {
-        const int r = e / D, dim = e % D;
-        const float x = load_elem<BF16>(src, (row0 + r) * stride + h * D + dim) * inv;
-        const unsigned w = pack4(x, 0.f, 0.f, 0.f);
-        dst[kv ? v_at<D>(old + r, dim) : (old + r) * D + dim] = (uint8_t)w;
-      }
-    }
+  const NewRows n = new_rows(a, pair, b, h, pair_len(c, pair), call_count(a, b));
+  if (n.count == 0) return;
+  if (!n.room) {
+    if (threadIdx.x == 0) atomicOr(c.err, (unsigned)BACON_CACHE_NO_BLOCKS);
+    return;
   }
-  if (t == 0) c.lens[pair] = len + count;
+  for (int i = n.b0; i <= n.b1; ++i) append_block<BF16, D>(a, pair, n, i);
+  if (threadIdx.x == 0) c.lens[pair] = n.len + n.count;
 }
 
 // ----------------------------------------------------------------- advance
@@ -297,16 +258,16 @@ __global__ __launch_bounds__(256) void k_cache_advance(CacheMoveArgs a) {
 int blocks_for(int64_t n, int per, int most) { return (int)std::max<int64_t>(1, std::min<int64_t>(most, (n + per - 1) / per)); }
 
 // The instance for a dtype and head size.
-#define CACHE_LAUNCH(kernel, grid, s, ...)                                             \
-  do {                                                                                 \
-    if (bf16 && head_dim == 128)                                                       \
-      hipLaunchKernelGGL((kernel<true, 128>), grid, dim3(256), 0, s, __VA_ARGS__);     \
-    else if (bf16)                                                                     \
-      hipLaunchKernelGGL((kernel<true, 64>), grid, dim3(256), 0, s, __VA_ARGS__);      \
-    else if (head_dim == 128)                                                          \
-      hipLaunchKernelGGL((kernel<false, 128>), grid, dim3(256), 0, s, __VA_ARGS__);    \
-    else                                                                               \
-      hipLaunchKernelGGL((kernel<false, 64>), grid, dim3(256), 0, s, __VA_ARGS__);     \
+#define CACHE_LAUNCH(kernel, grid, threads, s, ...)                                        \
+  do {                                                                                     \
+    if (bf16 && head_dim == 128)                                                           \
+      hipLaunchKernelGGL((kernel<true, 128>), grid, dim3(threads), 0, s, __VA_ARGS__);     \
+    else if (bf16)                                                                         \
+      hipLaunchKernelGGL((kernel<true, 64>), grid, dim3(threads), 0, s, __VA_ARGS__);      \
+    else if (head_dim == 128)                                                              \
+      hipLaunchKernelGGL((kernel<false, 128>), grid, dim3(threads), 0, s, __VA_ARGS__);    \
+    else                                                                                   \
+      hipLaunchKernelGGL((kernel<false, 64>), grid, dim3(threads), 0, s, __VA_ARGS__);     \
   } while (0)
 
 }  // namespace
@@ -328,20 +289,20 @@ hipError_t launch_cache_store(const CacheStoreArgs &a, bool bf16, int head_dim, 
   const int blocks = (most_rows + (1 << a.c.bt_log) - 1) >> a.c.bt_log;
   const int per_pair = (int)std::max<int64_t>(1, std::min<int64_t>(blocks, 8192 / std::min<int64_t>(pairs, 8192)));
   const dim3 grid((unsigned)(pairs * per_pair), 2);
-  CACHE_LAUNCH(k_cache_store, grid, s, a, per_pair);
+  CACHE_LAUNCH(k_cache_store, grid, 256, s, a, per_pair);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_load(const CacheLoadArgs &a, bool bf16, int head_dim, hipStream_t s) {
   const int64_t rows = (int64_t)a.layers * a.num_seqs * a.c.Hkv * a.count;
   const dim3 grid(blocks_for(rows * head_dim, 256, 1 << 20));
-  CACHE_LAUNCH(k_cache_load, grid, s, a, rows);
+  CACHE_LAUNCH(k_cache_load, grid, 256, s, a, rows);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_append(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s) {
   const dim3 grid((unsigned)(a.num_seqs * a.c.Hkv));
-  CACHE_LAUNCH(k_cache_append, grid, s, a);
+  CACHE_LAUNCH(k_cache_append, grid, 64, s, a);
   return hipGetLastError();
 }
 

@@ -426,9 +426,15 @@ bacon_status bacon_cache_step(bacon_cache *c, int32_t layer, int32_t first_seq, 
   TRY(check_append(c, layer, first_seq, num_seqs, tokens, d_counts, d_k, k_stride, d_v, v_stride));
   TRY(check_attend(c, layer, first_seq, num_seqs, tokens, d_counts, d_q, q_stride, max_tokens, d_out, d_lse, d_work,
                    work_bytes));
-  TRY(bacon_cache_append(c, layer, first_seq, num_seqs, tokens, d_counts, d_k, k_stride, d_v, v_stride, stream));
-  return bacon_cache_attend(c, layer, first_seq, num_seqs, tokens, d_counts, d_q, q_stride, max_tokens, d_out, d_lse,
-                            d_work, work_bytes, stream);
+  CacheStepArgs s = step_args(c, layer, first_seq, num_seqs, tokens, d_counts);
+  s.k = d_k;
+  s.v = d_v;
+  s.k_stride = k_stride;
+  s.v_stride = v_stride;
+  set_query(&s, c, d_q, q_stride, max_tokens, d_out, d_lse, d_work);
+  return launched(launch_cache_attend(s, c->shape.dtype == BACON_BF16, c->shape.head_dim,
+                                      static_cast<hipStream_t>(stream)),
+                  "cache_step");
 }
 
 bacon_status bacon_cache_advance(bacon_cache *c, int32_t first_layer, int32_t num_layers, int32_t first_seq,

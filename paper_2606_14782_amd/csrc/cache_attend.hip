@@ -36,12 +36,12 @@ struct TileIds {
   int k, v;
 };
 
-__device__ __forceinline__ TileIds tile_ids(const CacheDev &c, const int32_t *row, int base, int total) {
+__device__ __forceinline__ TileIds tile_ids(const CacheDev &c, const int32_t *row, int base, int to) {
   const int lane = threadIdx.x & 63;
   const int pk = base + 16 * ((lane & 15) >> 2), pv = base + 16 * (lane >> 4);
   TileIds t;
-  t.k = pk < total ? row[pk >> c.bt_log] : -1;
-  t.v = pv < total ? row[pv >> c.bt_log] : -1;
+  t.k = pk < to ? row[pk >> c.bt_log] : -1;
+  t.v = pv < to ? row[pv >> c.bt_log] : -1;
   return t;
 }
 
@@ -100,6 +100,8 @@ __device__ __forceinline__ float xor16_32_max(float v) {
 // Waves of a workgroup: 8 fill a compute unit at 256 registers a lane; more
 // query rows hold more outputs and take 4 waves of up to 512.
 constexpr int max_waves(int nt) { return nt == 1 ? 8 : 4; }
+// Whether a second tile's codes fit the registers beside the first's.
+constexpr bool prefetches(bool bf16, int d, int nt) { return d == 64 ? nt <= 2 || bf16 : bf16 ? nt <= 2 : nt == 1; }
 
 constexpr float kFloor = -1e30f;       // maximum of no logits
 
@@ -121,9 +123,15 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
   const int G = c.Hq / c.Hkv, R = G * a.tokens;
   const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
   const int32_t *row = c.table + pair * c.max_blocks;
-  const int total = pair_len(c, pair);
-  int count = a.tokens;
-  if (a.counts) count = min(max(a.counts[b], 0), a.tokens);
+  const int len = pair_len(c, pair), count = call_count(a, b);
+  const bool append = a.k && count > 0;
+  NewRows fresh{};
+  if (append) {
+    fresh = new_rows(a, pair, b, h, len, count);
+    if (!fresh.room && split == 0 && t == 0) atomicOr(c.err, (unsigned)BACON_CACHE_NO_BLOCKS);
+  }
+  const bool grow = append && fresh.room;
+  const int total = grow ? len + count : len;
   // this workgroup's rows
   const int chunk = max(a.chunk, ((total + a.splits - 1) / a.splits + 63) & ~63);
   const int from = split * chunk, to = min(total, from + chunk);
@@ -243,26 +251,47 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
       }
   };
 
-  // tiles of this wave, the next one's codes and the one after's ids on their way
+  // A tile's codes; the wave that owns a tile appends the new rows there first
+  // (no block passes the border of a tile, so no other wave reads them).
+  const auto load = [&](KvTile<D> &x, TileIds ids, int at) {
+    if (grow && at + 64 > fresh.b0 << c.bt_log) {
+      for (int i = max(fresh.b0, at >> c.bt_log); i <= min(fresh.b1, (at + 63) >> c.bt_log); ++i)
+        append_block<BF16, D>(a, pair, fresh, i);
+      __threadfence_block();
+    }
+    load_tile<D>(c, ids, at, x);
+  };
   const int step = 64 * waves;
   int base = from + 64 * wave;
   if (base < to) {
-    KvTile<D> x, y;
-    TileIds ix = tile_ids(c, row, base, to), iy = tile_ids(c, row, base + step, to);
-    load_tile<D>(c, ix, base, x);
-    for (;;) {
-      if (base + step < to) load_tile<D>(c, iy, base + step, y);
-      const TileIds ix2 = tile_ids(c, row, base + 2 * step, to);
-      work(x, ix, base);
-      base += step;
-      if (base >= to) break;
-      ix = ix2;
-      if (base + step < to) load_tile<D>(c, ix, base + step, x);
-      const TileIds iy2 = tile_ids(c, row, base + 2 * step, to);
-      work(y, iy, base);
-      base += step;
-      if (base >= to) break;
-      iy = iy2;
+    if constexpr (prefetches(BF16, D, NT)) {
+      // the next tile's codes and the ids of the one after on their way
+      KvTile<D> x, y;
+      TileIds ix = tile_ids(c, row, base, to), iy = tile_ids(c, row, base + step, to);
+      load(x, ix, base);
+      for (;;) {
+        if (base + step < to) load(y, iy, base + step);
+        const TileIds ix2 = tile_ids(c, row, base + 2 * step, to);
+        work(x, ix, base);
+        base += step;
+        if (base >= to) break;
+        ix = ix2;
+        if (base + step < to) load(x, ix, base + step);
+        const TileIds iy2 = tile_ids(c, row, base + 2 * step, to);
+        work(y, iy, base);
+        base += step;
+        if (base >= to) break;
+        iy = iy2;
+      }
+    } else {
+      KvTile<D> x;
+      TileIds ids = tile_ids(c, row, base, to);
+      for (; base < to; base += step) {
+        load(x, ids, base);
+        const TileIds next = tile_ids(c, row, base + step, to);
+        work(x, ids, base);
+        ids = next;
+      }
     }
   }
 
@@ -275,14 +304,17 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
     float l = sum[nt] + __shfl_xor(sum[nt], 16);
     l += __shfl_xor(l, 32);
     __syncthreads();                                         // the queries, or the last rows, are done with
-    if (g == 0) {
+    if (nt * 16 + m < R && g == 0) {
       ml[(wave * 16 + m) * 2] = mx[nt];
       ml[(wave * 16 + m) * 2 + 1] = l;
     }
+    if (nt * 16 + m < R)
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e)
-      *reinterpret_cast<f32x4 *>(oo + (wave * 16 + m) * P + 16 * e + 4 * g) = o[nt][e];
+      for (int e = 0; e < D / 16; ++e)
+        *reinterpret_cast<f32x4 *>(oo + (wave * 16 + m) * P + 16 * e + 4 * g) = o[nt][e];
     __syncthreads();
+    // every wave has read the old length
+    if (nt == 0 && grow && a.splits == 1 && t == 0) c.lens[pair] = total;
     for (int i = t; i < 16 * (D / 4); i += blockDim.x) {
       const int n = i / (D / 4), dim = i % (D / 4) * 4, r = nt * 16 + n;
       if (r >= R) continue;
@@ -329,6 +361,11 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
   const int t = threadIdx.x, G = c.Hq / c.Hkv, R = G * a.tokens;
   const int r = blockIdx.x % R, bh = blockIdx.x / R;
   const int b = bh / c.Hkv, h = bh - b * c.Hkv, j = r / G;
+  if (a.k && r == 0 && t == 0) {       // the new length, once every part was formed with the old one
+    const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
+    const NewRows n = new_rows(a, pair, b, h, pair_len(c, pair), call_count(a, b));
+    if (n.count > 0 && n.room) c.lens[pair] = n.len + n.count;
+  }
   const float2 *ml = a.part_ml + (int64_t)bh * a.splits * R + r;
   float top = kFloor;
   for (int i = t; i < a.splits; i += 256) top = fmaxf(top, ml[(int64_t)i * R].x);
@@ -367,7 +404,7 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, int most, hipStream_t s) {
   const int pairs = a.num_seqs * a.c.Hkv;
-  const int waves = NT == 1 && most > 256 && a.splits == 1 ? 8 : 4;
+  const int waves = NT == 1 && most > 256 ? 8 : 4;
   const int q = NT * (D / 32) * (BF16 ? 1 : 3) * 1024, o = waves * (128 + 64 * o_pitch<D>());
   hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(pairs * a.splits), dim3(64 * waves), std::max(q, o), s, a);
   if (a.splits > 1) {
@@ -381,9 +418,9 @@ hipError_t attend(const CacheStepArgs &a, int most, hipStream_t s) {
 
 CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens) {
   CachePlan p{};
-  // two workgroups a compute unit, each of at least 512 rows
-  const int64_t want = std::max<int64_t>(1, 1024 / pairs);
-  const int64_t by_rows = std::max<int64_t>(1, max_tokens / 512);
+  // two workgroups a compute unit, each of at least 1024 rows
+  const int64_t want = std::max<int64_t>(1, 512 / pairs);
+  const int64_t by_rows = std::max<int64_t>(1, max_tokens / 1024);
   p.splits = (int)std::min(want, by_rows);
   p.chunk = (int)((((int64_t)max_tokens + p.splits - 1) / p.splits + 63) / 64 * 64);
   if (p.splits > 1) {
@@ -401,6 +438,7 @@ hipError_t launch_cache_attend(const CacheStepArgs &a, bool bf16, int head_dim, 
               : (head_dim == 128 ? attend<false, 128, nt>(a, most, s) : attend<false, 64, nt>(a, most, s))
   if (R <= 16) ATTEND(1);
   if (R <= 32) ATTEND(2);
+  if (R <= 48) ATTEND(3);
   ATTEND(4);
 #undef ATTEND
 }

@@ -132,5 +132,82 @@ __device__ __forceinline__ void load8(const void *p, int64_t i, float (&x)[8]) {
   }
 }
 
+// New tokens of a pair in a call: sequence b of the call, `count` rows from
+// row `len` of the pair on, in blocks b0 .. b1 of its table.
+struct NewRows {
+  int b, h, len, count, b0, b1;
+  bool room;               // every block of them is one of the pool's
+};
+
+__device__ __forceinline__ int call_count(const CacheStepArgs &a, int b) {
+  return a.counts ? min(max(a.counts[b], 0), a.tokens) : a.tokens;
+}
+
+__device__ __forceinline__ NewRows new_rows(const CacheStepArgs &a, int64_t pair, int b, int h, int len, int count) {
+  NewRows n{b, h, len, count, len >> a.c.bt_log, (len + count - 1) >> a.c.bt_log, true};
+  for (int i = n.b0; i <= n.b1; ++i) n.room &= block_id(a.c, pair, i) >= 0;
+  return n;
+}
+
+// One wave puts the new rows of the pair's block i in place: 8 elements a
+// lane, D / 8 lanes a row.  The scale is the larger of the one that the block's old
+// rows have and the one that the new rows need; old codes are rounded again
+// where it grew (in whole words, before the new codes are written).
+template <bool BF16, int D>
+__device__ void append_block(const CacheStepArgs &a, int64_t pair, const NewRows &n, int i) {
+  constexpr int TR = D / 8, RP = 64 / TR;
+  const CacheDev &c = a.c;
+  const int lane = threadIdx.x & 63, bt = 1 << c.bt_log, base = i << c.bt_log;
+  const int id = block_id(c, pair, i);
+  const int from = max(n.len, base), old = from - base, m = min(n.len + n.count, base + bt) - from;
+  const int64_t row0 = (int64_t)n.b * a.tokens + (from - n.len);
+  float was[2], x[2][8], top[2] = {0.f, 0.f};
+  const int col = n.h * D + lane % TR * 8;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) was[kv] = c.scales[(int64_t)id * 2 + kv];
+  for (int r = lane / TR; r < m; r += RP)
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      load8<BF16>(kv ? a.v : a.k, (row0 + r) * (kv ? a.v_stride : a.k_stride) + col, x[kv]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top[kv] = fmaxf(top[kv], fabsf(x[kv][e]));
+    }
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    uint8_t *dst = block_codes<D>(c, id, kv);
+    float scale = block_scale(wave_max(top[kv]));
+    if (old && scale < was[kv]) scale = was[kv];
+    if (old && scale > was[kv]) {
+      const float f = was[kv] / scale;                       // a power of two: the product is exact
+      for (int e = lane; e < bt * D / 16; e += 64) {
+        u32x4 *p = reinterpret_cast<u32x4 *>(dst) + e;
+        u32x4 w = *p;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float y[4];
+          unpack4(w[j], y);
+          w[j] = pack4(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+        }
+        *p = w;
+      }
+      __threadfence_block();
+    }
+    if (lane == 0) c.scales[(int64_t)id * 2 + kv] = scale;
+    const float inv = 1.f / scale;
+    for (int r = lane / TR; r < m; r += RP) {
+      if (m > RP) load8<BF16>(kv ? a.v : a.k, (row0 + r) * (kv ? a.v_stride : a.k_stride) + col, x[kv]);
+      u32x2 w;
+      w[0] = pack4(x[kv][0] * inv, x[kv][1] * inv, x[kv][2] * inv, x[kv][3] * inv);
+      w[1] = pack4(x[kv][4] * inv, x[kv][5] * inv, x[kv][6] * inv, x[kv][7] * inv);
+      if (kv == 0) {
+        *reinterpret_cast<u32x2 *>(dst + (old + r) * D + lane % TR * 8) = w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dst[v_at<D>(old + r, lane % TR * 8 + e)] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+      }
+    }
+  }
+}
+
 }  // namespace
 }  // namespace bacon
