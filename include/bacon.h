@@ -394,7 +394,7 @@ int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
 typedef struct {
   int32_t num_layers;
   int32_t num_q_heads;
-  int32_t num_kv_heads;      /* num_q_heads % num_kv_heads == 0              */
+  int32_t num_kv_heads;      /* <= 1024, num_q_heads % num_kv_heads == 0      */
   int32_t head_dim;          /* 64 or 128                                    */
   int32_t window;            /* W >= 1 of the prompt's compression           */
   int32_t block_tokens;      /* 16, 32 or 64                                 */

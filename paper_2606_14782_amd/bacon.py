@@ -454,6 +454,9 @@ class Cache:
                                 max_batch, blocks, num_blocks, BF16 if dtype in ("bf16", BF16) else FP32)
         off = CacheOffsets()
         _check(lib().bacon_cache_layout(C.byref(self.shape), C.byref(off)))
+        self._torch, self._L = torch, lib()
+        self._raw_stream, self._current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        self._hq, self._hkv, self._d, self._work = num_q_heads, num_kv_heads, head_dim, {}
         dev = torch.device(device)
         self.device = dev if dev.index is not None else torch.device(dev.type, torch.cuda.current_device())
         self.torch_dtype = torch.bfloat16 if self.shape.dtype == BF16 else torch.float32
@@ -480,16 +483,15 @@ class Cache:
             _lib.bacon_cache_free(h)
             self._h = C.c_void_p()
 
-    # ---- checks and marshalling
+    # ---- checks and marshalling (short: a decode step's kernels take microseconds)
     def _call(self, fn, *args):
         """fn on the cache's device and that device's current stream."""
-        import torch
         at = self.device.index
-        stream = torch._C._cuda_getCurrentRawStream(at)
-        if torch._C._cuda_getDevice() == at:
+        stream = self._raw_stream(at)
+        if self._current() == at:
             status = fn(self._h, *args, stream)
         else:
-            with torch.cuda.device(self.device):
+            with self._torch.cuda.device(self.device):
                 status = fn(self._h, *args, stream)
         if status:
             _check(status)
@@ -498,58 +500,64 @@ class Cache:
         """The pointer of a contiguous tensor of this dtype (and shape)."""
         if t is None:
             return None
-        if t.device != self.device or t.dtype != dtype or not t.is_contiguous():
+        if t.dtype != dtype or not t.is_contiguous() or t.device != self.device:
             raise BaconError(ERR_INVALID, f"{name} must be a contiguous {dtype} tensor on {self.device}")
-        if shape is not None and tuple(t.shape) != shape:
-            raise BaconError(ERR_INVALID, f"{name} has shape {tuple(t.shape)}, {shape} expected")
+        if shape is not None and t.shape != shape:
+            raise BaconError(ERR_INVALID, f"{name} has shape {tuple(t.shape)}, {tuple(shape)} expected")
         return t.data_ptr()
 
-    def _tokens(self, t, name, heads, like=None):
-        """Pointer and token distance of rows [num_seqs, tokens, heads, d]."""
-        if t.device != self.device or t.dtype != self.torch_dtype or t.dim() != 4:
+    def _tokens(self, t, name, heads):
+        """Sequences, tokens, pointer and token distance of rows [num_seqs, tokens, heads, d]."""
+        if t.dtype != self.torch_dtype or t.dim() != 4 or t.device != self.device:
             raise BaconError(ERR_INVALID, f"{name} must be a 4-d {self.torch_dtype} tensor on {self.device}")
-        (b, n, h, d), (sb, sn, sh, sd) = t.shape, t.stride()
-        if h != heads or d != self.shape.head_dim or b < 1 or n < 1 or like is not None and like != (b, n):
+        b, n, h, d = t.shape
+        if h != heads or d != self._d or b < 1 or n < 1:
             raise BaconError(ERR_INVALID, f"{name} has shape {tuple(t.shape)}")
+        sb, sn, sh, sd = t.stride()
         step = sn if n > 1 else sb if b > 1 else h * d
         if sd != 1 or h > 1 and sh != d or n > 1 and b > 1 and sb != n * sn:
             raise BaconError(ERR_INVALID, f"{name} has strides {t.stride()}: a token's heads lie together, "
                                           "tokens evenly spaced")
-        return t.data_ptr(), step
+        return b, n, t.data_ptr(), step
+
+    def _new_rows(self, k, v):
+        """Sequences, tokens, and the pointers and distances of new tokens' K and V."""
+        b, n, kp, ks = self._tokens(k, "k", self._hkv)
+        bv, nv, vp, vs = self._tokens(v, "v", self._hkv)
+        if bv != b or nv != n:
+            raise BaconError(ERR_INVALID, f"k has {b} x {n} tokens, v {bv} x {nv}")
+        return b, n, kp, ks, vp, vs
 
     def _counts(self, counts, b, name="counts"):
-        import torch
-        return self._whole(counts, name, torch.int32, (b,))
+        return None if counts is None else self._whole(counts, name, self._torch.int32, (b,))
 
     # ---- entry points (same names as the C ABI)
     def bacon_cache_clear(self, first_seq=0, num_seqs=None):
         n = self.shape.max_batch - first_seq if num_seqs is None else num_seqs
-        self._call(lib().bacon_cache_clear, first_seq, n)
+        self._call(self._L.bacon_cache_clear, first_seq, n)
 
     def bacon_cache_tables(self, batch: BatchLayout, budgets=None, reserve=0, free=None, first_seq=0, used=None):
         """Lengths, tables and idx offsets of a prompt; budgets: None (the
         batch's) or int32 [num_layers, >= batch, Hkv] on the device; free: None
         or the int32 ids to take.  Returns the number of ids needed, int64 [1]
         on the device (more than given: some pairs found no blocks)."""
-        import torch
         s = self.shape
         if used is None:
-            used = torch.empty(1, dtype=torch.int64, device=self.device)
+            used = self._torch.empty(1, dtype=self._torch.int64, device=self.device)
         nb = 0
         if budgets is not None:
             if budgets.dim() != 3 or budgets.shape[0] != s.num_layers or budgets.shape[2] != s.num_kv_heads:
                 raise BaconError(ERR_INVALID, f"budgets have shape {tuple(budgets.shape)}")
             nb = budgets.shape[1]
-        self._call(lib().bacon_cache_tables, C.byref(batch.c), first_seq,
-                   self._whole(budgets, "budgets", torch.int32), nb, reserve,
-                   self._whole(free, "free", torch.int32), 0 if free is None else free.numel(),
-                   self._whole(used, "used", torch.int64, (1,)))
+        self._call(self._L.bacon_cache_tables, C.byref(batch.c), first_seq,
+                   self._whole(budgets, "budgets", self._torch.int32), nb, reserve,
+                   self._whole(free, "free", self._torch.int32), 0 if free is None else free.numel(),
+                   self._whole(used, "used", self._torch.int64, (1,)))
         return used
 
     def _layers(self, xs, name, dtype, shape):
         """Host array of per-layer pointers: a list of tensors, or one with the layers first."""
-        import torch
-        if isinstance(xs, torch.Tensor):
+        if isinstance(xs, self._torch.Tensor):
             if xs.dim() < 1 or shape is not None and tuple(xs.shape[1:]) != shape:
                 raise BaconError(ERR_INVALID, f"{name} has shape {tuple(xs.shape)}")
             base = self._whole(xs, name, dtype)
@@ -560,21 +568,19 @@ class Cache:
     def bacon_cache_store(self, batch: BatchLayout, ks, vs, idxs=None, first_seq=0, first_layer=0):
         """The kept rows of the layers first_layer, ..: ks, vs per-layer [T, Hkv,
         d] (lists, or stacked), idxs per-layer idx, or None (rows 0, 1, 2, ..)."""
-        import torch
         s = self.shape
         n = len(ks)
         if len(vs) != n or idxs is not None and len(idxs) != n or n < 1:
             raise BaconError(ERR_INVALID, f"{n} layers of K, {len(vs)} of V")
         rows = (batch.total, s.num_kv_heads, s.head_dim)
-        self._call(lib().bacon_cache_store, C.byref(batch.c), first_seq, first_layer, n,
+        self._call(self._L.bacon_cache_store, C.byref(batch.c), first_seq, first_layer, n,
                    self._layers(ks, "k", self.torch_dtype, rows), self._layers(vs, "v", self.torch_dtype, rows),
-                   None if idxs is None else self._layers(idxs, "idx", torch.int32, None))
+                   None if idxs is None else self._layers(idxs, "idx", self._torch.int32, None))
 
     def bacon_cache_load(self, count, first_token=0, first_layer=0, num_layers=None, first_seq=0, num_seqs=None,
                          out=None):
         """The values held, rows first_token .. first_token + count - 1 of every
         pair (first_token < 0: from its end): K, V [layers, seqs, Hkv, count, d]."""
-        import torch
         s = self.shape
         nl = s.num_layers - first_layer if num_layers is None else num_layers
         ns = s.max_batch - first_seq if num_seqs is None else num_seqs
@@ -582,67 +588,75 @@ class Cache:
         if out is None:
             if min(shape) < 1:
                 raise BaconError(ERR_INVALID, f"a load of shape {shape}")
-            out = torch.empty((2, *shape), dtype=self.torch_dtype, device=self.device).unbind(0)
+            out = self._torch.empty((2, *shape), dtype=self.torch_dtype, device=self.device).unbind(0)
         k, v = out
-        self._call(lib().bacon_cache_load, first_layer, nl, first_seq, ns, first_token, count,
+        self._call(self._L.bacon_cache_load, first_layer, nl, first_seq, ns, first_token, count,
                    self._whole(k, "k_out", self.torch_dtype, shape), self._whole(v, "v_out", self.torch_dtype, shape))
         return k, v
 
     def bacon_cache_append(self, layer, k, v, counts=None, first_seq=0):
         """Appends new tokens' rows k, v [num_seqs, tokens, Hkv, d]; counts
         (int32 [num_seqs], device): each sequence's own number of them."""
-        hkv = self.shape.num_kv_heads
-        kp, ks = self._tokens(k, "k", hkv)
-        b, n = k.shape[:2]
-        vp, vs = self._tokens(v, "v", hkv, (b, n))
-        self._call(lib().bacon_cache_append, layer, first_seq, b, n, self._counts(counts, b), kp, ks, vp, vs)
+        b, n, *rows = self._new_rows(k, v)
+        self._call(self._L.bacon_cache_append, layer, first_seq, b, n, self._counts(counts, b), *rows)
 
-    def _attend_out(self, q, max_tokens, out, lse, want_lse, work):
-        import torch
-        b, n, hq, d = q.shape
+    def _attend_out(self, b, n, max_tokens, out, lse, want_lse, work):
+        """Outputs and scratch of an attend, made where they are not given, and their pointers."""
+        torch, shape = self._torch, (b, n, self._hq, self._d)
         if out is None:
-            out = torch.empty((b, n, hq, d), dtype=self.torch_dtype, device=self.device)
-        if lse is None and want_lse:
-            lse = torch.empty((b, n, hq), dtype=torch.float32, device=self.device)
-        need = lib().bacon_cache_work_bytes(self._h, b, n, max_tokens)
-        if need and work is None:
+            out = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
+            outp = out.data_ptr()
+        else:
+            outp = self._whole(out, "out", self.torch_dtype, shape)
+        if lse is not None:
+            lsep = self._whole(lse, "lse", torch.float32, shape[:3])
+        elif want_lse:
+            lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device)
+            lsep = lse.data_ptr()
+        else:
+            lsep = None
+        key = (b, n, max_tokens)
+        need = self._work.get(key)
+        if need is None:
+            if len(self._work) > 1000:
+                self._work.clear()
+            need = self._work[key] = self._L.bacon_cache_work_bytes(self._h, b, n, max_tokens)
+        if not need:
+            return out, lse, outp, lsep, None, 0
+        if work is None:
             work = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return (out, lse, self._whole(out, "out", self.torch_dtype, (b, n, hq, d)),
-                self._whole(lse, "lse", torch.float32, (b, n, hq)),
-                self._whole(work, "work", torch.uint8), work.numel() if need else 0)
+        return out, lse, outp, lsep, self._whole(work, "work", torch.uint8), work.numel()
 
     def bacon_cache_attend(self, layer, q, counts=None, max_tokens=None, first_seq=0, out=None, lse=None,
                            want_lse=False, work=None):
         """Attention of q [num_seqs, tokens, Hq, d] over the layer's cache:
         out, or (out, lse [num_seqs, tokens, Hq]) with want_lse or lse given.
         max_tokens: the longest length to expect (None: the table's)."""
-        qp, qs = self._tokens(q, "q", self.shape.num_q_heads)
-        b, n = q.shape[:2]
+        b, n, qp, qs = self._tokens(q, "q", self._hq)
         most = max_tokens or 0
-        out, lse, *ptrs = self._attend_out(q, most, out, lse, want_lse, work)
-        self._call(lib().bacon_cache_attend, layer, first_seq, b, n, self._counts(counts, b), qp, qs, most, *ptrs)
+        out, lse, *ptrs = self._attend_out(b, n, most, out, lse, want_lse, work)
+        self._call(self._L.bacon_cache_attend, layer, first_seq, b, n, self._counts(counts, b), qp, qs, most, *ptrs)
         return out if lse is None else (out, lse)
 
     def bacon_cache_step(self, layer, q, k, v, counts=None, max_tokens=None, first_seq=0, out=None, lse=None,
                          want_lse=False, work=None):
         """bacon_cache_append(k, v), then bacon_cache_attend(q) over the grown cache."""
-        s = self.shape
-        qp, qs = self._tokens(q, "q", s.num_q_heads)
-        b, n = q.shape[:2]
-        kp, ks = self._tokens(k, "k", s.num_kv_heads, (b, n))
-        vp, vs = self._tokens(v, "v", s.num_kv_heads, (b, n))
+        b, n, qp, qs = self._tokens(q, "q", self._hq)
+        bk, nk, *rows = self._new_rows(k, v)
+        if bk != b or nk != n:
+            raise BaconError(ERR_INVALID, f"q has {b} x {n} tokens, k {bk} x {nk}")
         most = max_tokens or 0
-        out, lse, *ptrs = self._attend_out(q, most, out, lse, want_lse, work)
-        self._call(lib().bacon_cache_step, layer, first_seq, b, n, self._counts(counts, b), qp, qs, kp, ks, vp, vs,
-                   most, *ptrs)
+        out, lse, *ptrs = self._attend_out(b, n, most, out, lse, want_lse, work)
+        self._call(self._L.bacon_cache_step, layer, first_seq, b, n, self._counts(counts, b), qp, qs, *rows, most,
+                   *ptrs)
         return out if lse is None else (out, lse)
 
     def bacon_cache_advance(self, delta=0, counts=None, first_layer=0, num_layers=None, first_seq=0, num_seqs=None):
         """Moves the lengths by delta, or by counts (int32 [num_seqs], device; may be negative)."""
         nl = self.shape.num_layers - first_layer if num_layers is None else num_layers
         ns = self.shape.max_batch - first_seq if num_seqs is None else num_seqs
-        self._call(lib().bacon_cache_advance, first_layer, nl, first_seq, ns, delta, self._counts(counts, ns))
+        self._call(self._L.bacon_cache_advance, first_layer, nl, first_seq, ns, delta, self._counts(counts, ns))
 
     def bacon_cache_errors(self) -> int:
         """The error word (CACHE_* bits); waits for the device."""
-        return int(lib().bacon_cache_errors(self._h))
+        return int(self._L.bacon_cache_errors(self._h))

@@ -8,6 +8,7 @@ namespace bacon {
 
 constexpr int kCacheLow = -100, kCacheHigh = 120;   // exponents a block's scale may take
 constexpr int kCacheMaxBatch = 64;
+constexpr int kCacheMaxHeads = 1024;               // KV heads
 constexpr int kCacheMaxTokens = 64;                 // new tokens of one call
 constexpr int kCacheMaxQRows = 64;                  // G * tokens of one attend
 constexpr int kCacheLayersPerLaunch = 64;           // layers' pointers in one launch's arguments
@@ -41,6 +42,7 @@ struct CacheTablesArgs {
   const int32_t *free_ids; // optional [num_free]
   int64_t num_free;
   int64_t *used;           // optional
+  unsigned head_magic;     // 2^32 / Hkv, rounded up
 };
 
 struct CacheStoreArgs {
@@ -92,7 +94,7 @@ struct CacheMoveArgs {
 };
 
 hipError_t launch_cache_clear(const CacheDev &c, int first_seq, int num_seqs, bool errors, hipStream_t s);
-hipError_t launch_cache_tables(const CacheTablesArgs &a, hipStream_t s);
+hipError_t launch_cache_tables(CacheTablesArgs a, hipStream_t s);
 // most_rows: upper bound of a pair's rows.
 hipError_t launch_cache_store(const CacheStoreArgs &a, bool bf16, int head_dim, int most_rows, hipStream_t s);
 hipError_t launch_cache_load(const CacheLoadArgs &a, bool bf16, int head_dim, hipStream_t s);

@@ -28,39 +28,72 @@ __global__ __launch_bounds__(256) void k_cache_clear(CacheDev c, int first_seq, 
 }
 
 // ------------------------------------------------------------------ tables
-// Pairs in (layer, sequence, head) order; a workgroup owns kTabPairs of them and sums
-// the needs of all pairs before its own itself, which spares a second launch.
-constexpr int kTabPairs = 32;
+// Pairs in (layer, sequence, head) order.  A workgroup owns a few of them and
+// sums the needs of all pairs before its own itself: one launch, nothing
+// passed between workgroups.  Reading every budget again costs little (64 KB
+// from L2 for the 16384 pairs of 32 layers, 64 sequences and 8 heads).
+constexpr int kTabPairs = 32;          // most pairs of a workgroup
+
+// i / d for i < 2^16 and d <= 2^10, or any i * d < 2^32, with magic = 2^32 / d rounded up.
+__device__ __forceinline__ unsigned quotient(unsigned i, unsigned magic) { return __umulhi(i, magic); }
+
+// Steps of 256 through rows of `len` entries, without a division a step.
+struct Walk {
+  int row, at, len, rows, rest;
+  __device__ __forceinline__ Walk(int t, int n) : row(t / n), at(t % n), len(n), rows(256 / n), rest(256 % n) {}
+  __device__ __forceinline__ void next() {
+    row += rows;
+    at += rest;
+    if (at >= len) {
+      at -= len;
+      ++row;
+    }
+  }
+};
 
 struct PairNeed {
   int K, rows, need;
 };
 
-__device__ __forceinline__ PairNeed pair_need(const CacheTablesArgs &a, int64_t p) {
-  const int per = a.s.batch * a.c.Hkv;
-  const int l = (int)(p / per), r = (int)(p - (int64_t)l * per), b = r / a.c.Hkv, h = r - b * a.c.Hkv;
-  int K = a.budgets ? a.budgets[((int64_t)l * a.budgets_batch + b) * a.c.Hkv + h] : a.s.budget[b];
-  K = K < 0 ? 0 : K;
-  const int cand = a.s.cu[b + 1] - a.s.cu[b] - a.c.W;
+// Pair r of layer l of the batch.
+__device__ __forceinline__ PairNeed pair_need(const CacheTablesArgs &a, const int *cand, const int *budget, int l,
+                                              int r) {
+  const int b = a.c.Hkv == 1 ? r : (int)quotient(r, a.head_magic);
   PairNeed n;
-  n.K = K;
-  n.rows = (K < cand ? K : cand) + a.c.W;
+  n.K = a.budgets ? a.budgets[(int64_t)l * a.budgets_batch * a.c.Hkv + r] : budget[b];
+  n.K = n.K < 0 ? 0 : n.K;
+  n.rows = min(n.K, cand[b]) + a.c.W;
   n.need = (int)(((int64_t)n.rows + a.reserve + (1 << a.c.bt_log) - 1) >> a.c.bt_log);
   return n;
 }
 
-__global__ __launch_bounds__(256) void k_cache_tables(CacheTablesArgs a) {
-  __shared__ int64_t s_sum[4], s_k[4], s_first[kTabPairs];
-  __shared__ int s_need[kTabPairs];
+__global__ __launch_bounds__(256) void k_cache_tables(CacheTablesArgs a, int own) {
+  __shared__ int64_t s_sum[4], s_k[4], s_first[kTabPairs], s_row[kTabPairs];
+  __shared__ int s_need[kTabPairs], s_cand[kCacheMaxBatch], s_budget[kCacheMaxBatch];
   const CacheDev &c = a.c;
   const int t = threadIdx.x, lane = t & 63, per = a.s.batch * c.Hkv;
-  const int64_t pairs = (int64_t)per * c.L, p0 = (int64_t)blockIdx.x * kTabPairs;
-  const int64_t layer0 = p0 / per * per;                     // first pair of p0's layer
-  int64_t sum = 0, ksum = 0;
-  for (int64_t p = t; p < p0; p += 256) {
-    const PairNeed n = pair_need(a, p);
-    sum += n.need;
-    if (p >= layer0) ksum += n.K;
+  const int pairs = per * c.L, p0 = blockIdx.x * own;
+  const int l0 = p0 / per;                                   // p0's layer
+  if (t < a.s.batch) {
+    s_cand[t] = a.s.cu[t + 1] - a.s.cu[t] - c.W;
+    s_budget[t] = a.s.budget[t];
+  }
+  __syncthreads();
+  int64_t sum = 0, ksum = 0;                                 // needs before p0; budgets before p0 in its layer
+  Walk w(t, per);
+  for (int p = t; p < p0; p += 256 * 8) {
+    PairNeed x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i, w.next()) {
+      x[i] = PairNeed{0, 0, 0};
+      if (p + 256 * i < p0) x[i] = pair_need(a, s_cand, s_budget, w.row, w.at);
+      if (w.row != l0) x[i].K = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sum += x[i].need;
+      ksum += x[i].K;
+    }
   }
   for (int m = 32; m; m >>= 1) {
     sum += __shfl_xor(sum, m);
@@ -71,13 +104,13 @@ __global__ __launch_bounds__(256) void k_cache_tables(CacheTablesArgs a) {
     s_k[t >> 6] = ksum;
   }
   __syncthreads();
-  sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-  ksum = s_k[0] + s_k[1] + s_k[2] + s_k[3];
+  const int mine = min(own, pairs - p0);
   if (t < 64) {
-    const int64_t p = p0 + lane;
-    const bool mine = lane < kTabPairs && p < pairs;
+    sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+    ksum = s_k[0] + s_k[1] + s_k[2] + s_k[3];
+    const int p = p0 + lane, l = p / per;
     PairNeed n{0, 0, 0};
-    if (mine) n = pair_need(a, p);
+    if (lane < mine) n = pair_need(a, s_cand, s_budget, l, p - l * per);
     int64_t need_in = n.need, k_in = n.K;                    // inclusive scans over the lanes
     for (int m = 1; m < kTabPairs; m <<= 1) {
       const int64_t x = __shfl_up(need_in, m), y = __shfl_up(k_in, m);
@@ -87,140 +120,306 @@ __global__ __launch_bounds__(256) void k_cache_tables(CacheTablesArgs a) {
       }
     }
     const int64_t first = sum + need_in - n.need;
-    const int64_t layer = p / per * per;                     // first pair of this pair's layer
-    const int from = layer > p0 ? (int)(layer - p0) : 0;     // its lane, if it lies in this workgroup
-    const int64_t before = __shfl(k_in - n.K, from);
-    const int64_t start = k_in - n.K - before + (layer > p0 ? 0 : ksum);
-    if (mine) {
+    const int from = max(0, l * per - p0);                   // lane of the layer's first pair, if it is here
+    const int64_t start = k_in - n.K - __shfl(k_in - n.K, from & 63) + (l == l0 ? ksum : 0);
+    if (lane < mine) {
       const bool fits = first + n.need <= a.num_free && n.need <= c.max_blocks;
       if (!fits) atomicOr(c.err, (unsigned)BACON_CACHE_NO_BLOCKS);
+      const int64_t pair = ((int64_t)l * c.B + a.first_seq) * c.Hkv + (p - l * per);
       s_first[lane] = first;
       s_need[lane] = fits ? n.need : 0;
-      const int l = (int)(p / per);
-      const int64_t pair = ((int64_t)l * c.B + a.first_seq) * c.Hkv + (p - layer);
+      s_row[lane] = pair * c.max_blocks;
       c.lens[pair] = fits ? n.rows : 0;
       c.starts[pair] = (int)start;
       if (a.used && p == pairs - 1) *a.used = first + n.need;
     }
   }
   __syncthreads();
-  const int mine = (int)(pairs - p0 < kTabPairs ? pairs - p0 : kTabPairs);
-  for (int q = 0; q < mine; ++q) {
-    const int64_t p = p0 + q;
-    const int64_t pair = (p / per * c.B + a.first_seq) * c.Hkv + p % per;
-    for (int i = t; i < c.max_blocks; i += 256) {
-      int id = -1;
-      if (i < s_need[q]) {
-        const int64_t at = s_first[q] + i;
-        id = a.free_ids ? a.free_ids[at] : (int)at;
-        if ((unsigned)id >= (unsigned)c.num_blocks) {
-          atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
-          id = -1;
-        }
+  // the table rows, four entries of a thread on their way at a time
+  const int entries = mine * c.max_blocks;
+  Walk e(t, c.max_blocks);
+  for (int n = t; n < entries; n += 256 * 4) {
+    int id[4];
+    int64_t at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i, e.next()) {
+      id[i] = -1;
+      at[i] = -1;
+      if (n + 256 * i >= entries) continue;
+      at[i] = s_row[e.row] + e.at;
+      if (e.at < s_need[e.row]) {
+        const int64_t first = s_first[e.row] + e.at;
+        id[i] = a.free_ids ? a.free_ids[first] : (int)first;
       }
-      c.table[pair * c.max_blocks + i] = id;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (at[i] < 0) continue;
+      if (id[i] != -1 && (unsigned)id[i] >= (unsigned)c.num_blocks) {
+        atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
+        id[i] = -1;
+      }
+      c.table[at[i]] = id[i];
     }
   }
 }
 
 // ------------------------------------------------------------------- store
-// A workgroup takes K or V of one block at a time: its rows into registers
-// (8 elements a thread and pass), the largest magnitude, the codes out.  V's
-// codes are transposed through LDS.
+// A thread holds 4 rows of 8 dimensions of K and of V: lane bits 4 and 5
+// choose the rows of a group of 16, so that V's transpose ends in exchanges of
+// 16-lane rows and 16-byte stores.  A workgroup takes 4 groups (d 128) or 8.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <bool BF16>
+struct Raw8;                           // eight elements of a row as they lie in memory
+template <>
+struct Raw8<true> {
+  u32x4 w;
+};
+template <>
+struct Raw8<false> {
+  u32x4 w, x;
+};
+
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> raw8(const void *p, int64_t i) {
+  Raw8<BF16> r;
+  if constexpr (BF16) {
+    r.w = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + i);
+  } else {
+    const u32x4 *q = reinterpret_cast<const u32x4 *>(static_cast<const float *>(p) + i);
+    r.w = q[0];
+    r.x = q[1];
+  }
+  return r;
+}
+
+// The largest magnitude of four rows (bf16 magnitudes compare as integers).
+template <bool BF16>
+__device__ __forceinline__ float raw_top(const Raw8<BF16> (&r)[4]) {
+  if constexpr (BF16) {
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, r[i].w[j] & 0x7FFF7FFFu));
+    return bf16_float(m[0] > m[1] ? m[0] : m[1]);
+  } else {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m = max(max(m, r[i].w[j] & 0x7FFFFFFFu), r[i].x[j] & 0x7FFFFFFFu);
+    return __uint_as_float(m);
+  }
+}
+
+// Eight codes of a row: the conversion divides by the scale, a power of two,
+// and rounds to nearest even.
+template <bool BF16>
+__device__ __forceinline__ u32x2 raw_codes(const Raw8<BF16> &r, float scale) {
+  u32x2 out;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    s16x2 c = {0, 0};
+    if constexpr (BF16) {
+      const unsigned lo = r.w[2 * i], hi = r.w[2 * i + 1];
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, lo), scale, false);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, hi), scale, true);
+    } else {
+      const u32x4 w = i ? r.x : r.w;
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, __uint_as_float(w[0]), __uint_as_float(w[1]), scale, false);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, __uint_as_float(w[2]), __uint_as_float(w[3]), scale, true);
+    }
+    out[i] = __builtin_bit_cast(unsigned, c);
+  }
+  return out;
+}
+
+// Bytes j of a, b, c, d as word j.
+__device__ __forceinline__ void transpose4(unsigned a, unsigned b, unsigned c, unsigned d, unsigned (&w)[4]) {
+  const unsigned ab0 = __builtin_amdgcn_perm(b, a, 0x05010400), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602);
+  const unsigned cd0 = __builtin_amdgcn_perm(d, c, 0x05010400), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602);
+  w[0] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100);
+  w[1] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302);
+  w[2] = __builtin_amdgcn_perm(cd1, ab1, 0x05040100);
+  w[3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302);
+}
+
+// Four registers of four 16-lane rows, transposed: register i of row q becomes
+// register q of row i.
+__device__ __forceinline__ void transpose_rows(unsigned &a, unsigned &b, unsigned &c, unsigned &d) {
+  const auto ac = __builtin_amdgcn_permlane32_swap(a, c, false, false);
+  const auto bd = __builtin_amdgcn_permlane32_swap(b, d, false, false);
+  const auto ab = __builtin_amdgcn_permlane16_swap(ac[0], bd[0], false, false);
+  const auto cd = __builtin_amdgcn_permlane16_swap(ac[1], bd[1], false, false);
+  a = ab[0];
+  b = ab[1];
+  c = cd[0];
+  d = cd[1];
+}
+
 template <bool BF16, int D>
-__global__ __launch_bounds__(256) void k_cache_store(CacheStoreArgs a, int per_pair) {
-  constexpr int TR = D / 8, RP = 256 / TR;                   // threads of a row, rows of a pass
-  constexpr int PASSES = 64 / RP;                            // of the largest block
-  __shared__ float red[4];
-  __shared__ alignas(16) uint8_t tile[64 * D];
+__global__ __launch_bounds__(256) void k_cache_store(CacheStoreArgs a) {
+  constexpr int WG = 128 / D;                                // groups of 16 rows of a wave: 1 or 2
+  __shared__ float red[2][4 * WG];
   const CacheDev &c = a.c;
-  const int t = threadIdx.x, bt = 1 << c.bt_log;
-  const int x = blockIdx.x % per_pair, kv = blockIdx.y;
-  int64_t u = blockIdx.x / per_pair;
-  const int h = (int)(u % c.Hkv);
-  u /= c.Hkv;
-  const int b = (int)(u % a.s.batch), l = (int)(u / a.s.batch);
+  const int t = threadIdx.x, lane = t & 63, gl = c.bt_log - 4;
+  const int h = blockIdx.y, b = blockIdx.z % a.s.batch, l = blockIdx.z / a.s.batch;
   const int64_t pair = pair_of(c, a.first_layer + l, a.first_seq + b, h);
   const int len = pair_len(c, pair), cand = a.s.cu[b + 1] - a.s.cu[b] - c.W, kept = len - c.W;
-  const void *src = kv ? a.v[l] : a.k[l];
   const int32_t *idx = a.idx[l] ? a.idx[l] + c.starts[pair] : nullptr;
-  for (int blk = x; (blk << c.bt_log) < len; blk += per_pair) {
-    const int id = block_id(c, pair, blk);
-    if (id < 0) {
-      if (t == 0) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
-      continue;
-    }
-    float v[PASSES][8];
-    float top = 0.f;
+  const int group = (t >> 6) * WG + (WG == 2 ? lane >> 3 & 1 : 0);   // of the workgroup's
+  const int col = lane % (D / 8) * 8, q = lane >> 4, step = gridDim.x * 64 * WG;
+  const int64_t row_elems = (int64_t)c.Hkv * D, first = (int64_t)a.s.cu[b] * row_elems + h * D + col;
+  for (int base = blockIdx.x * 64 * WG; base < len; base += step) {
+    const int i0 = base + group * 16 + 4 * q, blk = i0 >> c.bt_log;
+    Raw8<BF16> v[2][4];
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int r = p * RP + t / TR, i = (blk << c.bt_log) + r;
+    for (int r = 0; r < 4; ++r) {
+      const int i = i0 + r;
+      int at = -1;
+      if (i < len) at = i < kept ? (idx ? idx[i] : i) : cand + (i - kept);
+      const bool ok = (unsigned)at < (unsigned)(i < kept ? cand : cand + c.W);
+      if (i < len && !ok && col == 0) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_INDEX);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[p][j] = 0.f;
-      if (r < bt && i < len) {
-        int at = i < kept ? (idx ? idx[i] : i) : cand + (i - kept);
-        const bool ok = (unsigned)at < (unsigned)(i < kept ? cand : cand + c.W);
-        if (!ok) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_INDEX);
-        if (ok) load8<BF16>(src, ((int64_t)(a.s.cu[b] + at) * c.Hkv + h) * D + (t % TR) * 8, v[p]);
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[p][j]));
-    }
-    __syncthreads();                                         // red and tile are free
-    const float scale = block_scale(block_max(top, red)), inv = 1.f / scale;
-    uint8_t *dst = block_codes<D>(c, id, kv);
-    if (t == 0) c.scales[(int64_t)id * 2 + kv] = scale;
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int r = p * RP + t / TR;
-      if (r >= bt) continue;
-      u32x2 w;
-      w[0] = pack4(v[p][0] * inv, v[p][1] * inv, v[p][2] * inv, v[p][3] * inv);
-      w[1] = pack4(v[p][4] * inv, v[p][5] * inv, v[p][6] * inv, v[p][7] * inv);
-      if (kv == 0) {
-        *reinterpret_cast<u32x2 *>(dst + r * D + (t % TR) * 8) = w;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) tile[v_at<D>(r, (t % TR) * 8 + j)] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+      for (int kv = 0; kv < 2; ++kv) {
+        v[kv][r] = Raw8<BF16>{};
+        if (ok) v[kv][r] = raw8<BF16>(kv ? a.v[l] : a.k[l], first + at * row_elems);
       }
     }
-    if (kv == 1) {
+    const bool any = blk << c.bt_log < len;
+    const int id = any ? block_id(c, pair, blk) : -1;
+    if (any && id < 0 && col == 0 && q == 0) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
+    float top[2];
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      top[kv] = raw_top<BF16>(v[kv]);
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1)
+        if (WG == 1 || m != 8) top[kv] = fmaxf(top[kv], __shfl_xor(top[kv], m));
+    }
+    if (gl) {                                                // a block of two or four groups
       __syncthreads();
-      for (int i = t * 16; i < bt * D; i += 256 * 16)
-        *reinterpret_cast<u32x4 *>(dst + i) = *reinterpret_cast<const u32x4 *>(tile + i);
+      if (col == 0 && q == 0) {
+        red[0][group] = top[0];
+        red[1][group] = top[1];
+      }
+      __syncthreads();
+      for (int i = 0; i < 1 << gl; ++i)
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) top[kv] = fmaxf(top[kv], red[kv][(group >> gl << gl) + i]);
     }
+    if (id < 0) continue;
+    const int row = (i0 & ((1 << c.bt_log) - 1));            // of the block: this thread's four rows from here on
+    const float ks = block_scale(top[0]), vs = block_scale(top[1]);
+    if (row == 0 && col == 0) *reinterpret_cast<float2 *>(c.scales + (int64_t)id * 2) = make_float2(ks, vs);
+    uint8_t *kd = block_codes<D>(c, id, 0) + row * D + col;
+    u32x2 w[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      *reinterpret_cast<u32x2 *>(kd + r * D) = raw_codes<BF16>(v[0][r], ks);
+      w[r] = raw_codes<BF16>(v[1][r], vs);
+    }
+    unsigned x[8];                                           // dimension j: the four rows' bytes
+    transpose4(w[0][0], w[1][0], w[2][0], w[3][0], *reinterpret_cast<unsigned(*)[4]>(x));
+    transpose4(w[0][1], w[1][1], w[2][1], w[3][1], *reinterpret_cast<unsigned(*)[4]>(x + 4));
+    transpose_rows(x[0], x[2], x[4], x[6]);                  // dimension 2 q: the group's 16 rows
+    transpose_rows(x[1], x[3], x[5], x[7]);
+    uint8_t *vd = block_codes<D>(c, id, 1) + v_at<D>(row & ~15, col + 2 * q);
+    *reinterpret_cast<u32x4 *>(vd) = u32x4{x[0], x[2], x[4], x[6]};
+    *reinterpret_cast<u32x4 *>(vd + 16) = u32x4{x[1], x[3], x[5], x[7]};
   }
 }
 
 // -------------------------------------------------------------------- load
+// The same division the other way: a thread takes 4 rows of 8 dimensions of
+// a group of 16 rows, V's as the words of 8 dimensions.
+template <bool BF16>
+__device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8]) {
+  if constexpr (BF16) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)        // values held are bf16 exactly
+      w[j] = __float_as_uint(x[2 * j]) >> 16 | (__float_as_uint(x[2 * j + 1]) & 0xFFFF0000u);
+    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + i) = w;
+  } else {
+    float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + i);
+    q[0] = make_float4(x[0], x[1], x[2], x[3]);
+    q[1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
+}
+
+template <int I>
+__device__ __forceinline__ float code_float(unsigned w) {
+  return __builtin_amdgcn_cvt_f32_fp8((int)w, I);
+}
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(256) void k_cache_load(CacheLoadArgs a, int64_t rows) {
+__global__ __launch_bounds__(256) void k_cache_load(CacheLoadArgs a, unsigned per_pair) {
+  constexpr int TR = D / 8, TG = 4 * TR;                     // threads of a row, of a group of 16 rows
   const CacheDev &c = a.c;
-  const int64_t step = (int64_t)gridDim.x * 256, n = rows * D;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
-    const int dim = (int)(i % D);
-    int64_t u = i / D;
-    const int r = (int)(u % a.count);
-    u /= a.count;
-    const int h = (int)(u % c.Hkv);
-    u /= c.Hkv;
-    const int64_t pair = pair_of(c, a.first_layer + (int)(u / a.num_seqs), a.first_seq + (int)(u % a.num_seqs), h);
-    const int len = pair_len(c, pair);
-    const int64_t pos = (int64_t)a.first_token + r + (a.first_token < 0 ? len : 0);
-    float k = 0.f, v = 0.f;
-    if (pos >= 0 && pos < len) {
-      const int id = block_id(c, pair, (int)(pos >> c.bt_log)), at = (int)pos & ((1 << c.bt_log) - 1);
-      if (id >= 0) {
-        const unsigned kc = block_codes<D>(c, id, 0)[at * D + dim], vc = block_codes<D>(c, id, 1)[v_at<D>(at, dim)];
-        k = __builtin_amdgcn_cvt_f32_fp8((int)kc, 0) * c.scales[(int64_t)id * 2];
-        v = __builtin_amdgcn_cvt_f32_fp8((int)vc, 0) * c.scales[(int64_t)id * 2 + 1];
-      } else if (dim == 0) {
-        atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
+  const int t = threadIdx.x;
+  const int part = (int)(blockIdx.x % per_pair);
+  unsigned u = blockIdx.x / per_pair;
+  const int64_t out_pair = u;
+  const int h = (int)(u % c.Hkv);
+  u /= c.Hkv;
+  const int64_t pair = pair_of(c, a.first_layer + (int)(u / a.num_seqs), a.first_seq + (int)(u % a.num_seqs), h);
+  const int len = pair_len(c, pair), col = t % TR * 8;
+  const int64_t start = (int64_t)a.first_token + (a.first_token < 0 ? len : 0);   // the pair's row of output row 0
+  const int64_t group = (start >> 4) + (int64_t)part * (256 / TG) + t / TG;
+  const int64_t pos0 = group * 16 + t % TG / TR * 4;         // this thread's four rows
+  if (pos0 + 3 < start || pos0 >= start + a.count) return;
+  unsigned kw[4][2] = {}, vw[8] = {};
+  float ks = 0.f, vs = 0.f;
+  if (pos0 >= 0 && pos0 < len) {
+    const int id = block_id(c, pair, (int)(pos0 >> c.bt_log)), at = (int)pos0 & ((1 << c.bt_log) - 1);
+    if (id >= 0) {
+      const uint8_t *k = block_codes<D>(c, id, 0) + at * D + col, *v = block_codes<D>(c, id, 1) + v_at<D>(at, col);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(k + r * D);
+        kw[r][0] = w[0];
+        kw[r][1] = w[1];
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vw[j] = *reinterpret_cast<const unsigned *>(v + 16 * j);
+      ks = c.scales[(int64_t)id * 2];
+      vs = c.scales[(int64_t)id * 2 + 1];
+    } else if (col == 0) {
+      atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
+      ks = 0.f;
     }
-    store_elem<BF16>(a.k, i, k);
-    store_elem<BF16>(a.v, i, v);
+  }
+  float v[4][8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[0][j] = code_float<0>(vw[j]);
+    v[1][j] = code_float<1>(vw[j]);
+    v[2][j] = code_float<2>(vw[j]);
+    v[3][j] = code_float<3>(vw[j]);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int64_t pos = pos0 + r, o = pos - start;
+    if (o < 0 || o >= a.count) continue;
+    const bool row = pos >= 0 && pos < len;                  // others hold any bytes
+    float x[4], y[4], k[8];
+    unpack4(kw[r][0], x);
+    unpack4(kw[r][1], y);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      k[j] = row ? x[j] * ks : 0.f;
+      k[4 + j] = row ? y[j] * ks : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[r][j] = row ? v[r][j] * vs : 0.f;
+    const int64_t out = (out_pair * a.count + o) * D + col;
+    store8<BF16>(a.k, out, k);
+    store8<BF16>(a.v, out, v[r]);
   }
 }
 
@@ -278,25 +477,33 @@ hipError_t launch_cache_clear(const CacheDev &c, int first_seq, int num_seqs, bo
   return hipGetLastError();
 }
 
-hipError_t launch_cache_tables(const CacheTablesArgs &a, hipStream_t s) {
-  const int64_t pairs = (int64_t)a.c.L * a.s.batch * a.c.Hkv;
-  hipLaunchKernelGGL(k_cache_tables, dim3((unsigned)((pairs + kTabPairs - 1) / kTabPairs)), dim3(256), 0, s, a);
+hipError_t launch_cache_tables(CacheTablesArgs a, hipStream_t s) {
+  const int pairs = a.c.L * a.s.batch * a.c.Hkv;
+  // about four workgroups a compute unit
+  const int own = std::max(1, std::min(kTabPairs, pairs / 1024));
+  a.head_magic = (unsigned)((0x100000000ull + a.c.Hkv - 1) / a.c.Hkv);
+  hipLaunchKernelGGL(k_cache_tables, dim3((unsigned)((pairs + own - 1) / own)), dim3(256), 0, s, a, own);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_store(const CacheStoreArgs &a, bool bf16, int head_dim, int most_rows, hipStream_t s) {
   const int64_t pairs = (int64_t)a.layers * a.s.batch * a.c.Hkv;
-  const int blocks = (most_rows + (1 << a.c.bt_log) - 1) >> a.c.bt_log;
-  const int per_pair = (int)std::max<int64_t>(1, std::min<int64_t>(blocks, 8192 / std::min<int64_t>(pairs, 8192)));
-  const dim3 grid((unsigned)(pairs * per_pair), 2);
-  CACHE_LAUNCH(k_cache_store, grid, 256, s, a, per_pair);
+  const int rows = 64 * (128 / head_dim), parts = (most_rows + rows - 1) / rows;
+  // (lengths known to the device alone may be far below most_rows: a bounded
+  // number of workgroups, each of several parts)
+  const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(parts, (1 << 18) / pairs)), a.c.Hkv,
+                  a.layers * a.s.batch);
+  CACHE_LAUNCH(k_cache_store, grid, 256, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_load(const CacheLoadArgs &a, bool bf16, int head_dim, hipStream_t s) {
-  const int64_t rows = (int64_t)a.layers * a.num_seqs * a.c.Hkv * a.count;
-  const dim3 grid(blocks_for(rows * head_dim, 256, 1 << 20));
-  CACHE_LAUNCH(k_cache_load, grid, 256, s, a, rows);
+  const int64_t pairs = (int64_t)a.layers * a.num_seqs * a.c.Hkv;
+  const int groups = 256 / (head_dim / 2);                   // of 16 rows, a workgroup's
+  const unsigned per_pair = (unsigned)((((int64_t)a.count + 15) / 16 + 1 + groups - 1) / groups);
+  if (pairs * per_pair > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)(pairs * per_pair));
+  CACHE_LAUNCH(k_cache_load, grid, 256, s, a, per_pair);
   return hipGetLastError();
 }
 

@@ -56,6 +56,8 @@ bacon_status check_shape(const bacon_cache_shape *s) {
   if (s->num_q_heads / s->num_kv_heads > kCacheMaxQRows)
     return fail(BACON_ERR_UNSUPPORTED, "%d query heads per KV head exceed %d", s->num_q_heads / s->num_kv_heads,
                 kCacheMaxQRows);
+  if (s->num_kv_heads > kCacheMaxHeads)
+    return fail(BACON_ERR_UNSUPPORTED, "%d KV heads exceed %d", s->num_kv_heads, kCacheMaxHeads);
   if (s->num_blocks > 0x7FFFFFFF) return fail(BACON_ERR_UNSUPPORTED, "num_blocks too large");
   if ((int64_t)s->max_blocks * s->block_tokens > (1 << 30))
     return fail(BACON_ERR_UNSUPPORTED, "a pair's %d blocks of %d tokens exceed 2^30 tokens", s->max_blocks,
@@ -369,6 +371,9 @@ bacon_status bacon_cache_load(bacon_cache *c, int32_t first_layer, int32_t num_l
     return fail(BACON_ERR_INVALID, "first_token %d outside [-2^30, 2^30]", first_token);
   TRY(check_ptr(d_k_out, "k_out", 16));
   TRY(check_ptr(d_v_out, "v_out", 16));
+  if ((double)num_layers * num_seqs * c->shape.num_kv_heads * ((double)count / 16 + 8) > (double)0x7FFFFFFF)
+    return fail(BACON_ERR_UNSUPPORTED, "a load of %d rows of %d layers and %d sequences is too large", count,
+                num_layers, num_seqs);
   TRY(check_cleared(c, first_seq, num_seqs));
   CacheLoadArgs a{};
   a.c = device_of(c);

@@ -401,11 +401,23 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
   if (t == 0 && a.lse) a.lse[at] = none ? -INFINITY : (top + __log2f(l)) * kLn2f;
 }
 
+// Allows a kernel more dynamic LDS than the default 64 KB, once per instance.
+template <bool BF16, int D, int NT>
+void allow_lds() {
+  static const bool done = [] {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_cache_attend<BF16, D, NT>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, 8 * (128 + 64 * o_pitch<D>()));
+    return true;
+  }();
+  (void)done;
+}
+
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, int most, hipStream_t s) {
   const int pairs = a.num_seqs * a.c.Hkv;
   const int waves = NT == 1 && most > 256 ? 8 : 4;
   const int q = NT * (D / 32) * (BF16 ? 1 : 3) * 1024, o = waves * (128 + 64 * o_pitch<D>());
+  allow_lds<BF16, D, NT>();
   hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(pairs * a.splits), dim3(64 * waves), std::max(q, o), s, a);
   if (a.splits > 1) {
     const int R = a.c.Hq / a.c.Hkv * a.tokens;
