@@ -30,17 +30,19 @@ __global__ __launch_bounds__(256) void k_cache_clear(CacheDev c, int first_seq, 
 // ------------------------------------------------------------------ tables
 // Pairs in (layer, sequence, head) order.  A workgroup owns a few of them and
 // sums the needs of all pairs before its own itself: one launch, nothing
-// passed between workgroups.  Reading every budget again costs little (64 KB
-// from L2 for the 16384 pairs of 32 layers, 64 sequences and 8 heads).
-constexpr int kTabPairs = 32;          // most pairs of a workgroup
+// passed between workgroups.  Large workgroups keep that small: of the 16384
+// pairs of 32 layers, 64 sequences and 8 heads, 256 workgroups read half on
+// average; 1024 of 256 threads spent 14 of 22 us there.
+constexpr int kTabPairs = 64;          // most pairs of a workgroup
+constexpr int kTabThreads = 1024;
 
 // i / d for i < 2^16 and d <= 2^10, or any i * d < 2^32, with magic = 2^32 / d rounded up.
 __device__ __forceinline__ unsigned quotient(unsigned i, unsigned magic) { return __umulhi(i, magic); }
 
-// Steps of 256 through rows of `len` entries, without a division a step.
+// Steps of kTabThreads through rows of `len` entries, without a division a step.
 struct Walk {
   int row, at, len, rows, rest;
-  __device__ __forceinline__ Walk(int t, int n) : row(t / n), at(t % n), len(n), rows(256 / n), rest(256 % n) {}
+  __device__ __forceinline__ Walk(int t, int n) : row(t / n), at(t % n), len(n), rows(kTabThreads / n), rest(kTabThreads % n) {}
   __device__ __forceinline__ void next() {
     row += rows;
     at += rest;
@@ -63,12 +65,12 @@ __device__ __forceinline__ PairNeed pair_need(const CacheTablesArgs &a, const in
   n.K = a.budgets ? a.budgets[(int64_t)l * a.budgets_batch * a.c.Hkv + r] : budget[b];
   n.K = n.K < 0 ? 0 : n.K;
   n.rows = min(n.K, cand[b]) + a.c.W;
-  n.need = (int)(((int64_t)n.rows + a.reserve + (1 << a.c.bt_log) - 1) >> a.c.bt_log);
+  n.need = (int)(((unsigned)n.rows + (unsigned)a.reserve + (1u << a.c.bt_log) - 1u) >> a.c.bt_log);
   return n;
 }
 
-__global__ __launch_bounds__(256) void k_cache_tables(CacheTablesArgs a, int own) {
-  __shared__ int64_t s_sum[4], s_k[4], s_first[kTabPairs], s_row[kTabPairs];
+__global__ __launch_bounds__(kTabThreads) void k_cache_tables(CacheTablesArgs a, int own) {
+  __shared__ int64_t s_sum[kTabThreads / 64], s_k[kTabThreads / 64], s_first[kTabPairs], s_row[kTabPairs];
   __shared__ int s_need[kTabPairs], s_cand[kCacheMaxBatch], s_budget[kCacheMaxBatch];
   const CacheDev &c = a.c;
   const int t = threadIdx.x, lane = t & 63, per = a.s.batch * c.Hkv;
@@ -81,19 +83,21 @@ __global__ __launch_bounds__(256) void k_cache_tables(CacheTablesArgs a, int own
   __syncthreads();
   int64_t sum = 0, ksum = 0;                                 // needs before p0; budgets before p0 in its layer
   Walk w(t, per);
-  for (int p = t; p < p0; p += 256 * 8) {
+  for (int p = t; p < p0; p += kTabThreads * 8) {
     PairNeed x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i, w.next()) {
       x[i] = PairNeed{0, 0, 0};
-      if (p + 256 * i < p0) x[i] = pair_need(a, s_cand, s_budget, w.row, w.at);
+      if (p + kTabThreads * i < p0) x[i] = pair_need(a, s_cand, s_budget, w.row, w.at);
       if (w.row != l0) x[i].K = 0;
     }
+    unsigned some = 0;                                       // eight needs below 2^28 each
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      sum += x[i].need;
+      some += x[i].need;
       ksum += x[i].K;
     }
+    sum += some;
   }
   for (int m = 32; m; m >>= 1) {
     sum += __shfl_xor(sum, m);
@@ -106,8 +110,11 @@ __global__ __launch_bounds__(256) void k_cache_tables(CacheTablesArgs a, int own
   __syncthreads();
   const int mine = min(own, pairs - p0);
   if (t < 64) {
-    sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-    ksum = s_k[0] + s_k[1] + s_k[2] + s_k[3];
+    sum = ksum = 0;
+    for (int i = 0; i < kTabThreads / 64; ++i) {
+      sum += s_sum[i];
+      ksum += s_k[i];
+    }
     const int p = p0 + lane, l = p / per;
     PairNeed n{0, 0, 0};
     if (lane < mine) n = pair_need(a, s_cand, s_budget, l, p - l * per);
@@ -138,14 +145,14 @@ __global__ __launch_bounds__(256) void k_cache_tables(CacheTablesArgs a, int own
   // the table rows, four entries of a thread on their way at a time
   const int entries = mine * c.max_blocks;
   Walk e(t, c.max_blocks);
-  for (int n = t; n < entries; n += 256 * 4) {
+  for (int n = t; n < entries; n += kTabThreads * 4) {
     int id[4];
     int64_t at[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i, e.next()) {
       id[i] = -1;
       at[i] = -1;
-      if (n + 256 * i >= entries) continue;
+      if (n + kTabThreads * i >= entries) continue;
       at[i] = s_row[e.row] + e.at;
       if (e.at < s_need[e.row]) {
         const int64_t first = s_first[e.row] + e.at;
@@ -335,91 +342,74 @@ __global__ __launch_bounds__(256) void k_cache_store(CacheStoreArgs a) {
 }
 
 // -------------------------------------------------------------------- load
-// The same division the other way: a thread takes 4 rows of 8 dimensions of
-// a group of 16 rows, V's as the words of 8 dimensions.
+// The store's division the other way: 16-byte reads of two dimensions' 16
+// rows, exchanged between 16-lane rows, then bytes transposed so that a conversion gives
+// neighbouring dimensions of a row.
 template <bool BF16>
-__device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8]) {
-  if constexpr (BF16) {
-    u32x4 w;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)        // values held are bf16 exactly
-      w[j] = __float_as_uint(x[2 * j]) >> 16 | (__float_as_uint(x[2 * j + 1]) & 0xFFFF0000u);
-    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + i) = w;
+__device__ __forceinline__ void store_codes8(void *p, int64_t i, unsigned lo, unsigned hi, float scale) {
+  if constexpr (BF16) {                // values held are bf16 exactly
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + i) =
+        u32x4{__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, c),
+              __builtin_bit_cast(unsigned, d)};
   } else {
+    float x[4], y[4];
+    unpack4(lo, x);
+    unpack4(hi, y);
     float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + i);
-    q[0] = make_float4(x[0], x[1], x[2], x[3]);
-    q[1] = make_float4(x[4], x[5], x[6], x[7]);
+    q[0] = make_float4(x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale);
+    q[1] = make_float4(y[0] * scale, y[1] * scale, y[2] * scale, y[3] * scale);
   }
-}
-
-template <int I>
-__device__ __forceinline__ float code_float(unsigned w) {
-  return __builtin_amdgcn_cvt_f32_fp8((int)w, I);
 }
 
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void k_cache_load(CacheLoadArgs a, unsigned per_pair) {
-  constexpr int TR = D / 8, TG = 4 * TR;                     // threads of a row, of a group of 16 rows
+  constexpr int WG = 128 / D;                                // groups of 16 rows of a wave: 1 or 2
   const CacheDev &c = a.c;
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, lane = t & 63;
   const int part = (int)(blockIdx.x % per_pair);
   unsigned u = blockIdx.x / per_pair;
   const int64_t out_pair = u;
   const int h = (int)(u % c.Hkv);
   u /= c.Hkv;
   const int64_t pair = pair_of(c, a.first_layer + (int)(u / a.num_seqs), a.first_seq + (int)(u % a.num_seqs), h);
-  const int len = pair_len(c, pair), col = t % TR * 8;
+  const int len = pair_len(c, pair), col = lane % (D / 8) * 8, q = lane >> 4;
   const int64_t start = (int64_t)a.first_token + (a.first_token < 0 ? len : 0);   // the pair's row of output row 0
-  const int64_t group = (start >> 4) + (int64_t)part * (256 / TG) + t / TG;
-  const int64_t pos0 = group * 16 + t % TG / TR * 4;         // this thread's four rows
-  if (pos0 + 3 < start || pos0 >= start + a.count) return;
-  unsigned kw[4][2] = {}, vw[8] = {};
-  float ks = 0.f, vs = 0.f;
-  if (pos0 >= 0 && pos0 < len) {
-    const int id = block_id(c, pair, (int)(pos0 >> c.bt_log)), at = (int)pos0 & ((1 << c.bt_log) - 1);
+  const int64_t group = (start >> 4) + (int64_t)part * 4 * WG + (t >> 6) * WG + (WG == 2 ? lane >> 3 & 1 : 0);
+  const int64_t base = group * 16, pos0 = base + 4 * q;      // this thread's four rows
+  u32x2 kw[4] = {};
+  u32x4 v0 = {0, 0, 0, 0}, v1 = {0, 0, 0, 0};
+  float2 scale = {0.f, 0.f};
+  if (base >= 0 && base < len && base < start + a.count) {
+    const int id = block_id(c, pair, (int)(base >> c.bt_log)), at = (int)base & ((1 << c.bt_log) - 1);
     if (id >= 0) {
-      const uint8_t *k = block_codes<D>(c, id, 0) + at * D + col, *v = block_codes<D>(c, id, 1) + v_at<D>(at, col);
+      const uint8_t *k = block_codes<D>(c, id, 0) + (at + 4 * q) * D + col;
+      const uint8_t *v = block_codes<D>(c, id, 1) + v_at<D>(at, col + 2 * q);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const u32x2 w = *reinterpret_cast<const u32x2 *>(k + r * D);
-        kw[r][0] = w[0];
-        kw[r][1] = w[1];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) vw[j] = *reinterpret_cast<const unsigned *>(v + 16 * j);
-      ks = c.scales[(int64_t)id * 2];
-      vs = c.scales[(int64_t)id * 2 + 1];
-    } else if (col == 0) {
+      for (int r = 0; r < 4; ++r) kw[r] = *reinterpret_cast<const u32x2 *>(k + r * D);
+      v0 = *reinterpret_cast<const u32x4 *>(v);
+      v1 = *reinterpret_cast<const u32x4 *>(v + 16);
+      scale = *reinterpret_cast<const float2 *>(c.scales + (int64_t)id * 2);
+    } else if (lane == 0) {
       atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
-      ks = 0.f;
     }
   }
-  float v[4][8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    v[0][j] = code_float<0>(vw[j]);
-    v[1][j] = code_float<1>(vw[j]);
-    v[2][j] = code_float<2>(vw[j]);
-    v[3][j] = code_float<3>(vw[j]);
-  }
+  unsigned x[8] = {v0[0], v1[0], v0[1], v1[1], v0[2], v1[2], v0[3], v1[3]}, w[8];
+  transpose_rows(x[0], x[2], x[4], x[6]);                    // dimension j: this thread's four rows' bytes
+  transpose_rows(x[1], x[3], x[5], x[7]);
+  transpose4(x[0], x[1], x[2], x[3], *reinterpret_cast<unsigned(*)[4]>(w));
+  transpose4(x[4], x[5], x[6], x[7], *reinterpret_cast<unsigned(*)[4]>(w + 4));
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int64_t pos = pos0 + r, o = pos - start;
     if (o < 0 || o >= a.count) continue;
     const bool row = pos >= 0 && pos < len;                  // others hold any bytes
-    float x[4], y[4], k[8];
-    unpack4(kw[r][0], x);
-    unpack4(kw[r][1], y);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      k[j] = row ? x[j] * ks : 0.f;
-      k[4 + j] = row ? y[j] * ks : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[r][j] = row ? v[r][j] * vs : 0.f;
     const int64_t out = (out_pair * a.count + o) * D + col;
-    store8<BF16>(a.k, out, k);
-    store8<BF16>(a.v, out, v[r]);
+    store_codes8<BF16>(a.k, out, row ? kw[r][0] : 0, row ? kw[r][1] : 0, row ? scale.x : 1.f);
+    store_codes8<BF16>(a.v, out, row ? w[r] : 0, row ? w[4 + r] : 0, row ? scale.y : 1.f);
   }
 }
 
@@ -479,10 +469,9 @@ hipError_t launch_cache_clear(const CacheDev &c, int first_seq, int num_seqs, bo
 
 hipError_t launch_cache_tables(CacheTablesArgs a, hipStream_t s) {
   const int pairs = a.c.L * a.s.batch * a.c.Hkv;
-  // about four workgroups a compute unit
-  const int own = std::max(1, std::min(kTabPairs, pairs / 1024));
+  const int own = std::max(1, std::min(kTabPairs, pairs / 256));
   a.head_magic = (unsigned)((0x100000000ull + a.c.Hkv - 1) / a.c.Hkv);
-  hipLaunchKernelGGL(k_cache_tables, dim3((unsigned)((pairs + own - 1) / own)), dim3(256), 0, s, a, own);
+  hipLaunchKernelGGL(k_cache_tables, dim3((unsigned)((pairs + own - 1) / own)), dim3(kTabThreads), 0, s, a, own);
   return hipGetLastError();
 }
 
