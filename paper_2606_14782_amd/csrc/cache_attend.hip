@@ -25,9 +25,14 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // The codes become bf16 in registers, exactly, with the block's scale applied by the
 // conversion.
 template <int D>
-struct KvTile {
-  u32x4 k[4][D / 64], v[D / 16];
-  float ks, vs;
+struct KTile {
+  u32x4 w[4][D / 64];
+  float scale;
+};
+template <int D>
+struct VTile {
+  u32x4 w[D / 16];
+  float scale;
 };
 
 // Block ids of a tile: of the rows this lane loads K of (group (lane & 15) >> 2)
@@ -36,32 +41,41 @@ struct TileIds {
   int k, v;
 };
 
-__device__ __forceinline__ TileIds tile_ids(const CacheDev &c, const int32_t *row, int base, int to) {
-  const int lane = threadIdx.x & 63;
-  const int pk = base + 16 * ((lane & 15) >> 2), pv = base + 16 * (lane >> 4);
-  TileIds t;
-  t.k = pk < to ? row[pk >> c.bt_log] : -1;
-  t.v = pv < to ? row[pv >> c.bt_log] : -1;
-  return t;
+// The entries for a tile's rows, whatever the pair's length (bounded by the table).
+__device__ __forceinline__ TileIds any_ids(const CacheDev &c, const int32_t *row, int base) {
+  const int lane = threadIdx.x & 63, last = c.max_blocks - 1;
+  return TileIds{row[min((base + 16 * ((lane & 15) >> 2)) >> c.bt_log, last)],
+                 row[min((base + 16 * (lane >> 4)) >> c.bt_log, last)]};
 }
 
+__device__ __forceinline__ TileIds bound_ids(TileIds t, int base, int to) {
+  const int lane = threadIdx.x & 63;
+  return TileIds{base + 16 * ((lane & 15) >> 2) < to ? t.k : -1, base + 16 * (lane >> 4) < to ? t.v : -1};
+}
+
+
+// (An absent block's rows are masked: any address of the pool will do.)
 template <int D>
-__device__ __forceinline__ void load_tile(const CacheDev &c, TileIds ids, int base, KvTile<D> &x) {
-  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, in = (1 << c.bt_log) - 1;
-  // an absent block's rows are masked: any address of the pool will do
-  const int ik = (unsigned)ids.k < (unsigned)c.num_blocks ? ids.k : 0;
-  const int iv = (unsigned)ids.v < (unsigned)c.num_blocks ? ids.v : 0;
-  const int rk = ((base + 16 * (m >> 2)) & in) + (m & 3), rv = (base + 16 * g) & in;
-  const uint8_t *k = block_codes<D>(c, ik, 0) + rk * D + 16 * g;
-  const uint8_t *v = block_codes<D>(c, iv, 1) + rv * D + 16 * m;
-  x.ks = c.scales[(int64_t)ik * 2];
-  x.vs = c.scales[(int64_t)iv * 2 + 1];
+__device__ __forceinline__ void load_k(const CacheDev &c, int id, int base, KTile<D> &x) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int i = (unsigned)id < (unsigned)c.num_blocks ? id : 0;
+  const int r = ((base + 16 * (m >> 2)) & ((1 << c.bt_log) - 1)) + (m & 3);
+  const uint8_t *p = block_codes<D>(c, i, 0) + r * D + 16 * g;
+  x.scale = c.scales[(int64_t)i * 2];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) x.k[t][j] = *reinterpret_cast<const u32x4 *>(k + 4 * t * D + 64 * j);
+    for (int j = 0; j < D / 64; ++j) x.w[t][j] = *reinterpret_cast<const u32x4 *>(p + 4 * t * D + 64 * j);
+}
+
+template <int D>
+__device__ __forceinline__ void load_v(const CacheDev &c, int id, int base, VTile<D> &x) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int i = (unsigned)id < (unsigned)c.num_blocks ? id : 0;
+  const uint8_t *p = block_codes<D>(c, i, 1) + ((base + 16 * g) & ((1 << c.bt_log) - 1)) * D + 16 * m;
+  x.scale = c.scales[(int64_t)i * 2 + 1];
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) x.v[e] = *reinterpret_cast<const u32x4 *>(v + 256 * e);
+  for (int e = 0; e < D / 16; ++e) x.w[e] = *reinterpret_cast<const u32x4 *>(p + 256 * e);
 }
 
 // Eight codes as bf16 values times the scale (exact).
@@ -92,6 +106,14 @@ __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// Barrier for LDS traffic alone: the global loads in flight stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);                        // lgkmcnt 0
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ float xor16_32_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16));
   return fmaxf(v, __shfl_xor(v, 32));
@@ -99,10 +121,7 @@ __device__ __forceinline__ float xor16_32_max(float v) {
 
 // Waves of a workgroup: 8 fill a compute unit at 256 registers a lane; more
 // query rows hold more outputs and take 4 waves of up to 512.
-constexpr int max_waves(int nt) { return nt == 1 ? 8 : 4; }
-// Whether a second tile's codes fit the registers beside the first's.
-constexpr bool prefetches(bool bf16, int d, int nt) { return d == 64 ? nt <= 2 || bf16 : bf16 ? nt <= 2 : nt == 1; }
-
+constexpr int max_waves(int nt) { return nt <= 2 ? 8 : 4; }
 constexpr float kFloor = -1e30f;       // maximum of no logits
 
 template <int D>
@@ -116,18 +135,26 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
   extern __shared__ __align__(16) char lds[];
   bf16x8 *q_lds = reinterpret_cast<bf16x8 *>(lds);           // [NT][KS][QP][64]
   const CacheDev &c = a.c;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, waves = blockDim.x >> 6;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), waves = blockDim.x >> 6;
   const int m = lane & 15, g = lane >> 4;
   const int split = blockIdx.x % a.splits, bh = blockIdx.x / a.splits;
   const int b = bh / c.Hkv, h = bh - b * c.Hkv;
   const int G = c.Hq / c.Hkv, R = G * a.tokens;
   const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
   const int32_t *row = c.table + pair * c.max_blocks;
-  const int len = pair_len(c, pair), count = call_count(a, b);
+  // The first two tiles' ids are asked for before the length is known (and
+  // before any codes: a wait for an id is then no wait for codes).
+  const int step = 64 * waves;
+  const int guess = (int)min((int64_t)split * a.chunk + 64 * wave, (int64_t)1 << 30);
+  TileIds id0 = any_ids(c, row, guess), id1 = any_ids(c, row, guess + step);
+  // (scalar, so that the loops below end for a whole wave at once)
+  const int len = __builtin_amdgcn_readfirstlane(pair_len(c, pair));
+  const int count = __builtin_amdgcn_readfirstlane(call_count(a, b));
   const bool append = a.k && count > 0;
   NewRows fresh{};
   if (append) {
     fresh = new_rows(a, pair, b, h, len, count);
+    fresh.room = __builtin_amdgcn_readfirstlane((int)fresh.room);
     if (!fresh.room && split == 0 && t == 0) atomicOr(c.err, (unsigned)BACON_CACHE_NO_BLOCKS);
   }
   const bool grow = append && fresh.room;
@@ -136,6 +163,37 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
   const int chunk = max(a.chunk, ((total + a.splits - 1) / a.splits + 63) & ~63);
   const int from = split * chunk, to = min(total, from + chunk);
   const int first_end = total - (count - 1);                 // of the first query: below it nothing is masked
+
+  // the first tile's codes, asked for before the queries are formed
+  int base = from + 64 * wave;
+  KTile<D> kt;
+  VTile<D> vt;
+  if (base != guess) {
+    id0 = any_ids(c, row, base);
+    id1 = any_ids(c, row, base + step);
+  }
+  TileIds ids = bound_ids(id0, base, to);
+  const bool late = grow && base + 64 > fresh.b0 << c.bt_log;
+  if (base < to && !late) {
+    load_k<D>(c, ids.k, base, kt);
+    load_v<D>(c, ids.v, base, vt);
+  }
+  // The new rows: the wave that owns a tile puts those of its blocks in place
+  // before it reads them (no block passes the border of a tile, so no other wave does).
+  if (grow) {
+    for (int i = fresh.b0; i <= fresh.b1; ++i) {
+      const int at = (i << c.bt_log & ~63) - from;
+      if (at >= 0 && at < to - from && (at >> 6) % waves == wave) append_block<BF16, D>(a, pair, fresh, i);
+    }
+    __threadfence_block();
+    // all of it ends here: what the compiler takes to be still in flight it
+    // waits for again in every round of the loop below
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt 0
+  }
+  if (base < to && late) {
+    load_k<D>(c, ids.k, base, kt);
+    load_v<D>(c, ids.v, base, vt);
+  }
 
   // queries: lane (n, g) holds 8 dimensions of query n for each step of 32
   for (int i = wave; i < NT * KS; i += waves) {
@@ -155,7 +213,7 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
     const int r = nt * 16 + m, j = r / G;
     end[nt] = r < R && j < count ? max(0, total - (count - 1 - j)) : 0;
   }
-  __syncthreads();
+  lds_barrier();
 
   f32x4 o[NT][D / 16];
   float mx[NT], sum[NT];
@@ -167,24 +225,14 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
     for (int e = 0; e < D / 16; ++e) o[nt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const auto work = [&](KvTile<D> &x, TileIds ids, int base) {
+  // A tile's K gives way to the next tile's as soon as the logits are formed,
+  // its V once the outputs have it: each is in flight while the other half of
+  // the work is done, in one set of registers.  No load hangs on a condition,
+  // since the compiler would wait for all of them where the paths meet: past
+  // the end they read block 0.
+  for (; base < to; base += step) {
     const bool here = (unsigned)ids.v < (unsigned)c.num_blocks;
     const bool masked = base + 64 > first_end || !__all(here);
-    if (masked) {
-      // rows that hold nothing: their codes may be any bytes
-      const int n = here ? total - (base + 16 * g) : 0;
-      if (!here && base + 16 * g < total) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
-      if (n < 16) {
-        if (n <= 0) x.vs = 1.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int left = n - 4 * w;
-          const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-#pragma unroll
-          for (int e = 0; e < D / 16; ++e) x.v[e][w] &= keep;
-        }
-      }
-    }
     f32x4 s[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -194,7 +242,8 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
     for (int k = 0; k < KS; ++k) {
       bf16x8 kk[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) kk[i] = dequant(x.k[i][k >> 1][2 * (k & 1)], x.k[i][k >> 1][2 * (k & 1) + 1], x.ks);
+      for (int i = 0; i < 4; ++i)
+        kk[i] = dequant(kt.w[i][k >> 1][2 * (k & 1)], kt.w[i][k >> 1][2 * (k & 1) + 1], kt.scale);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -204,6 +253,9 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
           for (int i = 0; i < 4; ++i) s[nt][i] = mfma(kk[i], qq, s[nt][i]);
         }
     }
+    const TileIds next = bound_ids(id1, base + step, to);
+    id1 = any_ids(c, row, base + 2 * step);
+    load_k<D>(c, next.k, base + step, kt);
     bf16x8 w[NT][2][PP];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -239,60 +291,31 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
         split8<PP>(x8, w[nt][u]);
       }
     }
+    if (masked) {
+      // rows that hold nothing: their codes may be any bytes
+      const int n = here ? total - (base + 16 * g) : 0;
+      if (!here && base + 16 * g < total) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
+      if (n <= 0) vt.scale = 1.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int left = n - 4 * i;
+        const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) vt.w[e][i] &= keep;
+      }
+    }
 #pragma unroll
     for (int e = 0; e < D / 16; ++e)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const bf16x8 vv = dequant(x.v[e][2 * u], x.v[e][2 * u + 1], x.vs);
+        const bf16x8 vv = dequant(vt.w[e][2 * u], vt.w[e][2 * u + 1], vt.scale);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int p = 0; p < PP; ++p) o[nt][e] = mfma(vv, w[nt][u][p], o[nt][e]);
       }
-  };
-
-  // A tile's codes; the wave that owns a tile appends the new rows there first
-  // (no block passes the border of a tile, so no other wave reads them).
-  const auto load = [&](KvTile<D> &x, TileIds ids, int at) {
-    if (grow && at + 64 > fresh.b0 << c.bt_log) {
-      for (int i = max(fresh.b0, at >> c.bt_log); i <= min(fresh.b1, (at + 63) >> c.bt_log); ++i)
-        append_block<BF16, D>(a, pair, fresh, i);
-      __threadfence_block();
-    }
-    load_tile<D>(c, ids, at, x);
-  };
-  const int step = 64 * waves;
-  int base = from + 64 * wave;
-  if (base < to) {
-    if constexpr (prefetches(BF16, D, NT)) {
-      // the next tile's codes and the ids of the one after on their way
-      KvTile<D> x, y;
-      TileIds ix = tile_ids(c, row, base, to), iy = tile_ids(c, row, base + step, to);
-      load(x, ix, base);
-      for (;;) {
-        if (base + step < to) load(y, iy, base + step);
-        const TileIds ix2 = tile_ids(c, row, base + 2 * step, to);
-        work(x, ix, base);
-        base += step;
-        if (base >= to) break;
-        ix = ix2;
-        if (base + step < to) load(x, ix, base + step);
-        const TileIds iy2 = tile_ids(c, row, base + 2 * step, to);
-        work(y, iy, base);
-        base += step;
-        if (base >= to) break;
-        iy = iy2;
-      }
-    } else {
-      KvTile<D> x;
-      TileIds ids = tile_ids(c, row, base, to);
-      for (; base < to; base += step) {
-        load(x, ids, base);
-        const TileIds next = tile_ids(c, row, base + step, to);
-        work(x, ids, base);
-        ids = next;
-      }
-    }
+    ids = next;
+    load_v<D>(c, ids.v, base + step, vt);
   }
 
   // join the waves, 16 query rows at a time
@@ -303,7 +326,7 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
   for (int nt = 0; nt < NT; ++nt) {
     float l = sum[nt] + __shfl_xor(sum[nt], 16);
     l += __shfl_xor(l, 32);
-    __syncthreads();                                         // the queries, or the last rows, are done with
+    lds_barrier();                                         // the queries, or the last rows, are done with
     if (nt * 16 + m < R && g == 0) {
       ml[(wave * 16 + m) * 2] = mx[nt];
       ml[(wave * 16 + m) * 2 + 1] = l;
@@ -312,7 +335,7 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
 #pragma unroll
       for (int e = 0; e < D / 16; ++e)
         *reinterpret_cast<f32x4 *>(oo + (wave * 16 + m) * P + 16 * e + 4 * g) = o[nt][e];
-    __syncthreads();
+    lds_barrier();
     // every wave has read the old length
     if (nt == 0 && grow && a.splits == 1 && t == 0) c.lens[pair] = total;
     for (int i = t; i < 16 * (D / 4); i += blockDim.x) {
@@ -413,9 +436,10 @@ void allow_lds() {
 }
 
 template <bool BF16, int D, int NT>
-hipError_t attend(const CacheStepArgs &a, int most, hipStream_t s) {
+hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const int pairs = a.num_seqs * a.c.Hkv;
-  const int waves = NT == 1 && most > 256 ? 8 : 4;
+  // where workgroups are few, eight waves shorten each; else more workgroups fill the units evenly
+  const int waves = max_waves(NT) == 8 && a.chunk > 256 && (NT == 2 || pairs * a.splits < 256) ? 8 : 4;
   const int q = NT * (D / 32) * (BF16 ? 1 : 3) * 1024, o = waves * (128 + 64 * o_pitch<D>());
   allow_lds<BF16, D, NT>();
   hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(pairs * a.splits), dim3(64 * waves), std::max(q, o), s, a);
@@ -430,9 +454,9 @@ hipError_t attend(const CacheStepArgs &a, int most, hipStream_t s) {
 
 CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens) {
   CachePlan p{};
-  // two workgroups a compute unit, each of at least 1024 rows
-  const int64_t want = std::max<int64_t>(1, 512 / pairs);
-  const int64_t by_rows = std::max<int64_t>(1, max_tokens / 1024);
+  // a workgroup a compute unit, each of at least 256 rows
+  const int64_t want = (256 + pairs - 1) / pairs;
+  const int64_t by_rows = std::max<int64_t>(1, max_tokens / 256);
   p.splits = (int)std::min(want, by_rows);
   p.chunk = (int)((((int64_t)max_tokens + p.splits - 1) / p.splits + 63) / 64 * 64);
   if (p.splits > 1) {
@@ -444,10 +468,10 @@ CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens) {
 }
 
 hipError_t launch_cache_attend(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s) {
-  const int R = a.c.Hq / a.c.Hkv * a.tokens, most = a.chunk * a.splits;
+  const int R = a.c.Hq / a.c.Hkv * a.tokens;
 #define ATTEND(nt)                                                                   \
-  return bf16 ? (head_dim == 128 ? attend<true, 128, nt>(a, most, s) : attend<true, 64, nt>(a, most, s)) \
-              : (head_dim == 128 ? attend<false, 128, nt>(a, most, s) : attend<false, 64, nt>(a, most, s))
+  return bf16 ? (head_dim == 128 ? attend<true, 128, nt>(a, s) : attend<true, 64, nt>(a, s)) \
+              : (head_dim == 128 ? attend<false, 128, nt>(a, s) : attend<false, 64, nt>(a, s))
   if (R <= 16) ATTEND(1);
   if (R <= 32) ATTEND(2);
   if (R <= 48) ATTEND(3);
