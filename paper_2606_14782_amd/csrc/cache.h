@@ -73,6 +73,7 @@ struct CacheStepArgs {
   void *out;
   float *lse;              // optional
   float scale_log2;        // log2(e) / sqrt(d)
+  unsigned group_magic;    // 2^16 / G, rounded up (set by the launch)
   // Division of a pair's rows: `splits` workgroups of `chunk` rows (more where
   // the pair is longer); with several, each leaves its part in work.
   int splits, chunk;
@@ -99,7 +100,10 @@ hipError_t launch_cache_tables(CacheTablesArgs a, hipStream_t s);
 hipError_t launch_cache_store(const CacheStoreArgs &a, bool bf16, int head_dim, int most_rows, hipStream_t s);
 hipError_t launch_cache_load(const CacheLoadArgs &a, bool bf16, int head_dim, hipStream_t s);
 hipError_t launch_cache_append(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s);
-hipError_t launch_cache_attend(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s);
+// Whether an attend of q_rows query rows per pair also appends a's new rows
+// (a.k not NULL); otherwise one workgroup would read rows that another writes.
+bool cache_appends(int q_rows);
+hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStream_t s);
 hipError_t launch_cache_advance(const CacheMoveArgs &a, hipStream_t s);
 
 }  // namespace bacon

@@ -437,6 +437,12 @@ bacon_status bacon_cache_step(bacon_cache *c, int32_t layer, int32_t first_seq, 
   s.k_stride = k_stride;
   s.v_stride = v_stride;
   set_query(&s, c, d_q, q_stride, max_tokens, d_out, d_lse, d_work);
+  if (!cache_appends(c->shape.num_q_heads / c->shape.num_kv_heads * tokens)) {
+    TRY(launched(launch_cache_append(s, c->shape.dtype == BACON_BF16, c->shape.head_dim,
+                                     static_cast<hipStream_t>(stream)),
+                 "cache_append"));
+    s.k = s.v = nullptr;
+  }
   return launched(launch_cache_attend(s, c->shape.dtype == BACON_BF16, c->shape.head_dim,
                                       static_cast<hipStream_t>(stream)),
                   "cache_step");

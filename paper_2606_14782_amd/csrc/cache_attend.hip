@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_dev.h"
 
@@ -119,16 +120,36 @@ __device__ __forceinline__ float xor16_32_max(float v) {
   return fmaxf(v, __shfl_xor(v, 32));
 }
 
-// Waves of a workgroup: 8 fill a compute unit at 256 registers a lane; more
-// query rows hold more outputs and take 4 waves of up to 512.
-constexpr int max_waves(int nt) { return nt <= 2 ? 8 : 4; }
+// Most waves of a workgroup: 8 fill a compute unit at 256 registers a lane;
+// 32 fp32 queries of 128 dimensions need more and take 4.
+constexpr int max_waves(bool bf16, int d, int nt) { return nt == 2 && !bf16 && d == 128 ? 4 : 8; }
+
 constexpr float kFloor = -1e30f;       // maximum of no logits
 
 template <int D>
 constexpr int o_pitch() { return D + 4; }
 
+// Token of query row r < 64 of a pair (r / G).
+__device__ __forceinline__ int token_of(const CacheStepArgs &a, int r) { return (int)((unsigned)r * a.group_magic >> 16); }
+
+// Four dimensions of a query's output from their weighted sums, and its normaliser.
+template <bool BF16, int D>
+__device__ __forceinline__ void store_out(const CacheStepArgs &a, int64_t at, int dim, f32x4 acc, float l, float top,
+                                          bool none) {
+  const float inv = none ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc[e] = none ? 0.f : acc[e] * inv;
+  if constexpr (BF16) {
+    const u32x2 u = {float_bf16(acc[0]) | float_bf16(acc[1]) << 16, float_bf16(acc[2]) | float_bf16(acc[3]) << 16};
+    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + at * D + dim) = u;
+  } else {
+    *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at * D + dim) = acc;
+  }
+  if (dim == 0 && a.lse) a.lse[at] = none ? -INFINITY : (top + __log2f(l)) * kLn2f;
+}
+
 template <bool BF16, int D, int NT>
-__global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepArgs a) {
+__global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(CacheStepArgs a) {
   constexpr int QP = BF16 ? 1 : 3;     // parts of a query: bf16 is one; fp32 needs three for its 24 bits
   constexpr int PP = BF16 ? 2 : 3;     // parts of a weight: one would add 2^-9 to a bf16 output's own 2^-9
   constexpr int KS = D / 32;
@@ -137,7 +158,7 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
   const CacheDev &c = a.c;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), waves = blockDim.x >> 6;
   const int m = lane & 15, g = lane >> 4;
-  const int split = blockIdx.x % a.splits, bh = blockIdx.x / a.splits;
+  const int split = blockIdx.x % a.splits, bh = blockIdx.x / a.splits, row0 = blockIdx.y * 32;   // of the queries
   const int b = bh / c.Hkv, h = bh - b * c.Hkv;
   const int G = c.Hq / c.Hkv, R = G * a.tokens;
   const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
@@ -171,6 +192,7 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
   if (base != guess) {
     id0 = any_ids(c, row, base);
     id1 = any_ids(c, row, base + step);
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt 0, as below
   }
   TileIds ids = bound_ids(id0, base, to);
   const bool late = grow && base + 64 > fresh.b0 << c.bt_log;
@@ -195,22 +217,33 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
     load_v<D>(c, ids.v, base, vt);
   }
 
-  // queries: lane (n, g) holds 8 dimensions of query n for each step of 32
-  for (int i = wave; i < NT * KS; i += waves) {
-    const int nt = i / KS, s = i - nt * KS, r = nt * 16 + m;
-    float x[8] = {};
-    const int j = r / G, hq = h * G + (r - j * G);
-    if (r < R)
-      load8<BF16>(a.q, ((int64_t)b * a.tokens + j) * a.q_stride + hq * D + 64 * (s >> 1) + 16 * g + 8 * (s & 1), x);
+  // queries: lane (n, g) holds 8 dimensions of query n for each step of 32,
+  // all of a wave's asked for at once
+  constexpr int QI = (NT * KS + 3) / 4;
+  float qx[QI][8];
+#pragma unroll
+  for (int u = 0; u < QI; ++u) {
+    const int i = wave + u * waves, nt = i / KS, s = i - nt * KS, r = row0 + nt * 16 + m;
+    const int j = token_of(a, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qx[u][e] = 0.f;
+    if (i < NT * KS && r < R)
+      load8<BF16>(a.q, ((int64_t)b * a.tokens + j) * a.q_stride + (h * G + r - j * G) * D + 64 * (s >> 1) + 16 * g + 8 * (s & 1),
+                  qx[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < QI; ++u) {
+    const int i = wave + u * waves;
+    if (i >= NT * KS) continue;
     bf16x8 part[QP];
-    split8<QP>(x, part);
+    split8<QP>(qx[u], part);
 #pragma unroll
     for (int p = 0; p < QP; ++p) q_lds[(i * QP + p) * 64 + lane] = part[p];
   }
   int end[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = nt * 16 + m, j = r / G;
+    const int r = row0 + nt * 16 + m, j = token_of(a, r);
     end[nt] = r < R && j < count ? max(0, total - (count - 1 - j)) : 0;
   }
   lds_barrier();
@@ -318,59 +351,60 @@ __global__ __launch_bounds__(64 * max_waves(NT)) void k_cache_attend(CacheStepAr
     load_v<D>(c, ids.v, base + step, vt);
   }
 
-  // join the waves, 16 query rows at a time
-  float *ml = reinterpret_cast<float *>(lds);                // [waves][16][2]
-  float *oo = ml + waves * 32;                               // [waves][16][o_pitch]
+  // Join the waves through LDS, all query rows at once.
+  float *ml = reinterpret_cast<float *>(lds);                // [waves][NT * 16][2]
+  float *oo = ml + waves * NT * 32;                          // [waves][NT * 16][o_pitch]
   constexpr int P = o_pitch<D>();
+  lds_barrier();                                             // the queries are done with
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     float l = sum[nt] + __shfl_xor(sum[nt], 16);
     l += __shfl_xor(l, 32);
-    lds_barrier();                                         // the queries, or the last rows, are done with
-    if (nt * 16 + m < R && g == 0) {
-      ml[(wave * 16 + m) * 2] = mx[nt];
-      ml[(wave * 16 + m) * 2 + 1] = l;
-    }
-    if (nt * 16 + m < R)
+    const int n = nt * 16 + m, at = wave * NT * 16 + n;
+    if (row0 + n >= R) continue;
+    if (g == 0) *reinterpret_cast<float2 *>(ml + at * 2) = make_float2(mx[nt], l);
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e)
-        *reinterpret_cast<f32x4 *>(oo + (wave * 16 + m) * P + 16 * e + 4 * g) = o[nt][e];
-    lds_barrier();
-    // every wave has read the old length
-    if (nt == 0 && grow && a.splits == 1 && t == 0) c.lens[pair] = total;
-    for (int i = t; i < 16 * (D / 4); i += blockDim.x) {
-      const int n = i / (D / 4), dim = i % (D / 4) * 4, r = nt * 16 + n;
-      if (r >= R) continue;
-      float top = kFloor;
-      for (int w = 0; w < waves; ++w) top = fmaxf(top, ml[(w * 16 + n) * 2]);
-      float l = 0.f;
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-      for (int w = 0; w < waves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + n) * 2] - top);
-        l += f * ml[(w * 16 + n) * 2 + 1];
-        acc += f * *reinterpret_cast<const f32x4 *>(oo + (w * 16 + n) * P + dim);
+    for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4 *>(oo + at * P + 16 * e + 4 * g) = o[nt][e];
+  }
+  lds_barrier();
+  // every wave has read the old length
+  if (grow && a.splits == 1 && t == 0) c.lens[pair] = total;
+  const auto join = [&](auto count_waves) {
+    constexpr int WAVES = decltype(count_waves)::value;
+    for (int i = t; i < min(NT * 16, R - row0) * (D / 4); i += 64 * WAVES) {
+      const int n = i / (D / 4), dim = i % (D / 4) * 4, r = row0 + n;
+      float2 part[WAVES];
+      f32x4 x[WAVES];
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        part[w] = *reinterpret_cast<const float2 *>(ml + (w * NT * 16 + n) * 2);
+        x[w] = *reinterpret_cast<const f32x4 *>(oo + (w * NT * 16 + n) * P + dim);
       }
-      const int j = r / G;
+      float top = kFloor, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) top = fmaxf(top, part[w].x);
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(part[w].x - top);
+        l += f * part[w].y;
+        acc += f * x[w];
+      }
+      const int j = token_of(a, r);
       const bool none = j >= count || !(l > 0.f);
       if (a.splits > 1) {
         const int64_t at = ((int64_t)bh * a.splits + split) * R + r;
         if (dim == 0) a.part_ml[at] = make_float2(top, none ? 0.f : l);
         *reinterpret_cast<f32x4 *>(a.part_o + at * D + dim) = acc;
       } else {
-        const int64_t at = ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G);
-        const float inv = none ? 0.f : 1.f / l;
-        f32x4 y = acc * inv;
-        if (none) y = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (BF16) {
-          const u32x2 u = {float_bf16(y[0]) | float_bf16(y[1]) << 16, float_bf16(y[2]) | float_bf16(y[3]) << 16};
-          *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + at * D + dim) = u;
-        } else {
-          *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at * D + dim) = y;
-        }
-        if (dim == 0 && a.lse) a.lse[at] = none ? -INFINITY : (top + __log2f(l)) * kLn2f;
+        store_out<BF16, D>(a, ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G), dim, acc, l, top, none);
       }
     }
-  }
+  };
+  if (waves == 8)
+    join(std::integral_constant<int, 8>{});
+  else
+    join(std::integral_constant<int, 4>{});
 }
 
 // Joins the parts of one query row: 256 threads, D / 4 of them a part, the
@@ -383,7 +417,7 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
   const CacheDev &c = a.c;
   const int t = threadIdx.x, G = c.Hq / c.Hkv, R = G * a.tokens;
   const int r = blockIdx.x % R, bh = blockIdx.x / R;
-  const int b = bh / c.Hkv, h = bh - b * c.Hkv, j = r / G;
+  const int b = bh / c.Hkv, h = bh - b * c.Hkv, j = token_of(a, r);
   if (a.k && r == 0 && t == 0) {       // the new length, once every part was formed with the old one
     const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
     const NewRows n = new_rows(a, pair, b, h, pair_len(c, pair), call_count(a, b));
@@ -412,16 +446,13 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
     l += l_lds[i];
     acc += acc_lds[i * TR + t];
   }
-  const bool none = !(l > 0.f);
-  const int64_t at = ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G);
-  f32x4 y = acc * (none ? 0.f : 1.f / l);
-  if constexpr (BF16) {
-    const u32x2 u = {float_bf16(y[0]) | float_bf16(y[1]) << 16, float_bf16(y[2]) | float_bf16(y[3]) << 16};
-    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + at * D + t * 4) = u;
-  } else {
-    *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at * D + t * 4) = y;
-  }
-  if (t == 0 && a.lse) a.lse[at] = none ? -INFINITY : (top + __log2f(l)) * kLn2f;
+  store_out<BF16, D>(a, ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G), t * 4, acc, l, top, !(l > 0.f));
+}
+
+template <bool BF16, int D, int NT>
+constexpr int attend_lds(int waves) {
+  const int q = NT * (D / 32) * (BF16 ? 1 : 3) * 1024, o = waves * NT * (128 + 64 * o_pitch<D>());
+  return q > o ? q : o;
 }
 
 // Allows a kernel more dynamic LDS than the default 64 KB, once per instance.
@@ -429,7 +460,8 @@ template <bool BF16, int D, int NT>
 void allow_lds() {
   static const bool done = [] {
     (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_cache_attend<BF16, D, NT>),
-                              hipFuncAttributeMaxDynamicSharedMemorySize, 8 * (128 + 64 * o_pitch<D>()));
+                              hipFuncAttributeMaxDynamicSharedMemorySize,
+                              attend_lds<BF16, D, NT>(max_waves(BF16, D, NT)));
     return true;
   }();
   (void)done;
@@ -437,16 +469,15 @@ void allow_lds() {
 
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
-  const int pairs = a.num_seqs * a.c.Hkv;
-  // where workgroups are few, eight waves shorten each; else more workgroups fill the units evenly
-  const int waves = max_waves(NT) == 8 && a.chunk > 256 && (NT == 2 || pairs * a.splits < 256) ? 8 : 4;
-  const int q = NT * (D / 32) * (BF16 ? 1 : 3) * 1024, o = waves * (128 + 64 * o_pitch<D>());
+  const int pairs = a.num_seqs * a.c.Hkv, R = a.c.Hq / a.c.Hkv * a.tokens, groups = (R + 31) / 32;
+  // where workgroups are few, or each holds 32 queries, eight waves shorten
+  // them; else more workgroups fill the units evenly
+  const int waves =
+      max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (NT == 2 || pairs * a.splits < 256) ? 8 : 4;
   allow_lds<BF16, D, NT>();
-  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(pairs * a.splits), dim3(64 * waves), std::max(q, o), s, a);
-  if (a.splits > 1) {
-    const int R = a.c.Hq / a.c.Hkv * a.tokens;
-    hipLaunchKernelGGL((k_cache_join<BF16, D>), dim3(pairs * R), dim3(256), 0, s, a);
-  }
+  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(pairs * a.splits, groups), dim3(64 * waves),
+                     (attend_lds<BF16, D, NT>(waves)), s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((k_cache_join<BF16, D>), dim3(pairs * R), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -467,15 +498,16 @@ CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens) {
   return p;
 }
 
-hipError_t launch_cache_attend(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s) {
-  const int R = a.c.Hq / a.c.Hkv * a.tokens;
-#define ATTEND(nt)                                                                   \
-  return bf16 ? (head_dim == 128 ? attend<true, 128, nt>(a, s) : attend<true, 64, nt>(a, s)) \
+bool cache_appends(int q_rows) { return q_rows <= 32; }
+
+hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStream_t s) {
+  const int G = a.c.Hq / a.c.Hkv, R = G * a.tokens;
+  a.group_magic = (65536 + G - 1) / G;
+#define ATTEND(nt)                                                                                \
+  return bf16 ? (head_dim == 128 ? attend<true, 128, nt>(a, s) : attend<true, 64, nt>(a, s))      \
               : (head_dim == 128 ? attend<false, 128, nt>(a, s) : attend<false, 64, nt>(a, s))
   if (R <= 16) ATTEND(1);
-  if (R <= 32) ATTEND(2);
-  if (R <= 48) ATTEND(3);
-  ATTEND(4);
+  ATTEND(2);
 #undef ATTEND
 }
 
