@@ -74,6 +74,7 @@ struct CacheStepArgs {
   float *lse;              // optional
   float scale_log2;        // log2(e) / sqrt(d)
   unsigned group_magic;    // 2^16 / G, rounded up (set by the launch)
+  int groups;              // of 32 query rows: 1 or 2 (set by the launch)
   // Division of a pair's rows: `splits` workgroups of `chunk` rows (more where
   // the pair is longer); with several, each leaves its part in work.
   int splits, chunk;

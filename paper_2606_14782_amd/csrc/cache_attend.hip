@@ -158,7 +158,12 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   const CacheDev &c = a.c;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), waves = blockDim.x >> 6;
   const int m = lane & 15, g = lane >> 4;
-  const int split = blockIdx.x % a.splits, bh = blockIdx.x / a.splits, row0 = blockIdx.y * 32;   // of the queries
+  // The workgroups of a second 32 query rows follow the first's eight apart: on
+  // the same die (workgroups go to the eight in turn), which then still holds the codes.
+  const int unit = a.groups == 1 ? blockIdx.x : (blockIdx.x >> 4) * 8 + (blockIdx.x & 7);
+  const int row0 = a.groups == 1 ? 0 : (blockIdx.x & 8) * 4;
+  if (unit >= a.num_seqs * c.Hkv * a.splits) return;
+  const int split = unit % a.splits, bh = unit / a.splits;
   const int b = bh / c.Hkv, h = bh - b * c.Hkv;
   const int G = c.Hq / c.Hkv, R = G * a.tokens;
   const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
@@ -395,7 +400,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
       if (a.splits > 1) {
         const int64_t at = ((int64_t)bh * a.splits + split) * R + r;
         if (dim == 0) a.part_ml[at] = make_float2(top, none ? 0.f : l);
-        *reinterpret_cast<f32x4 *>(a.part_o + at * D + dim) = acc;
+        *reinterpret_cast<f32x4 *>(a.part_o + at * D + dim) = acc;   // finite, also where there is none
       } else {
         store_out<BF16, D>(a, ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G), dim, acc, l, top, none);
       }
@@ -407,44 +412,70 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     join(std::integral_constant<int, 4>{});
 }
 
-// Joins the parts of one query row: 256 threads, D / 4 of them a part, the
-// parts divided among the others.
+// Joins the parts of one query row: D / 4 threads a part, each group of them
+// every SP-th part with a running maximum, then the groups through LDS.
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
   constexpr int TR = D / 4, SP = 256 / TR;
-  __shared__ float red[4];
-  __shared__ f32x4 acc_lds[256];
+  __shared__ f32x4 acc_lds[SP][TR];
+  __shared__ float2 ml_lds[SP];
   const CacheDev &c = a.c;
-  const int t = threadIdx.x, G = c.Hq / c.Hkv, R = G * a.tokens;
+  const int t = threadIdx.x, G = c.Hq / c.Hkv, R = G * a.tokens, dim = t % TR, group = t / TR;
   const int r = blockIdx.x % R, bh = blockIdx.x / R;
   const int b = bh / c.Hkv, h = bh - b * c.Hkv, j = token_of(a, r);
-  if (a.k && r == 0 && t == 0) {       // the new length, once every part was formed with the old one
+  const float2 *ml = a.part_ml + (int64_t)bh * a.splits * R + r;
+  const f32x4 *o = reinterpret_cast<const f32x4 *>(a.part_o) + ((int64_t)bh * a.splits * R + r) * TR + dim;
+  float top = kFloor, l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i = group; i < a.splits; i += 4 * SP) {
+    float2 x[4];
+    f32x4 y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t at = (int64_t)min(i + u * SP, a.splits - 1) * R;
+      x[u] = ml[at];
+      y[u] = o[at * TR];
+      if (i + u * SP >= a.splits) x[u] = make_float2(kFloor, 0.f);
+    }
+    const float m = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), top);
+    const float f = __builtin_amdgcn_exp2f(top - m);
+    l *= f;
+    acc *= f;
+    top = m;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float g = x[u].y > 0.f ? __builtin_amdgcn_exp2f(x[u].x - m) : 0.f;
+      l += g * x[u].y;
+      acc += g * y[u];
+    }
+  }
+  acc_lds[group][dim] = acc;
+  if (dim == 0) ml_lds[group] = make_float2(top, l);
+  // the new length, once every part was formed with the old one
+  if (a.k && r == 0 && t == 255) {
     const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
     const NewRows n = new_rows(a, pair, b, h, pair_len(c, pair), call_count(a, b));
     if (n.count > 0 && n.room) c.lens[pair] = n.len + n.count;
   }
-  const float2 *ml = a.part_ml + (int64_t)bh * a.splits * R + r;
-  float top = kFloor;
-  for (int i = t; i < a.splits; i += 256) top = fmaxf(top, ml[(int64_t)i * R].x);
-  top = block_max(top, red);
-  float l = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int i = t / TR; i < a.splits; i += SP) {
-    const float2 x = ml[(int64_t)i * R];
-    if (!(x.y > 0.f)) continue;
-    const float f = __builtin_amdgcn_exp2f(x.x - top);
-    l += f * x.y;
-    acc += f * *reinterpret_cast<const f32x4 *>(a.part_o + (((int64_t)bh * a.splits + i) * R + r) * D + t % TR * 4);
-  }
-  __shared__ float l_lds[SP];
-  acc_lds[t] = acc;
-  if (t % TR == 0) l_lds[t / TR] = l;
-  __syncthreads();
+  lds_barrier();
   if (t >= TR) return;
-  l = l_lds[0];
-  for (int i = 1; i < SP; ++i) {
-    l += l_lds[i];
-    acc += acc_lds[i * TR + t];
+  float2 x[SP];
+  f32x4 y[SP];
+#pragma unroll
+  for (int i = 0; i < SP; ++i) {
+    x[i] = ml_lds[i];
+    y[i] = acc_lds[i][dim];
+  }
+  top = x[0].x;
+#pragma unroll
+  for (int i = 1; i < SP; ++i) top = fmaxf(top, x[i].x);
+  l = 0.f;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < SP; ++i) {
+    const float g = __builtin_amdgcn_exp2f(x[i].x - top);
+    l += g * x[i].y;
+    acc += g * y[i];
   }
   store_out<BF16, D>(a, ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G), t * 4, acc, l, top, !(l > 0.f));
 }
@@ -469,13 +500,13 @@ void allow_lds() {
 
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
-  const int pairs = a.num_seqs * a.c.Hkv, R = a.c.Hq / a.c.Hkv * a.tokens, groups = (R + 31) / 32;
+  const int pairs = a.num_seqs * a.c.Hkv, R = a.c.Hq / a.c.Hkv * a.tokens, units = pairs * a.splits;
   // where workgroups are few, or each holds 32 queries, eight waves shorten
   // them; else more workgroups fill the units evenly
   const int waves =
-      max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (NT == 2 || pairs * a.splits < 256) ? 8 : 4;
+      max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (NT == 2 || units < 256) ? 8 : 4;
   allow_lds<BF16, D, NT>();
-  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(pairs * a.splits, groups), dim3(64 * waves),
+  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(a.groups == 1 ? units : (units + 7) / 8 * 16), dim3(64 * waves),
                      (attend_lds<BF16, D, NT>(waves)), s, a);
   if (a.splits > 1) hipLaunchKernelGGL((k_cache_join<BF16, D>), dim3(pairs * R), dim3(256), 0, s, a);
   return hipGetLastError();
@@ -503,6 +534,7 @@ bool cache_appends(int q_rows) { return q_rows <= 32; }
 hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStream_t s) {
   const int G = a.c.Hq / a.c.Hkv, R = G * a.tokens;
   a.group_magic = (65536 + G - 1) / G;
+  a.groups = R > 32 ? 2 : 1;
 #define ATTEND(nt)                                                                                \
   return bf16 ? (head_dim == 128 ? attend<true, 128, nt>(a, s) : attend<true, 64, nt>(a, s))      \
               : (head_dim == 128 ? attend<false, 128, nt>(a, s) : attend<false, 64, nt>(a, s))
