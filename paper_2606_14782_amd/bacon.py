@@ -557,13 +557,14 @@ class Cache:
 
     def _layers(self, xs, name, dtype, shape):
         """Host array of per-layer pointers: a list of tensors, or one with the layers first."""
+        n = len(xs)
         if isinstance(xs, self._torch.Tensor):
-            if xs.dim() < 1 or shape is not None and tuple(xs.shape[1:]) != shape:
+            if shape is not None and xs.shape[1:] != shape:
                 raise BaconError(ERR_INVALID, f"{name} has shape {tuple(xs.shape)}")
             base = self._whole(xs, name, dtype)
             step = xs.stride(0) * xs.element_size()
-            return (C.c_void_p * len(xs))(*[base + step * i for i in range(len(xs))])
-        return (C.c_void_p * len(xs))(*[self._whole(x, name, dtype, shape) for x in xs])
+            return (C.c_uint64 * n)(*range(base, base + step * n, step)) if step else (C.c_uint64 * n)(base)
+        return (C.c_uint64 * n)(*[self._whole(x, name, dtype, shape) for x in xs])
 
     def bacon_cache_store(self, batch: BatchLayout, ks, vs, idxs=None, first_seq=0, first_layer=0):
         """The kept rows of the layers first_layer, ..: ks, vs per-layer [T, Hkv,
@@ -588,10 +589,14 @@ class Cache:
         if out is None:
             if min(shape) < 1:
                 raise BaconError(ERR_INVALID, f"a load of shape {shape}")
-            out = self._torch.empty((2, *shape), dtype=self.torch_dtype, device=self.device).unbind(0)
-        k, v = out
-        self._call(self._L.bacon_cache_load, first_layer, nl, first_seq, ns, first_token, count,
-                   self._whole(k, "k_out", self.torch_dtype, shape), self._whole(v, "v_out", self.torch_dtype, shape))
+            both = self._torch.empty((2, *shape), dtype=self.torch_dtype, device=self.device)
+            k, v = both.unbind(0)
+            kp = both.data_ptr()
+            vp = kp + both.nbytes // 2
+        else:
+            k, v = out
+            kp, vp = (self._whole(k, "k_out", self.torch_dtype, shape), self._whole(v, "v_out", self.torch_dtype, shape))
+        self._call(self._L.bacon_cache_load, first_layer, nl, first_seq, ns, first_token, count, kp, vp)
         return k, v
 
     def bacon_cache_append(self, layer, k, v, counts=None, first_seq=0):
