@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     if (!fresh.room && split == 0 && t == 0) atomicOr(c.err, (unsigned)BACON_CACHE_NO_BLOCKS);
   }
   const bool grow = append && fresh.room;
-  const int total = grow ? len + count : len;
+  const int total = __builtin_amdgcn_readfirstlane(grow ? len + count : len);
   // this workgroup's rows
   const int chunk = max(a.chunk, ((total + a.splits - 1) / a.splits + 63) & ~63);
   const int from = split * chunk, to = min(total, from + chunk);
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   if (base != guess) {
     id0 = any_ids(c, row, base);
     id1 = any_ids(c, row, base + step);
-    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt 0, as below
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt 0: else the loop waits for ids after codes
   }
   TileIds ids = bound_ids(id0, base, to);
   const bool late = grow && base + 64 > fresh.b0 << c.bt_log;
@@ -213,15 +213,17 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
       const int at = (i << c.bt_log & ~63) - from;
       if (at >= 0 && at < to - from && (at >> 6) % waves == wave) append_block<BF16, D>(a, pair, fresh, i);
     }
+    // (a wave's loads follow its stores through the unit's L1 in order: the
+    // fence keeps the compiler to that and waits for nothing)
     __threadfence_block();
-    // all of it ends here: what the compiler takes to be still in flight it
-    // waits for again in every round of the loop below
-    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt 0
   }
   if (base < to && late) {
     load_k<D>(c, ids.k, base, kt);
     load_v<D>(c, ids.v, base, vt);
   }
+
+  // (taken to be waited for here: nothing in the loop then waits for them)
+  asm volatile("" : "+v"(id1.k), "+v"(id1.v));
 
   // queries: lane (n, g) holds 8 dimensions of query n for each step of 32,
   // all of a wave's asked for at once
@@ -502,10 +504,10 @@ void allow_lds() {
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const int pairs = a.num_seqs * a.c.Hkv, R = a.c.Hq / a.c.Hkv * a.tokens, units = pairs * a.splits;
-  // Eight waves shorten a workgroup where workgroups are few or its rows many
-  // (32 sequences over 32K rows: 352 us, with four waves 367), and where it holds 32 queries; four
-  // start and join sooner (64 sequences over 300 to 993 rows: 18 us, with eight 23).
-  const bool eight = max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (NT == 2 || units < 256 || a.chunk >= 4096);
+  // Eight waves shorten a workgroup where workgroups are few (one sequence over 288 rows: 6.9
+  // us, with four waves 7.5) and where it holds 32 queries; elsewhere four start and join
+  // sooner (64 sequences over 300 to 993 rows: 18 us, with eight 23; 32 over 32K rows: 352 both ways).
+  const bool eight = max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (NT == 2 || units < 256);
   const int waves = eight ? 8 : 4;
   allow_lds<BF16, D, NT>();
   hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(a.groups == 1 ? units : (units + 7) / 8 * 8 * a.groups), dim3(64 * waves),
