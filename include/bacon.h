@@ -353,7 +353,8 @@ int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
  * The rows that a prompt's compression keeps (bacon_select_topk, the fused
  * calls) move into blocks of block_tokens tokens of one (layer, sequence, KV
  * head) -- a pair below -- each with K and V in e4m3 and one scale for its K
- * and one for its V.  New tokens are appended there, and decoding attends over them.
+ * and one for its V.  New tokens are appended there, and decoding attends over
+ * them.
  *
  *   scale of a block of rows X:  2^e, e the smallest integer with
  *       max |X| <= 448 2^e, held to -100 <= e <= 120 (max |X| = 0: e = -100)
@@ -386,10 +387,10 @@ int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
  * no allocation, no synchronisation, the caller's buffers, all work on the
  * given stream.  Calls on one cache run one after the other (one stream, or
  * events between streams), but attends and loads of one cache may run beside
- * each other, each attend with a work buffer of its own.  What only the device can see is
- * bounded there and noted in the error word: a pair that finds no blocks, an
- * append beyond the table, an id outside the pool (its rows count as absent),
- * an idx entry outside the candidates (its row is zero). */
+ * each other, each attend with a work buffer of its own.  What only the device
+ * can see is bounded there and noted in the error word: a pair that finds no
+ * blocks, an append beyond the table, an id outside the pool (its rows count
+ * as absent), an idx entry outside the candidates (its row is zero). */
 
 typedef struct {
   int32_t num_layers;
@@ -453,12 +454,15 @@ bacon_status bacon_cache_tables(bacon_cache *cache, const bacon_batch *batch, in
 /* The kept rows of num_layers layers of a prompt, quantised into the blocks
  * that bacon_cache_tables gave (the same batch and first_seq).  d_k, d_v: host
  * arrays of num_layers device pointers to the layers' K and V [T, Hkv, d], as
- * bacon_compact reads them; d_idx: such an array of their idx.  The pair's rows are its kept positions in
- * ascending order, then the window's; d_idx NULL stands for idx entries 0, 1, 2, ...
- * (every row, where the budget is N_b - W). */
+ * bacon_compact reads them; d_idx: such an array of their idx, idx_count
+ * entries each.  The pair's rows are its kept positions in ascending order,
+ * then the window's; d_idx NULL stands for idx entries 0, 1, 2, ... (every row,
+ * where the budget is N_b - W).  An entry past idx_count, or outside the
+ * candidates, gives a zero row (BAD_INDEX). */
 bacon_status bacon_cache_store(bacon_cache *cache, const bacon_batch *batch, int32_t first_seq,
                                int32_t first_layer, int32_t num_layers, const void *const *d_k,
-                               const void *const *d_v, const int32_t *const *d_idx, void *stream);
+                               const void *const *d_v, const int32_t *const *d_idx, int64_t idx_count,
+                               void *stream);
 
 /* The values held: rows first_token .. first_token + count - 1 of every pair
  * of the named layers and sequences to d_k_out, d_v_out [num_layers, num_seqs,
@@ -470,10 +474,11 @@ bacon_status bacon_cache_load(bacon_cache *cache, int32_t first_layer, int32_t n
 
 /* Appends new tokens of one layer: token j of sequence b is row b * tokens + j
  * of d_k and d_v, rows of Hkv x d elements k_stride and v_stride elements
- * apart (>= Hkv d, 16 bytes a multiple; a view of a fused projection's output will do).  d_counts [num_seqs] (int32,
- * device, optional; held to 0..tokens) gives each sequence's own number of new tokens.  Every pair's length
- * grows by that number.  In each block touched, e is the larger of the old
- * rows' (if the block has any) and of the one the new rows need; where it
+ * apart (>= Hkv d, a multiple of 16 bytes; a view of a fused projection's
+ * output will do).  d_counts [num_seqs] (int32, device, optional; held to
+ * 0..tokens) gives each sequence's own number of new tokens.  Every pair's
+ * length grows by that number.  In each block touched, e is the larger of the
+ * old rows' (if the block has any) and of the one the new rows need; where it
  * grows the old codes are rounded again at it.  A pair without room (in its
  * table's blocks) is left as it is (NO_BLOCKS).  1 <= tokens <= 64. */
 bacon_status bacon_cache_append(bacon_cache *cache, int32_t layer, int32_t first_seq, int32_t num_seqs,
@@ -487,8 +492,8 @@ bacon_status bacon_cache_append(bacon_cache *cache, int32_t layer, int32_t first
  * dtype; d_lse (optional) [num_seqs, tokens, Hq] float32, the natural log of
  * the normaliser.  A query that sees no row, and a query j >= c (a padded
  * batch), gives zeros and -infinity.  G * tokens <= 64, G = Hq / Hkv.
- * max_tokens: the longest length to expect (0: the table's), which settles how the work is
- * divided; longer pairs are right, only slower.  d_work: scratch of
+ * max_tokens: the longest length to expect (0: the table's), which settles
+ * how the work is divided; longer pairs are right, only slower.  d_work: scratch of
  * bacon_cache_work_bytes (0: may be NULL), 256-byte aligned, of this call
  * alone until its work is done. */
 bacon_status bacon_cache_attend(bacon_cache *cache, int32_t layer, int32_t first_seq, int32_t num_seqs,

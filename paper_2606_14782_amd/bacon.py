@@ -133,7 +133,7 @@ def lib() -> C.CDLL:
         L.bacon_cache_free.argtypes = [vp]
         L.bacon_cache_clear.argtypes = [vp, i32, i32, vp]
         L.bacon_cache_tables.argtypes = [vp, cap, i32, vp, i32, i32, vp, i64, vp, vp]
-        L.bacon_cache_store.argtypes = [vp, cap, i32, i32, i32, vp, vp, vp, vp]
+        L.bacon_cache_store.argtypes = [vp, cap, i32, i32, i32, vp, vp, vp, i64, vp]
         L.bacon_cache_load.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]
         L.bacon_cache_append.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp]
         L.bacon_cache_attend.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, i32, vp, vp, vp, sz, vp]
@@ -440,8 +440,8 @@ class Cache:
     block_tokens * d] (uint8, e4m3) are views of that memory.  max_tokens: the
     longest a pair may become.  Tensors given to the calls are on the cache's
     device; every call runs on that device's current stream.  New tokens and
-    queries may be views of one projection's output: only the heads of a token have
-    to lie together, tokens evenly spaced.
+    queries may be views of one projection's output: only the heads of a token
+    have to lie together, tokens evenly spaced.
     """
 
     def __init__(self, num_layers, num_q_heads, num_kv_heads, head_dim, window, block_tokens, max_batch,
@@ -449,9 +449,12 @@ class Cache:
         import torch
         if block_tokens < 1:
             raise BaconError(ERR_INVALID, "block_tokens must be >= 1")
+        if dtype not in ("bf16", "fp32", BF16, FP32, torch.bfloat16, torch.float32):
+            raise BaconError(ERR_UNSUPPORTED, f"dtype {dtype} is not supported (bf16 or fp32)")
+        bf16 = dtype in ("bf16", BF16, torch.bfloat16)
         blocks = (max_tokens + block_tokens - 1) // block_tokens
         self.shape = CacheShape(num_layers, num_q_heads, num_kv_heads, head_dim, window, block_tokens,
-                                max_batch, blocks, num_blocks, BF16 if dtype in ("bf16", BF16) else FP32)
+                                max_batch, blocks, num_blocks, BF16 if bf16 else FP32)
         off = CacheOffsets()
         _check(lib().bacon_cache_layout(C.byref(self.shape), C.byref(off)))
         self._torch, self._L = torch, lib()
@@ -572,11 +575,17 @@ class Cache:
         s = self.shape
         n = len(ks)
         if len(vs) != n or idxs is not None and len(idxs) != n or n < 1:
-            raise BaconError(ERR_INVALID, f"{n} layers of K, {len(vs)} of V")
+            raise BaconError(ERR_INVALID, f"{n} layers of K, {len(vs)} of V" +
+                             ("" if idxs is None else f", {len(idxs)} of idx"))
         rows = (batch.total, s.num_kv_heads, s.head_dim)
+        idx, count = None, 0
+        if idxs is not None:
+            idx = self._layers(idxs, "idx", self._torch.int32, None)
+            count = (idxs.numel() // n if isinstance(idxs, self._torch.Tensor) else
+                     min(x.numel() for x in idxs))
         self._call(self._L.bacon_cache_store, C.byref(batch.c), first_seq, first_layer, n,
-                   self._layers(ks, "k", self.torch_dtype, rows), self._layers(vs, "v", self.torch_dtype, rows),
-                   None if idxs is None else self._layers(idxs, "idx", self._torch.int32, None))
+                   self._layers(ks, "k", self.torch_dtype, rows), self._layers(vs, "v", self.torch_dtype, rows), idx,
+                   count)
 
     def bacon_cache_load(self, count, first_token=0, first_layer=0, num_layers=None, first_seq=0, num_seqs=None,
                          out=None):

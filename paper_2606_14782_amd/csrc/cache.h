@@ -51,6 +51,7 @@ struct CacheStoreArgs {
   int first_seq, first_layer, layers;
   const void *k[kCacheLayersPerLaunch], *v[kCacheLayersPerLaunch];
   const int32_t *idx[kCacheLayersPerLaunch];   // NULL: entries 0, 1, 2, ...
+  int64_t idx_count;       // entries of each
 };
 
 struct CacheLoadArgs {

@@ -277,7 +277,8 @@ __global__ __launch_bounds__(256) void k_cache_store(CacheStoreArgs a) {
   const int h = blockIdx.y, b = blockIdx.z % a.s.batch, l = blockIdx.z / a.s.batch;
   const int64_t pair = pair_of(c, a.first_layer + l, a.first_seq + b, h);
   const int len = pair_len(c, pair), cand = a.s.cu[b + 1] - a.s.cu[b] - c.W, kept = len - c.W;
-  const int32_t *idx = a.idx[l] ? a.idx[l] + c.starts[pair] : nullptr;
+  const int32_t *idx = a.idx[l];
+  const int64_t start = c.starts[pair];
   const int group = (t >> 6) * WG + (WG == 2 ? lane >> 3 & 1 : 0);   // of the workgroup's
   const int col = lane % (D / 8) * 8, q = lane >> 4, step = gridDim.x * 64 * WG;
   const int64_t row_elems = (int64_t)c.Hkv * D, first = (int64_t)a.s.cu[b] * row_elems + h * D + col;
@@ -288,7 +289,10 @@ __global__ __launch_bounds__(256) void k_cache_store(CacheStoreArgs a) {
     for (int r = 0; r < 4; ++r) {
       const int i = i0 + r;
       int at = -1;
-      if (i < len) at = i < kept ? (idx ? idx[i] : i) : cand + (i - kept);
+      if (i >= kept && i < len)
+        at = cand + (i - kept);
+      else if (i < kept)
+        at = !idx ? i : start >= 0 && start + i < a.idx_count ? idx[start + i] : -1;
       const bool ok = (unsigned)at < (unsigned)(i < kept ? cand : cand + c.W);
       if (i < len && !ok && col == 0) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_INDEX);
 #pragma unroll

@@ -329,12 +329,13 @@ bacon_status bacon_cache_tables(bacon_cache *c, const bacon_batch *bt, int32_t f
 
 bacon_status bacon_cache_store(bacon_cache *c, const bacon_batch *bt, int32_t first_seq, int32_t first_layer,
                                int32_t num_layers, const void *const *d_k, const void *const *d_v,
-                               const int32_t *const *d_idx, void *stream) {
+                               const int32_t *const *d_idx, int64_t idx_count, void *stream) {
   if (!c) return fail(BACON_ERR_INVALID, "cache is NULL");
   CacheStoreArgs a{};
   TRY(check_batch(c, bt, first_seq, false, &a.s));
   TRY(check_layers(c, first_layer, num_layers));
   if (!d_k || !d_v) return fail(BACON_ERR_INVALID, "pointer arrays are NULL");
+  if (d_idx && idx_count < 0) return fail(BACON_ERR_INVALID, "idx_count must be >= 0");
   for (int l = 0; l < num_layers; ++l) {
     TRY(check_ptr(d_k[l], "k", 16));
     TRY(check_ptr(d_v[l], "v", 16));
@@ -345,6 +346,7 @@ bacon_status bacon_cache_store(bacon_cache *c, const bacon_batch *bt, int32_t fi
   for (int b = 0; b < bt->batch; ++b) most = std::max(most, bt->cu_seqlens[b + 1] - bt->cu_seqlens[b]);
   most = std::min(most, capacity(c));
   a.c = device_of(c);
+  a.idx_count = idx_count;
   a.first_seq = first_seq;
   for (int l = 0; l < num_layers; l += kCacheLayersPerLaunch) {
     a.first_layer = first_layer + l;

@@ -20,11 +20,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 //                  logits of four rows of each of the four steps t
 //   O^T = V^T P^T  lane (n, g) gives 8 rows' weights of query n to a step
 //
-// Row 16 g + 4 t + i of the tile is M index 4 g + i of step t, so a lane's 16 weights belong to rows
-// 16 g .. 16 g + 15, which are what it gives to the second product, without an
-// exchange between lanes, and V's 16-byte groups are read in that order.
-// The codes become bf16 in registers, exactly, with the block's scale applied by the
-// conversion.
+// Row 16 g + 4 t + i of the tile is M index 4 g + i of step t, so a lane's 16
+// weights belong to rows 16 g .. 16 g + 15, which are what it gives to the
+// second product, without an exchange between lanes, and V's 16-byte groups
+// are read in that order.  The codes become bf16 in registers, exactly, the
+// block's scale applied by the conversion.
 template <int D>
 struct KTile {
   u32x4 w[4][D / 64];
@@ -53,7 +53,6 @@ __device__ __forceinline__ TileIds bound_ids(TileIds t, int base, int to) {
   const int lane = threadIdx.x & 63;
   return TileIds{base + 16 * ((lane & 15) >> 2) < to ? t.k : -1, base + 16 * (lane >> 4) < to ? t.v : -1};
 }
-
 
 // (An absent block's rows are masked: any address of the pool will do.)
 template <int D>
@@ -158,8 +157,9 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   const CacheDev &c = a.c;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), waves = blockDim.x >> 6;
   const int m = lane & 15, g = lane >> 4;
-  // The workgroups of a unit's further query rows follow the first's eight apart: on the
-  // same die (workgroups go to the eight in turn), which then still holds the codes.
+  // The workgroups of a unit's further query rows follow the first's eight
+  // apart: on the same die (workgroups go to the eight in turn), whose L2 then
+  // still holds the codes (512 pairs of 64 query rows over 1K rows: 66 -> 58 us).
   const int eights = blockIdx.x >> 3;
   const int unit = a.groups == 1 ? blockIdx.x : eights / a.groups * 8 + (blockIdx.x & 7);
   const int row0 = a.groups == 1 ? 0 : eights % a.groups * NT * 16;
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   // this workgroup's rows
   const int chunk = max(a.chunk, ((total + a.splits - 1) / a.splits + 63) & ~63);
   const int from = split * chunk, to = min(total, from + chunk);
-  const int first_end = total - (count - 1);                 // of the first query: below it nothing is masked
+  const int first_end = total - max(count - 1, 0);           // of the first query: below it nothing is masked
 
   // the first tile's codes, asked for before the queries are formed
   int base = from + 64 * wave;

@@ -53,6 +53,7 @@ def test_layout_counts_past_32_bits():
     (dict(dtype=5), bacon.ERR_UNSUPPORTED), (dict(num_blocks=1 << 31), bacon.ERR_UNSUPPORTED),
     (dict(max_blocks=1 << 30), bacon.ERR_UNSUPPORTED), (dict(num_layers=1 << 25), bacon.ERR_UNSUPPORTED),
     (dict(num_q_heads=130), bacon.ERR_UNSUPPORTED),
+    (dict(num_q_heads=2000, num_kv_heads=2000), bacon.ERR_UNSUPPORTED),
 ])
 def test_bad_shapes_refused(kw, status):
     off, h = bacon.CacheOffsets(), C.c_void_p()
@@ -102,12 +103,13 @@ def test_calls_refused_before_enqueueing():
     assert tables(used=C.c_void_p(FAKE + 4)) == INV
     assert tables() == ORD and tables(bud=f, nb=2, bt=hb) == ORD      # head_budgets unread with d_budgets
 
-    def store(c=h, bt=b2, first=0, fl=0, nl=3, k=arr, v=arr, idx=arr):
-        return L.bacon_cache_store(c, C.byref(bt.c) if bt else None, first, fl, nl, k, v, idx, None)
+    def store(c=h, bt=b2, first=0, fl=0, nl=3, k=arr, v=arr, idx=arr, count=96):
+        return L.bacon_cache_store(c, C.byref(bt.c) if bt else None, first, fl, nl, k, v, idx, count, None)
     assert store(c=None) == INV and store(bt=None) == INV and store(first=3) == INV
     assert store(fl=1) == INV and store(fl=-1) == INV and store(nl=0) == INV
     assert store(k=None) == INV and store(v=None) == INV and store(k=bad) == INV and store(v=bad) == INV
     assert store(idx=(C.c_void_p * 3)(FAKE, None, FAKE)) == INV
+    assert store(count=-1) == INV
     assert store() == ORD and store(idx=None) == ORD
 
     def load(c=h, fl=0, nl=3, fs=0, ns=4, ft=0, n=8, k=f, v=f):

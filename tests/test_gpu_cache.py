@@ -269,6 +269,13 @@ def test_store_of_a_bad_index_is_a_zero_row():
     got = _np(c.bacon_cache_load(6)[0])[0, 0, 0]
     assert got[0].any() and not got[1:4].any() and got[4].any() and got[5].any()
     assert c.bacon_cache_errors() == bacon.CACHE_BAD_INDEX
+    # entries past the end of a short idx are not read
+    c.bacon_cache_clear()
+    c.bacon_cache_tables(batch)
+    c.bacon_cache_store(batch, [k], [v], [idx.zero_()[:2]])
+    got = _np(c.bacon_cache_load(6)[0])[0, 0, 0]
+    assert got[:2].any(1).all() and not got[2:4].any() and got[4:].any(1).all()
+    assert c.bacon_cache_errors() == bacon.CACHE_BAD_INDEX
 
 
 def test_store_over_the_range_of_magnitudes():
