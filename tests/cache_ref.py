@@ -39,11 +39,11 @@ class Rows:
         self.bt, self.x, self.e = bt, np.zeros((0, d)), []
 
     def store(self, x):
-        self.x, self.e = np.zeros((0, x.shape[1])), []
+        self.x, self.e = np.zeros(x.shape), []
         for i in range(0, len(x), self.bt):
             part = x[i:i + self.bt].astype(np.float64)
             self.e.append(exponent(np.abs(part).max()))
-            self.x = np.concatenate([self.x, round8(part, self.e[-1])])
+            self.x[i:i + self.bt] = round8(part, self.e[-1])
 
     def append(self, new):
         new = new.astype(np.float64)

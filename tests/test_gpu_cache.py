@@ -278,6 +278,13 @@ def test_store_of_a_bad_index_is_a_zero_row():
     assert c.bacon_cache_errors() == bacon.CACHE_BAD_INDEX
 
 
+def test_store_of_many_layers():
+    """More layers than one launch takes, from lists of separate tensors."""
+    m = Model([[5, 20]], 2, 64, 16, "bf16", layers=67)
+    for l in (0, 1, 63, 64, 66):
+        m.check_values(l)
+
+
 def test_store_over_the_range_of_magnitudes():
     """Zero blocks, the least and the largest magnitudes, ties and subnormal codes."""
     import torch
@@ -406,6 +413,13 @@ def test_attend_long_and_ragged(dtype, d, G, n, most):
     m.check_attend(q, out, lse)
 
 
+def test_attend_over_the_longest():
+    """More rows than the longest prompt, of which the last queries see different numbers."""
+    m = Model([[131072 + 17]], 4, 64, 64, "bf16")
+    q = m.tokens(2, 4, 1.5)
+    m.check_attend(q, *m.c.bacon_cache_attend(0, q, want_lse=True))
+
+
 def test_attend_padded_and_empty():
     """Sequences without rows, padding queries, queries whose mask leaves nothing."""
     import torch
@@ -481,7 +495,8 @@ def test_attend_far_into_the_pool():
 # ------------------------------------------------------------------ step
 
 @pytest.mark.parametrize("dtype,d,bt,G,n", [("bf16", 128, 64, 4, 1), ("fp32", 64, 16, 1, 1), ("bf16", 64, 32, 7, 4),
-                                            ("bf16", 128, 16, 1, 30)])
+                                            ("bf16", 128, 16, 1, 30), ("fp32", 128, 64, 5, 6), ("fp32", 64, 16, 2, 16),
+                                            ("bf16", 128, 32, 8, 8), ("fp32", 64, 64, 1, 64)])
 def test_step_is_append_then_attend(dtype, d, bt, G, n):
     import torch
     lens = [[1, 16], [15, 700], [64, 63], [200, 33]]
@@ -628,6 +643,66 @@ def test_captured_step_replays(lens):
         assert torch.equal(gout, eager) and torch.equal(glse, elog), i
         x, y = a.c.bacon_cache_load(200), b.c.bacon_cache_load(200)
         assert torch.equal(a.c.lens, b.c.lens) and torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+
+
+def test_two_captured_graphs_replay_beside_each_other():
+    """Each captured attend owns its scratch: replays on two streams do not mix."""
+    import torch
+    m = Model([[3000, 2900]], 8, 128, 64, "bf16", layers=2)
+    qs = [m.tokens(1, 8), m.tokens(1, 8)]
+    want = [m.c.bacon_cache_attend(l, qs[l], want_lse=True) for l in range(2)]
+    graphs, got, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for l in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got.append(m.c.bacon_cache_attend(l, qs[l], want_lse=True))
+        graphs.append(g)
+    for _ in range(5):
+        torch.cuda.synchronize()
+        for l in range(2):
+            got[l][0].zero_()
+        torch.cuda.synchronize()
+        for l in range(2):
+            with torch.cuda.stream(streams[l]):
+                graphs[l].replay()
+        torch.cuda.synchronize()
+        for l in range(2):
+            assert torch.equal(got[l][0], want[l][0]) and torch.equal(got[l][1], want[l][1])
+
+
+def test_tables_and_store_in_a_captured_graph():
+    """A prompt that joins a batch, captured: every replay gives the same cache
+    as eager calls, with other work between the replays."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(21)
+    d, W, bt, N, K = 64, 4, 16, [200, 90], [50, 60]
+    cu = np.concatenate([[0], np.cumsum(N)])
+    batch = bacon.BatchLayout(cu, K)
+    c = _cache(2, 4, 2, d, W, bt, 2, 100, 60, "bf16")
+    k, v = (_rand(rng, 2, int(cu[-1]), 2, d) for _ in range(2))
+    bud = torch.from_numpy(rng.integers(1, 60, (2, 2, 2)).astype(np.int32)).cuda()
+    used = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def fill():
+        c.bacon_cache_clear()
+        c.bacon_cache_tables(batch, bud, 5, used=used)
+        c.bacon_cache_store(batch, k, v)
+        return c.bacon_cache_load(64)
+    fill()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        gk, gv = fill()
+    for i in range(4):
+        bud.copy_(torch.from_numpy(rng.integers(1, 60, (2, 2, 2)).astype(np.int32)))
+        k.copy_(_rand(rng, 2, int(cu[-1]), 2, d))
+        g.replay()
+        torch.cuda.synchronize()
+        table, lens, n = c.table.clone(), c.lens.clone(), int(used)
+        a, b = gk.clone(), gv.clone()
+        ek, ev = fill()
+        assert torch.equal(table, c.table) and torch.equal(lens, c.lens) and n == int(used)
+        assert torch.equal(a, ek) and torch.equal(b, ev), i
 
 
 def test_rows_that_are_not_named_stay():
