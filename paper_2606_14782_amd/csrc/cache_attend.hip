@@ -504,10 +504,12 @@ void allow_lds() {
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const int pairs = a.num_seqs * a.c.Hkv, R = a.c.Hq / a.c.Hkv * a.tokens, units = pairs * a.splits;
-  // Eight waves shorten a workgroup where workgroups are few (one sequence over 288 rows: 6.9
-  // us, with four waves 7.5) and where it holds 32 queries; elsewhere four start and join
-  // sooner (64 sequences over 300 to 993 rows: 18 us, with eight 23; 32 over 32K rows: 352 both ways).
-  const bool eight = max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (NT == 2 || units < 256);
+  // Eight waves shorten a workgroup where workgroups are few (one sequence over
+  // 288 rows: 6.9 us, with four waves 7.5), and where one holds all of 17 to 32
+  // query rows (a step of 64 sequences of four drafted tokens 19.5 and 20.6);
+  // elsewhere four start and join sooner (64 over 300 to 993 rows: 18 us, with
+  // eight 23).
+  const bool eight = max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (units < 256 || (NT == 2 && a.groups == 1));
   const int waves = eight ? 8 : 4;
   allow_lds<BF16, D, NT>();
   hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(a.groups == 1 ? units : (units + 7) / 8 * 8 * a.groups), dim3(64 * waves),
@@ -540,12 +542,16 @@ bool cache_appends(int q_rows) { return q_rows <= 32; }
 hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStream_t s) {
   const int G = a.c.Hq / a.c.Hkv, R = G * a.tokens;
   a.group_magic = (65536 + G - 1) / G;
-  // 16 query rows a workgroup: of 28 (28/4 heads, four tokens) over one
-  // sequence's 64 rows 5.6 us against 7.4 with 32, of five fp32 tokens of four
-  // sequences 13.9 against 17.6, and no loss where workgroups are many (512 pairs of 64 query rows
-  // over 1K rows: 58 us both ways).  A step of 17 to 32 query rows keeps
-  // them in one workgroup, which appends: two would not see each other's rows.
-  const bool one = !a.k || R <= 16;
+  // 16 query rows a workgroup or 32: 32 share the codes' conversion, 16 are
+  // sooner done with a tile.  bf16, us with 16 and with 32: three sequences up
+  // to 70K rows (28/4 heads, five tokens) 68 and 56, four over 4K (64/8, eight
+  // tokens) 27 and 23, eight over 16K (32 query rows) 58 and 52; but 64 over 300 to 993 rows
+  // (28) 16.6 and 17.7, one over 64 rows 5.6 and 7.4.  fp32, whose parts fill the
+  // registers: five tokens of four sequences 13.5 and 15.2.  A step of 17 to 32
+  // query rows keeps them in the one workgroup that appends: two would not see
+  // each other's rows.
+  const bool shared = bf16 && a.chunk > 256 && (R > 32 || a.chunk > 1024);
+  const bool one = R <= 16 || !(a.k || shared);
   a.groups = (R + (one ? 15 : 31)) / (one ? 16 : 32);
 #define ATTEND(nt)                                                                                \
   return bf16 ? (head_dim == 128 ? attend<true, 128, nt>(a, s) : attend<true, 64, nt>(a, s))      \
