@@ -413,6 +413,16 @@ def test_attend_long_and_ragged(dtype, d, G, n, most):
     m.check_attend(q, out, lse)
 
 
+@pytest.mark.parametrize("dtype,d,G,n", [("bf16", 64, 7, 3), ("bf16", 128, 8, 6), ("fp32", 64, 7, 3), ("bf16", 64, 4, 1)])
+def test_attend_many_pairs(dtype, d, G, n):
+    """128 pairs, a few of them long: long parts, in which more query rows share a workgroup."""
+    lens = np.random.default_rng(5).integers(1, 40, (4, 32))
+    lens[1, 3], lens[3, 31], lens[0, 0] = 2300, 1100, 513
+    m = Model(lens, 32 * G, d, 32, dtype)
+    q = m.tokens(n, 32 * G, 1.5)
+    m.check_attend(q, *m.c.bacon_cache_attend(0, q, want_lse=True))
+
+
 def test_attend_over_the_longest():
     """More rows than the longest prompt, of which the last queries see different numbers."""
     m = Model([[131072 + 17]], 4, 64, 64, "bf16")
