@@ -90,16 +90,22 @@ __device__ __forceinline__ bf16x8 dequant(unsigned lo, unsigned hi, float scale)
   return r;
 }
 
-// Eight floats as NP bf16 parts whose sum they are, to 8 bits more a part.
+// Eight floats as NP bf16 parts whose sum they are, to 8 bits more a part: all
+// but the last are cut off (a mask, and the rest is exact), the last is rounded.
 template <int NP>
 __device__ __forceinline__ void split8(float (&x)[8], bf16x8 (&part)[NP]) {
 #pragma unroll
-  for (int p = 0; p < NP; ++p)
+  for (int p = 0; p + 1 < NP; ++p) {
+    u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      part[p][i] = (__bf16)x[i];
-      if (p + 1 < NP) x[i] -= (float)part[p][i];
-    }
+    for (int i = 0; i < 4; ++i)
+      w[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302);
+    part[p] = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] -= __uint_as_float(__float_as_uint(x[i]) & 0xFFFF0000u);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) part[NP - 1][i] = (__bf16)x[i];
 }
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
