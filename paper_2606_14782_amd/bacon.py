@@ -461,6 +461,8 @@ class Cache:
         self._raw_stream, self._current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         self._hq, self._hkv, self._d, self._work = num_q_heads, num_kv_heads, head_dim, {}
         dev = torch.device(device)
+        if dev.type != "cuda":
+            raise BaconError(ERR_INVALID, f"a cache lives on a GPU, not on {dev}")
         self.device = dev if dev.index is not None else torch.device(dev.type, torch.cuda.current_device())
         self.torch_dtype = torch.bfloat16 if self.shape.dtype == BF16 else torch.float32
         self.memory = torch.empty(off.total + 256, dtype=torch.uint8, device=self.device)
@@ -673,4 +675,5 @@ class Cache:
 
     def bacon_cache_errors(self) -> int:
         """The error word (CACHE_* bits); waits for the device."""
-        return int(self._L.bacon_cache_errors(self._h))
+        with self._torch.cuda.device(self.device):
+            return int(self._L.bacon_cache_errors(self._h))

@@ -36,13 +36,14 @@ __global__ __launch_bounds__(256) void k_cache_clear(CacheDev c, int first_seq, 
 constexpr int kTabPairs = 64;          // most pairs of a workgroup
 constexpr int kTabThreads = 1024;
 
-// i / d for i < 2^16 and d <= 2^10, or any i * d < 2^32, with magic = 2^32 / d rounded up.
+// i / d for i d < 2^32 and d > 1, with magic = 2^32 / d rounded up.
 __device__ __forceinline__ unsigned quotient(unsigned i, unsigned magic) { return __umulhi(i, magic); }
 
 // Steps of kTabThreads through rows of `len` entries, without a division a step.
 struct Walk {
   int row, at, len, rows, rest;
-  __device__ __forceinline__ Walk(int t, int n) : row(t / n), at(t % n), len(n), rows(kTabThreads / n), rest(kTabThreads % n) {}
+  __device__ __forceinline__ Walk(int t, int n)
+      : row(t / n), at(t % n), len(n), rows(kTabThreads / n), rest(kTabThreads % n) {}
   __device__ __forceinline__ void next() {
     row += rows;
     at += rest;
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(256) void k_cache_load(CacheLoadArgs a, unsigned pe
       v0 = *reinterpret_cast<const u32x4 *>(v);
       v1 = *reinterpret_cast<const u32x4 *>(v + 16);
       scale = *reinterpret_cast<const float2 *>(c.scales + (int64_t)id * 2);
-    } else if (lane == 0) {
+    } else if (col == 0 && q == 0) {
       atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
     }
   }
@@ -467,7 +468,9 @@ __global__ __launch_bounds__(256) void k_cache_advance(CacheMoveArgs a) {
   c.lens[pair] = (int)(n < 0 ? 0 : n > cap ? cap : n);
 }
 
-int blocks_for(int64_t n, int per, int most) { return (int)std::max<int64_t>(1, std::min<int64_t>(most, (n + per - 1) / per)); }
+int blocks_for(int64_t n, int per, int most) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, (n + per - 1) / per));
+}
 
 // The instance for a dtype and head size.
 #define CACHE_LAUNCH(kernel, grid, threads, s, ...)                                        \

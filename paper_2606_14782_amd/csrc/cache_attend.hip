@@ -135,7 +135,9 @@ template <int D>
 constexpr int o_pitch() { return D + 4; }
 
 // Token of query row r < 64 of a pair (r / G).
-__device__ __forceinline__ int token_of(const CacheStepArgs &a, int r) { return (int)((unsigned)r * a.group_magic >> 16); }
+__device__ __forceinline__ int token_of(const CacheStepArgs &a, int r) {
+  return (int)((unsigned)r * a.group_magic >> 16);
+}
 
 // Four dimensions of a query's output from their weighted sums, and its normaliser.
 template <bool BF16, int D>
@@ -241,9 +243,9 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     const int j = token_of(a, r);
 #pragma unroll
     for (int e = 0; e < 8; ++e) qx[u][e] = 0.f;
+    const int dim = 64 * (s >> 1) + 16 * g + 8 * (s & 1);
     if (i < NT * KS && r < R)
-      load8<BF16>(a.q, ((int64_t)b * a.tokens + j) * a.q_stride + (h * G + r - j * G) * D + 64 * (s >> 1) + 16 * g + 8 * (s & 1),
-                  qx[u]);
+      load8<BF16>(a.q, ((int64_t)b * a.tokens + j) * a.q_stride + (h * G + r - j * G) * D + dim, qx[u]);
   }
 #pragma unroll
   for (int u = 0; u < QI; ++u) {
@@ -518,8 +520,9 @@ hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const bool eight = max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (units < 256 || (NT == 2 && a.groups == 1));
   const int waves = eight ? 8 : 4;
   allow_lds<BF16, D, NT>();
-  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(a.groups == 1 ? units : (units + 7) / 8 * 8 * a.groups), dim3(64 * waves),
-                     (attend_lds<BF16, D, NT>(waves)), s, a);
+  const int grid = a.groups == 1 ? units : (units + 7) / 8 * 8 * a.groups;
+  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(grid), dim3(64 * waves), (attend_lds<BF16, D, NT>(waves)), s,
+                     a);
   if (a.splits > 1) hipLaunchKernelGGL((k_cache_join<BF16, D>), dim3(pairs * R), dim3(256), 0, s, a);
   return hipGetLastError();
 }

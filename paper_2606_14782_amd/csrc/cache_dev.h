@@ -15,7 +15,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kTop = 448.f;          // largest e4m3 value
 constexpr float kLn2f = 0.69314718055994531f;
 
 __device__ __forceinline__ float bf16_float(unsigned bits) { return __uint_as_float(bits << 16); }
@@ -87,32 +86,6 @@ __device__ __forceinline__ float wave_max(float v) {
   for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
   return v;
 }
-__device__ __forceinline__ float wave_add(float v) {
-  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-  return v;
-}
-
-// The largest v of a 256-thread workgroup; red holds 4 floats, free again
-// after the next barrier.
-__device__ __forceinline__ float block_max(float v, float *red) {
-  v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-}
-
-template <bool BF16>
-__device__ __forceinline__ float load_elem(const void *p, int64_t i) {
-  if constexpr (BF16) return bf16_float(static_cast<const uint16_t *>(p)[i]);
-  return static_cast<const float *>(p)[i];
-}
-template <bool BF16>
-__device__ __forceinline__ void store_elem(void *p, int64_t i, float x) {
-  if constexpr (BF16)
-    static_cast<uint16_t *>(p)[i] = (uint16_t)float_bf16(x);
-  else
-    static_cast<float *>(p)[i] = x;
-}
 
 // Eight consecutive elements as floats (i a multiple of 8).
 template <bool BF16>
@@ -150,9 +123,11 @@ __device__ __forceinline__ NewRows new_rows(const CacheStepArgs &a, int64_t pair
 }
 
 // One wave puts the new rows of the pair's block i in place: 8 elements a
-// lane, D / 8 lanes a row.  The scale is the larger of the one that the block's old
-// rows have and the one that the new rows need; old codes are rounded again
-// where it grew (in whole words, before the new codes are written).
+// lane, D / 8 lanes a row.  The scale is the larger of the one that the block's
+// old rows have and the one that the new rows need; old codes are rounded again
+// where it grew (in whole words, before the new codes are written).  A chain
+// of reads bounds it (id, scale and new rows, store): in a step over 288 rows it
+// costs 1.0 us of 8.2.
 template <bool BF16, int D>
 __device__ void append_block(const CacheStepArgs &a, int64_t pair, const NewRows &n, int i) {
   constexpr int TR = D / 8, RP = 64 / TR;

@@ -165,6 +165,18 @@ def test_work_is_asked_for_and_checked():
     L.bacon_cache_free(h)
 
 
+def test_binding_refuses_other_devices_and_dtypes():
+    for kw, status in ((dict(device="cpu"), bacon.ERR_INVALID), (dict(dtype="fp16"), bacon.ERR_UNSUPPORTED),
+                       (dict(block_tokens=0), bacon.ERR_INVALID), (dict(block_tokens=24), bacon.ERR_UNSUPPORTED),
+                       (dict(max_tokens=0), bacon.ERR_INVALID)):
+        a = dict(num_layers=1, num_q_heads=4, num_kv_heads=2, head_dim=64, window=8, block_tokens=16, max_batch=2,
+                 max_tokens=100, num_blocks=10, dtype="bf16", device="cpu")
+        a.update(kw)
+        with pytest.raises(bacon.BaconError) as e:
+            bacon.Cache(**a)
+        assert e.value.status == status, kw
+
+
 def test_reference_rounding():
     """The test's own rounding: values, ties to even, the exponents' borders."""
     assert R.E4M3[-1] == 448.0 and len(R.E4M3) == 127

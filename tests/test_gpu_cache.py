@@ -464,6 +464,11 @@ def test_attend_over_absent_blocks():
     m = Model([[100, 40]], 2, 64, 16, "bf16")
     m.c.table[0, 0, 0, 2] = -1
     m.c.table[0, 0, 0, 4] = 1 << 30
+    k, v = m.c.bacon_cache_load(100)
+    assert m.c.bacon_cache_errors() == bacon.CACHE_BAD_BLOCK
+    for t in (k, v):
+        rows = t[0, 0, 0].any(-1)
+        assert not rows[32:48].any() and not rows[64:80].any() and int(rows.sum()) == 68
     q = m.tokens(1, 2)
     out, lse = m.c.bacon_cache_attend(0, q, want_lse=True)
     assert m.c.bacon_cache_errors() == bacon.CACHE_BAD_BLOCK
