@@ -42,7 +42,8 @@ struct CacheTablesArgs {
   const int32_t *free_ids; // optional [num_free]
   int64_t num_free;
   int64_t *used;           // optional
-  unsigned head_magic;     // 2^32 / Hkv, rounded up
+  unsigned head_magic;     // 2^32 / Hkv, rounded up (set by the launch)
+  int row_threads;         // threads of a table row, 64 to 1024 (set by the launch)
 };
 
 struct CacheStoreArgs {

@@ -143,31 +143,31 @@ __global__ __launch_bounds__(kTabThreads) void k_cache_tables(CacheTablesArgs a,
     }
   }
   __syncthreads();
-  // the table rows, four entries of a thread on their way at a time
-  const int entries = mine * c.max_blocks;
-  Walk e(t, c.max_blocks);
-  for (int n = t; n < entries; n += kTabThreads * 4) {
-    int id[4];
-    int64_t at[4];
+  // the table rows: whole waves to a pair, four entries of a thread on their way at a time
+  const int wide = a.row_threads;
+  for (int q = t / wide; q < mine; q += kTabThreads / wide) {
+    const int need = __builtin_amdgcn_readfirstlane(s_need[q]);
+    const int64_t first = s_first[q];
+    const int32_t *ids = a.free_ids ? a.free_ids + first : nullptr;
+    int32_t *row = c.table + s_row[q];
+    for (int i0 = t & (wide - 1); i0 < c.max_blocks; i0 += 4 * wide) {
+      int id[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i, e.next()) {
-      id[i] = -1;
-      at[i] = -1;
-      if (n + kTabThreads * i >= entries) continue;
-      at[i] = s_row[e.row] + e.at;
-      if (e.at < s_need[e.row]) {
-        const int64_t first = s_first[e.row] + e.at;
-        id[i] = a.free_ids ? a.free_ids[first] : (int)first;
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * wide;
+        id[u] = -1;
+        if (i < need) id[u] = ids ? ids[i] : (int)(first + i);
       }
-    }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (at[i] < 0) continue;
-      if (id[i] != -1 && (unsigned)id[i] >= (unsigned)c.num_blocks) {
-        atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
-        id[i] = -1;
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * wide;
+        if (i >= c.max_blocks) break;
+        if (i < need && (unsigned)id[u] >= (unsigned)c.num_blocks) {
+          atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
+          id[u] = -1;
+        }
+        row[i] = id[u];
       }
-      c.table[at[i]] = id[i];
     }
   }
 }
@@ -496,6 +496,8 @@ hipError_t launch_cache_clear(const CacheDev &c, int first_seq, int num_seqs, bo
 hipError_t launch_cache_tables(CacheTablesArgs a, hipStream_t s) {
   const int pairs = a.c.L * a.s.batch * a.c.Hkv;
   const int own = std::max(1, std::min(kTabPairs, pairs / 256));
+  a.row_threads = 64;
+  while (a.row_threads < kTabThreads && a.row_threads * own < kTabThreads) a.row_threads *= 2;
   a.head_magic = (unsigned)((0x100000000ull + a.c.Hkv - 1) / a.c.Hkv);
   hipLaunchKernelGGL(k_cache_tables, dim3((unsigned)((pairs + own - 1) / own)), dim3(kTabThreads), 0, s, a, own);
   return hipGetLastError();
