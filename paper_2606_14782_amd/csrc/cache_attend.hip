@@ -417,10 +417,10 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
       }
     }
   };
-  if (waves == 8)
-    join(std::integral_constant<int, 8>{});
-  else
+  if (waves == 4)
     join(std::integral_constant<int, 4>{});
+  else
+    join(std::integral_constant<int, 8>{});
 }
 
 // Joins the parts of one query row: D / 4 threads a part, each group of them
@@ -512,13 +512,12 @@ void allow_lds() {
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const int pairs = a.num_seqs * a.c.Hkv, R = a.c.Hq / a.c.Hkv * a.tokens, units = pairs * a.splits;
-  // Eight waves shorten a workgroup where workgroups are few (one sequence over
-  // 288 rows: 6.9 us, with four waves 7.5), and where one holds all of 17 to 32
-  // query rows (a step of 64 sequences of four drafted tokens 19.5 and 20.6);
-  // elsewhere four start and join sooner (64 over 300 to 993 rows: 18 us, with
-  // eight 23).
-  const bool eight = max_waves(BF16, D, NT) == 8 && a.chunk > 256 && (units < 256 || (NT == 2 && a.groups == 1));
-  const int waves = eight ? 8 : 4;
+  // Four waves, also where some have no tile (they share the queries and the
+  // join: one sequence over 1K rows in parts of 64 takes 7.8 us, 8.0 with a wave
+  // each); eight where one holds all of 17 to 32 query rows (a step of 64
+  // sequences of four drafted tokens 19.5 us, with four 20.6).  Elsewhere eight are slower (64
+  // sequences over 300 to 993 rows 23 us, with four 18).
+  const int waves = NT == 2 && a.groups == 1 && a.chunk > 256 && max_waves(BF16, D, NT) == 8 ? 8 : 4;
   allow_lds<BF16, D, NT>();
   const int grid = a.groups == 1 ? units : (units + 7) / 8 * 8 * a.groups;
   hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(grid), dim3(64 * waves), (attend_lds<BF16, D, NT>(waves)), s,
@@ -531,11 +530,15 @@ hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
 
 CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens) {
   CachePlan p{};
-  // A workgroup a compute unit, each of at least 256 rows, a tile a wave: one
-  // sequence over 32K rows (8 pairs) takes 17 us divided into 256, 19 into 128 and 18 into 512;
-  // over 1K rows 8.7 us in parts of 256 and 10 in parts of 512 or whole.
+  // About 256 workgroups, one a compute unit: one sequence over 32K rows (8
+  // pairs) takes 17 us divided into 256, 19 into 128 and 18 into 512.  A pair of
+  // up to 768 rows stays whole (over 512 rows 6.9 us, in parts 7.5); longer ones
+  // may go down to a tile a part (over 1K rows 7.5 us, in parts of 256 8.5,
+  // whole 9.1), with more than 16 query rows, whose workgroups are more
+  // already, to 256 rows (three over 2K rows, 56 query rows: 13.6 us, in parts
+  // of 128 18.6).
   const int64_t want = (256 + pairs - 1) / pairs;
-  const int64_t by_rows = std::max<int64_t>(1, max_tokens / 256);
+  const int64_t by_rows = max_tokens <= 768 ? 1 : max_tokens / (q_rows > 16 ? 256 : 64);
   p.splits = (int)std::min(want, by_rows);
   p.chunk = (int)((((int64_t)max_tokens + p.splits - 1) / p.splits + 63) / 64 * 64);
   if (p.splits > 1) {

@@ -404,7 +404,8 @@ def test_attend(dtype, d, bt, G, n):
 
 
 @pytest.mark.parametrize("dtype,d,G,n,most", [("bf16", 128, 4, 1, None), ("bf16", 128, 4, 1, 6000),
-                                              ("bf16", 64, 7, 3, 100), ("fp32", 128, 2, 2, 6000)])
+                                              ("bf16", 64, 7, 3, 100), ("fp32", 128, 2, 2, 6000),
+                                              ("bf16", 128, 16, 4, None), ("fp32", 64, 16, 3, None)])
 def test_attend_long_and_ragged(dtype, d, G, n, most):
     """Few long pairs (work divided along them) beside short ones, whatever length was expected."""
     m = Model([[5003, 7], [1, 2500]], 2 * G, d, 64, dtype)
