@@ -677,3 +677,39 @@ class Cache:
         """The error word (CACHE_* bits); waits for the device."""
         with self._torch.cuda.device(self.device):
             return int(self._L.bacon_cache_errors(self._h))
+
+
+def bacon_cache_clear(cache: Cache, first_seq=0, num_seqs=None):
+    return cache.bacon_cache_clear(first_seq, num_seqs)
+
+
+def bacon_cache_tables(cache: Cache, batch, budgets=None, reserve=0, free=None, first_seq=0, used=None):
+    return cache.bacon_cache_tables(batch, budgets, reserve, free, first_seq, used)
+
+
+def bacon_cache_store(cache: Cache, batch, ks, vs, idxs=None, first_seq=0, first_layer=0):
+    return cache.bacon_cache_store(batch, ks, vs, idxs, first_seq, first_layer)
+
+
+def bacon_cache_load(cache: Cache, count, first_token=0, first_layer=0, num_layers=None, first_seq=0, num_seqs=None,
+                     out=None):
+    return cache.bacon_cache_load(count, first_token, first_layer, num_layers, first_seq, num_seqs, out)
+
+
+def bacon_cache_append(cache: Cache, layer, k, v, counts=None, first_seq=0):
+    return cache.bacon_cache_append(layer, k, v, counts, first_seq)
+
+
+def bacon_cache_attend(cache: Cache, layer, q, counts=None, max_tokens=None, first_seq=0, out=None, lse=None,
+                       want_lse=False, work=None):
+    return cache.bacon_cache_attend(layer, q, counts, max_tokens, first_seq, out, lse, want_lse, work)
+
+
+def bacon_cache_step(cache: Cache, layer, q, k, v, counts=None, max_tokens=None, first_seq=0, out=None, lse=None,
+                     want_lse=False, work=None):
+    return cache.bacon_cache_step(layer, q, k, v, counts, max_tokens, first_seq, out, lse, want_lse, work)
+
+
+def bacon_cache_advance(cache: Cache, delta=0, counts=None, first_layer=0, num_layers=None, first_seq=0,
+                        num_seqs=None):
+    return cache.bacon_cache_advance(delta, counts, first_layer, num_layers, first_seq, num_seqs)

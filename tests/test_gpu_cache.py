@@ -741,6 +741,67 @@ def test_rows_that_are_not_named_stay():
     assert changed[1, 1].all() and int(changed.sum()) == 2 and torch.equal(m.c.table, before_table)
 
 
+def test_outputs_and_scratch_keep_to_their_buffers():
+    """Guards before and after every buffer of a call, odd sizes; and the same
+    bits from a second run."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    m = Model([[1500, 3], [70, 900]], 14, 64, 32, "bf16")
+    n, G = 3, 7
+
+    def guarded(numel, dtype):
+        t = torch.full((numel + 256,), 7, dtype=dtype, device="cuda")
+        return t, t[128:128 + numel]
+
+    def untouched(t, numel):
+        return bool((t[:128] == 7).all()) and bool((t[128 + numel:] == 7).all())
+    q = m.tokens(n, 14)
+    need = bacon.lib().bacon_cache_work_bytes(m.c._h, 2, n, 1600)
+    assert need > 0
+    sizes = (2 * n * 14 * 64, 2 * n * 14, need)
+    bufs = [guarded(x, d) for x, d in zip(sizes, (torch.bfloat16, torch.float32, torch.uint8))]
+    work = torch.full((need + 1024,), 7, dtype=torch.uint8, device="cuda")
+    skip = -work.data_ptr() % 256 + 256
+    got = []
+    for _ in range(2):
+        out, lse = bufs[0][1].view(2, n, 14, 64), bufs[1][1].view(2, n, 14)
+        m.c.bacon_cache_attend(0, q, max_tokens=1600, out=out, lse=lse, work=work[skip:skip + need])
+        got.append((out.clone(), lse.clone()))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    m.check_attend(q, out, lse)
+    assert untouched(bufs[0][0], sizes[0]) and untouched(bufs[1][0], sizes[1])
+    assert bool((work[:skip] == 7).all()) and bool((work[skip + need:] == 7).all())
+    for count, first in ((33, 0), (1501, 0), (17, -17), (5, -1502)):
+        size = 2 * 2 * count * 64
+        k, v = guarded(size, torch.bfloat16), guarded(size, torch.bfloat16)
+        shape = (1, 2, 2, count, 64)
+        m.c.bacon_cache_load(count, first_token=first, out=(k[1].view(shape), v[1].view(shape)))
+        assert untouched(k[0], size) and untouched(v[0], size)
+    # blocks that no table names are as they were
+    used = torch.zeros(m.c.codes.shape[0], dtype=torch.bool, device="cuda")
+    used[m.c.table[m.c.table >= 0].long()] = True
+    assert bool((m.c.codes[~used] == 0x7F).all()) and bool(m.c.scales[~used].isnan().all())
+
+
+def test_functions_of_the_module_are_the_methods():
+    import torch
+    from paper_2606_14782_amd import bacon
+    m = Model([[20, 21]], 4, 64, 16, "bf16")
+    q, k, v = m.tokens(1, 4), m.tokens(1, 2), m.tokens(1, 2)
+    bacon.bacon_cache_append(m.c, 0, k, v)
+    m.append(k, v)
+    m.check_attend(q, *bacon.bacon_cache_attend(m.c, 0, q, want_lse=True))
+    bacon.bacon_cache_step(m.c, 0, q, k, v)
+    bacon.bacon_cache_advance(m.c, -1)
+    a, b = bacon.bacon_cache_load(m.c, 22), m.c.bacon_cache_load(22)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    bacon.bacon_cache_clear(m.c)
+    assert int(bacon.bacon_cache_tables(m.c, m.batch)) > 0
+    x = torch.zeros(1, m.batch.total, 2, 64, dtype=torch.bfloat16, device="cuda")
+    bacon.bacon_cache_store(m.c, m.batch, x, x)
+    assert not bacon.bacon_cache_load(m.c, 5)[0].any()
+
+
 # -------------------------------------------------------------- together
 
 @pytest.mark.parametrize("adaptive", [False, True])
