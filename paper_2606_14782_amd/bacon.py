@@ -560,34 +560,31 @@ class Cache:
                    self._whole(used, "used", self._torch.int64, (1,)))
         return used
 
-    def _layers(self, xs, name, dtype, shape):
-        """Host array of per-layer pointers: a list of tensors, or one with the layers first."""
-        n = len(xs)
+    def _layers(self, xs, name, dtype, shape=None):
+        """Number of layers, host array of their pointers and a layer's elements:
+        a list of tensors, or one with the layers first."""
         if isinstance(xs, self._torch.Tensor):
-            if shape is not None and xs.shape[1:] != shape:
+            base, n = self._whole(xs, name, dtype), xs.shape[0]
+            if n < 1 or shape is not None and xs.shape != (n, *shape):
                 raise BaconError(ERR_INVALID, f"{name} has shape {tuple(xs.shape)}")
-            base = self._whole(xs, name, dtype)
-            step = xs.stride(0) * xs.element_size()
-            return (C.c_uint64 * n)(*range(base, base + step * n, step)) if step else (C.c_uint64 * n)(base)
-        return (C.c_uint64 * n)(*[self._whole(x, name, dtype, shape) for x in xs])
+            size = xs.nbytes // n
+            if not size:
+                raise BaconError(ERR_INVALID, f"{name} is empty")
+            return n, (C.c_uint64 * n)(*range(base, base + n * size, size)), xs.numel() // n
+        n = len(xs)
+        ptrs = [self._whole(x, name, dtype, shape) for x in xs]
+        return n, (C.c_uint64 * n)(*ptrs), min((x.numel() for x in xs), default=0)
 
     def bacon_cache_store(self, batch: BatchLayout, ks, vs, idxs=None, first_seq=0, first_layer=0):
         """The kept rows of the layers first_layer, ..: ks, vs per-layer [T, Hkv,
         d] (lists, or stacked), idxs per-layer idx, or None (rows 0, 1, 2, ..)."""
-        s = self.shape
-        n = len(ks)
-        if len(vs) != n or idxs is not None and len(idxs) != n or n < 1:
-            raise BaconError(ERR_INVALID, f"{n} layers of K, {len(vs)} of V" +
-                             ("" if idxs is None else f", {len(idxs)} of idx"))
-        rows = (batch.total, s.num_kv_heads, s.head_dim)
-        idx, count = None, 0
-        if idxs is not None:
-            idx = self._layers(idxs, "idx", self._torch.int32, None)
-            count = (idxs.numel() // n if isinstance(idxs, self._torch.Tensor) else
-                     min(x.numel() for x in idxs))
-        self._call(self._L.bacon_cache_store, C.byref(batch.c), first_seq, first_layer, n,
-                   self._layers(ks, "k", self.torch_dtype, rows), self._layers(vs, "v", self.torch_dtype, rows), idx,
-                   count)
+        rows = (batch.total, self._hkv, self._d)
+        n, k, _ = self._layers(ks, "k", self.torch_dtype, rows)
+        nv, v, _ = self._layers(vs, "v", self.torch_dtype, rows)
+        ni, idx, count = (n, None, 0) if idxs is None else self._layers(idxs, "idx", self._torch.int32)
+        if nv != n or ni != n:
+            raise BaconError(ERR_INVALID, f"{n} layers of K, {nv} of V" + ("" if idxs is None else f", {ni} of idx"))
+        self._call(self._L.bacon_cache_store, C.byref(batch.c), first_seq, first_layer, n, k, v, idx, count)
 
     def bacon_cache_load(self, count, first_token=0, first_layer=0, num_layers=None, first_seq=0, num_seqs=None,
                          out=None):
@@ -600,7 +597,7 @@ class Cache:
         if out is None:
             if min(shape) < 1:
                 raise BaconError(ERR_INVALID, f"a load of shape {shape}")
-            both = self._torch.empty((2, *shape), dtype=self.torch_dtype, device=self.device)
+            both = self.scales.new_empty((2, *shape), dtype=self.torch_dtype)
             k, v = both.unbind(0)
             kp = both.data_ptr()
             vp = kp + both.nbytes // 2
@@ -616,18 +613,18 @@ class Cache:
         b, n, *rows = self._new_rows(k, v)
         self._call(self._L.bacon_cache_append, layer, first_seq, b, n, self._counts(counts, b), *rows)
 
-    def _attend_out(self, b, n, max_tokens, out, lse, want_lse, work):
+    def _attend_out(self, q, b, n, max_tokens, out, lse, want_lse, work):
         """Outputs and scratch of an attend, made where they are not given, and their pointers."""
         torch, shape = self._torch, (b, n, self._hq, self._d)
         if out is None:
-            out = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
+            out = q.new_empty(shape)
             outp = out.data_ptr()
         else:
             outp = self._whole(out, "out", self.torch_dtype, shape)
         if lse is not None:
             lsep = self._whole(lse, "lse", torch.float32, shape[:3])
         elif want_lse:
-            lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device)
+            lse = q.new_empty(shape[:3], dtype=torch.float32)
             lsep = lse.data_ptr()
         else:
             lsep = None
@@ -640,7 +637,7 @@ class Cache:
         if not need:
             return out, lse, outp, lsep, None, 0
         if work is None:
-            work = torch.empty(need, dtype=torch.uint8, device=self.device)
+            work = q.new_empty(need, dtype=torch.uint8)
         return out, lse, outp, lsep, self._whole(work, "work", torch.uint8), work.numel()
 
     def bacon_cache_attend(self, layer, q, counts=None, max_tokens=None, first_seq=0, out=None, lse=None,
@@ -650,7 +647,7 @@ class Cache:
         max_tokens: the longest length to expect (None: the table's)."""
         b, n, qp, qs = self._tokens(q, "q", self._hq)
         most = max_tokens or 0
-        out, lse, *ptrs = self._attend_out(b, n, most, out, lse, want_lse, work)
+        out, lse, *ptrs = self._attend_out(q, b, n, most, out, lse, want_lse, work)
         self._call(self._L.bacon_cache_attend, layer, first_seq, b, n, self._counts(counts, b), qp, qs, most, *ptrs)
         return out if lse is None else (out, lse)
 
@@ -662,7 +659,7 @@ class Cache:
         if bk != b or nk != n:
             raise BaconError(ERR_INVALID, f"q has {b} x {n} tokens, k {bk} x {nk}")
         most = max_tokens or 0
-        out, lse, *ptrs = self._attend_out(b, n, most, out, lse, want_lse, work)
+        out, lse, *ptrs = self._attend_out(q, b, n, most, out, lse, want_lse, work)
         self._call(self._L.bacon_cache_step, layer, first_seq, b, n, self._counts(counts, b), qp, qs, *rows, most,
                    *ptrs)
         return out if lse is None else (out, lse)
