@@ -75,8 +75,9 @@ struct CacheStepArgs {
   void *out;
   float *lse;              // optional
   float scale_log2;        // log2(e) / sqrt(d)
-  unsigned group_magic;    // 2^16 / G, rounded up (set by the launch)
-  int groups;              // of 32 query rows: 1 or 2 (set by the launch)
+  int G, R;                // query heads of a KV head, query rows of a pair (set by the launch, as the next two)
+  unsigned group_magic;    // 2^16 / G, rounded up
+  int groups;              // workgroups that a unit's query rows take
   // Division of a pair's rows: `splits` workgroups of `chunk` rows (more where
   // the pair is longer); with several, each leaves its part in work.
   int splits, chunk;

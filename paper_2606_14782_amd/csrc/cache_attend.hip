@@ -139,6 +139,36 @@ __device__ __forceinline__ int token_of(const CacheStepArgs &a, int r) {
   return (int)((unsigned)r * a.group_magic >> 16);
 }
 
+// Eight elements of a query as they lie in memory, and as floats.
+template <bool BF16>
+struct QRaw {
+  u32x4 w[BF16 ? 1 : 2];
+};
+
+template <bool BF16>
+__device__ __forceinline__ QRaw<BF16> load_raw(const void *p, int64_t i) {
+  const u32x4 *q = reinterpret_cast<const u32x4 *>(static_cast<const char *>(p) + i * (BF16 ? 2 : 4));
+  QRaw<BF16> r;
+  r.w[0] = q[0];
+  if constexpr (!BF16) r.w[1] = q[1];
+  return r;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void raw_floats(const QRaw<BF16> &r, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const unsigned w = r.w[0][j];
+    if constexpr (BF16) {
+      x[2 * j] = bf16_float(w & 0xFFFFu);
+      x[2 * j + 1] = __uint_as_float(w & 0xFFFF0000u);
+    } else {
+      x[j] = __uint_as_float(w);
+      x[4 + j] = __uint_as_float(r.w[1][j]);
+    }
+  }
+}
+
 // Four dimensions of a query's output from their weighted sums, and its normaliser.
 template <bool BF16, int D>
 __device__ __forceinline__ void store_out(const CacheStepArgs &a, int64_t at, int dim, f32x4 acc, float l, float top,
@@ -165,16 +195,33 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   const CacheDev &c = a.c;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), waves = blockDim.x >> 6;
   const int m = lane & 15, g = lane >> 4;
+  // One workgroup a unit (pair and part): a grid of parts, heads and sequences.
   // The workgroups of a unit's further query rows follow the first's eight
   // apart: on the same die (workgroups go to the eight in turn), whose L2 then
   // still holds the codes (512 pairs of 64 query rows over 1K rows: 66 -> 58 us).
-  const int eights = blockIdx.x >> 3;
-  const int unit = a.groups == 1 ? blockIdx.x : eights / a.groups * 8 + (blockIdx.x & 7);
-  const int row0 = a.groups == 1 ? 0 : eights % a.groups * NT * 16;
-  if (unit >= a.num_seqs * c.Hkv * a.splits) return;
-  const int split = unit % a.splits, bh = unit / a.splits;
-  const int b = bh / c.Hkv, h = bh - b * c.Hkv;
-  const int G = c.Hq / c.Hkv, R = G * a.tokens;
+  int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z, row0 = 0;
+  if (a.groups > 1) {
+    const int eights = blockIdx.x >> 3, unit = eights / a.groups * 8 + (blockIdx.x & 7);
+    if (unit >= a.num_seqs * c.Hkv * a.splits) return;
+    row0 = eights % a.groups * NT * 16;
+    split = unit % a.splits;
+    const int pair = unit / a.splits;
+    b = pair / c.Hkv;
+    h = pair - b * c.Hkv;
+  }
+  const int G = a.G, R = a.R, bh = b * c.Hkv + h;
+  // Queries: lane (n, g) holds 8 dimensions of query n for each step of 32.
+  // A wave's are asked for first of all, and formed while codes are on their way.
+  constexpr int QI = (NT * KS + 3) / 4;
+  QRaw<BF16> q_raw[QI];
+#pragma unroll
+  for (int u = 0; u < QI; ++u) {
+    const int i = wave + u * waves, nt = i / KS, s = i - nt * KS, r = row0 + nt * 16 + m;
+    const int j = token_of(a, r), dim = 64 * (s >> 1) + 16 * g + 8 * (s & 1);
+    q_raw[u] = QRaw<BF16>{};
+    if (i < NT * KS && r < R)
+      q_raw[u] = load_raw<BF16>(a.q, ((int64_t)b * a.tokens + j) * a.q_stride + (h * G + r - j * G) * D + dim);
+  }
   const int64_t pair = pair_of(c, a.layer, a.first_seq + b, h);
   const int32_t *row = c.table + pair * c.max_blocks;
   // The first two tiles' ids are asked for before the length is known (and
@@ -214,8 +261,29 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     load_k<D>(c, ids.k, base, kt);
     load_v<D>(c, ids.v, base, vt);
   }
+  // (taken to be waited for here: nothing in the loop then waits for them)
+  asm volatile("" : "+v"(id1.k), "+v"(id1.v));
+#pragma unroll
+  for (int u = 0; u < QI; ++u) {
+    const int i = wave + u * waves;
+    if (i >= NT * KS) continue;
+    float x[8];
+    raw_floats<BF16>(q_raw[u], x);
+    bf16x8 part[QP];
+    split8<QP>(x, part);
+#pragma unroll
+    for (int p = 0; p < QP; ++p) q_lds[(i * QP + p) * 64 + lane] = part[p];
+  }
+  int end[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = row0 + nt * 16 + m, j = token_of(a, r);
+    end[nt] = r < R && j < count ? max(0, total - (count - 1 - j)) : 0;
+  }
+  lds_barrier();
   // The new rows: the wave that owns a tile puts those of its blocks in place
-  // before it reads them (no block passes the border of a tile, so no other wave does).
+  // before it reads them (no block passes the border of a tile, so no other wave
+  // does).  After the barrier: the other waves go on.
   if (grow) {
     for (int i = fresh.b0; i <= fresh.b1; ++i) {
       const int at = (i << c.bt_log & ~63) - from;
@@ -229,40 +297,6 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     load_k<D>(c, ids.k, base, kt);
     load_v<D>(c, ids.v, base, vt);
   }
-
-  // (taken to be waited for here: nothing in the loop then waits for them)
-  asm volatile("" : "+v"(id1.k), "+v"(id1.v));
-
-  // queries: lane (n, g) holds 8 dimensions of query n for each step of 32,
-  // all of a wave's asked for at once
-  constexpr int QI = (NT * KS + 3) / 4;
-  float qx[QI][8];
-#pragma unroll
-  for (int u = 0; u < QI; ++u) {
-    const int i = wave + u * waves, nt = i / KS, s = i - nt * KS, r = row0 + nt * 16 + m;
-    const int j = token_of(a, r);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) qx[u][e] = 0.f;
-    const int dim = 64 * (s >> 1) + 16 * g + 8 * (s & 1);
-    if (i < NT * KS && r < R)
-      load8<BF16>(a.q, ((int64_t)b * a.tokens + j) * a.q_stride + (h * G + r - j * G) * D + dim, qx[u]);
-  }
-#pragma unroll
-  for (int u = 0; u < QI; ++u) {
-    const int i = wave + u * waves;
-    if (i >= NT * KS) continue;
-    bf16x8 part[QP];
-    split8<QP>(qx[u], part);
-#pragma unroll
-    for (int p = 0; p < QP; ++p) q_lds[(i * QP + p) * 64 + lane] = part[p];
-  }
-  int end[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = row0 + nt * 16 + m, j = token_of(a, r);
-    end[nt] = r < R && j < count ? max(0, total - (count - 1 - j)) : 0;
-  }
-  lds_barrier();
 
   f32x4 o[NT][D / 16];
   float mx[NT], sum[NT];
@@ -431,9 +465,8 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
   __shared__ f32x4 acc_lds[SP][TR];
   __shared__ float2 ml_lds[SP];
   const CacheDev &c = a.c;
-  const int t = threadIdx.x, G = c.Hq / c.Hkv, R = G * a.tokens, dim = t % TR, group = t / TR;
-  const int r = blockIdx.x % R, bh = blockIdx.x / R;
-  const int b = bh / c.Hkv, h = bh - b * c.Hkv, j = token_of(a, r);
+  const int t = threadIdx.x, G = a.G, R = a.R, dim = t % TR, group = t / TR;
+  const int r = blockIdx.x, h = blockIdx.y, b = blockIdx.z, bh = b * c.Hkv + h, j = token_of(a, r);
   const float2 *ml = a.part_ml + (int64_t)bh * a.splits * R + r;
   const f32x4 *o = reinterpret_cast<const f32x4 *>(a.part_o) + ((int64_t)bh * a.splits * R + r) * TR + dim;
   float top = kFloor, l = 0.f;
@@ -511,7 +544,7 @@ void allow_lds() {
 
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
-  const int pairs = a.num_seqs * a.c.Hkv, R = a.c.Hq / a.c.Hkv * a.tokens, units = pairs * a.splits;
+  const int units = a.num_seqs * a.c.Hkv * a.splits;
   // Four waves, also where some have no tile (they share the queries and the
   // join: one sequence over 1K rows in parts of 64 takes 7.8 us, 8.0 with a wave
   // each); eight where one holds all of 17 to 32 query rows (a step of 64
@@ -519,10 +552,10 @@ hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   // sequences over 300 to 993 rows 23 us, with four 18).
   const int waves = NT == 2 && a.groups == 1 && a.chunk > 256 && max_waves(BF16, D, NT) == 8 ? 8 : 4;
   allow_lds<BF16, D, NT>();
-  const int grid = a.groups == 1 ? units : (units + 7) / 8 * 8 * a.groups;
-  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), dim3(grid), dim3(64 * waves), (attend_lds<BF16, D, NT>(waves)), s,
+  const dim3 grid = a.groups == 1 ? dim3(a.splits, a.c.Hkv, a.num_seqs) : dim3((units + 7) / 8 * 8 * a.groups);
+  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), grid, dim3(64 * waves), (attend_lds<BF16, D, NT>(waves)), s,
                      a);
-  if (a.splits > 1) hipLaunchKernelGGL((k_cache_join<BF16, D>), dim3(pairs * R), dim3(256), 0, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((k_cache_join<BF16, D>), dim3(a.R, a.c.Hkv, a.num_seqs), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -553,6 +586,8 @@ bool cache_appends(int q_rows) { return q_rows <= 32; }
 
 hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStream_t s) {
   const int G = a.c.Hq / a.c.Hkv, R = G * a.tokens;
+  a.G = G;
+  a.R = R;
   a.group_magic = (65536 + G - 1) / G;
   // 16 query rows a workgroup or 32: 32 share the codes' conversion, 16 are
   // sooner done with a tile.  bf16, us with 16 and with 32: three sequences up
