@@ -198,7 +198,8 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   // One workgroup a unit (pair and part): a grid of parts, heads and sequences.
   // The workgroups of a unit's further query rows follow the first's eight
   // apart: on the same die (workgroups go to the eight in turn), whose L2 then
-  // still holds the codes (512 pairs of 64 query rows over 1K rows: 66 -> 58 us).
+  // still holds the codes (it took 512 pairs of 64 query rows over 1K rows from
+  // 66 us to 58; they take 42 now).
   int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z, row0 = 0;
   if (a.groups > 1) {
     const int eights = blockIdx.x >> 3, unit = eights / a.groups * 8 + (blockIdx.x & 7);
@@ -546,10 +547,10 @@ template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const int units = a.num_seqs * a.c.Hkv * a.splits;
   // Four waves, also where some have no tile (they share the queries and the
-  // join: one sequence over 1K rows in parts of 64 takes 7.8 us, 8.0 with a wave
-  // each); eight where one holds all of 17 to 32 query rows (a step of 64
-  // sequences of four drafted tokens 19.5 us, with four 20.6).  Elsewhere eight are slower (64
-  // sequences over 300 to 993 rows 23 us, with four 18).
+  // join: one sequence over 1K rows in parts of 64 takes 7.4 us with four and
+  // with one); eight where one holds all of 17 to 32 query rows (a step of 64
+  // sequences of four drafted tokens 18.5 us, with four 19.1).  Elsewhere eight
+  // are slower (64 sequences over 300 to 993 rows 22.6 us, with four 17.2).
   const int waves = NT == 2 && a.groups == 1 && a.chunk > 256 && max_waves(BF16, D, NT) == 8 ? 8 : 4;
   allow_lds<BF16, D, NT>();
   const dim3 grid = a.groups == 1 ? dim3(a.splits, a.c.Hkv, a.num_seqs) : dim3((units + 7) / 8 * 8 * a.groups);
@@ -565,11 +566,11 @@ CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens) {
   CachePlan p{};
   // About 256 workgroups, one a compute unit: one sequence over 32K rows (8
   // pairs) takes 17 us divided into 256, 19 into 128 and 18 into 512.  A pair of
-  // up to 768 rows stays whole (over 512 rows 6.9 us, in parts 7.5); longer ones
-  // may go down to a tile a part (over 1K rows 7.5 us, in parts of 256 8.5,
-  // whole 9.1), with more than 16 query rows, whose workgroups are more
-  // already, to 256 rows (three over 2K rows, 56 query rows: 13.6 us, in parts
-  // of 128 18.6).
+  // up to 768 rows stays whole (over 512 rows 6.7 us, in parts 7.2; over 768
+  // 7.7 and 7.3, but the second launch costs the host 3 more); longer ones may
+  // go down to a tile a part (over 1K rows 7.3 us, in parts of 256 8.1, whole
+  // 8.9), with more than 16 query rows, whose workgroups are more already, to
+  // 256 rows (three over 2K rows, 56 query rows: 18.0 us, in parts of 128 21.8).
   const int64_t want = (256 + pairs - 1) / pairs;
   const int64_t by_rows = max_tokens <= 768 ? 1 : max_tokens / (q_rows > 16 ? 256 : 64);
   p.splits = (int)std::min(want, by_rows);
@@ -591,12 +592,12 @@ hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStre
   a.group_magic = (65536 + G - 1) / G;
   // 16 query rows a workgroup or 32: 32 share the codes' conversion, 16 are
   // sooner done with a tile.  bf16, us with 16 and with 32: three sequences up
-  // to 70K rows (28/4 heads, five tokens) 68 and 56, four over 4K (64/8, eight
-  // tokens) 27 and 23, eight over 16K (32 query rows) 58 and 52; but 64 over 300 to 993 rows
-  // (28) 16.6 and 17.7, one over 64 rows 5.6 and 7.4.  fp32, whose parts fill the
-  // registers: five tokens of four sequences 13.5 and 15.2.  A step of 17 to 32
-  // query rows keeps them in the one workgroup that appends: two would not see
-  // each other's rows.
+  // to 70K rows (28/4 heads, five tokens) 56 and 49, four over 4K (64/8, eight
+  // tokens) 25 and 20, eight over 16K (32 query rows) 54 and 48; but 64 over 300
+  // to 993 rows (28) 15.0 and 16.2, one over 64 rows 5.5 and 6.9.  fp32, whose
+  // parts fill the registers: five tokens of four sequences 12.8 and 14.4.  A
+  // step of 17 to 32 query rows keeps them in the one workgroup that appends:
+  // two would not see each other's rows.
   const bool shared = bf16 && a.chunk > 256 && (R > 32 || a.chunk > 1024);
   const bool one = R <= 16 || !(a.k || shared);
   a.groups = (R + (one ? 15 : 31)) / (one ? 16 : 32);
