@@ -129,7 +129,16 @@ __device__ __forceinline__ float xor16_32_max(float v) {
 // 32 fp32 queries of 128 dimensions need more and take 4.
 constexpr int max_waves(bool bf16, int d, int nt) { return nt == 2 && !bf16 && d == 128 ? 4 : 8; }
 
-constexpr float kFloor = -1e30f;       // maximum of no logits
+// Maximum of no logits: below every finite one, since a sum of products in 32
+// bits is scaled by log2(e) / sqrt(d) < 1/5.
+constexpr float kFloor = -3.402823466e38f;
+
+// a - b of two values rounded before (a product and a subtraction joined into
+// one rounding would not give 0 for equal ones).
+__device__ __forceinline__ float minus(float a, float b) {
+#pragma clang fp contract(off)
+  return a - b;
+}
 
 template <int D>
 constexpr int o_pitch() { return D + 4; }
@@ -343,6 +352,12 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     bf16x8 w[NT][2][PP];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      // In units of log2, rounded before the maximum is taken from them: the
+      // largest logit's weight is then 1 whatever its size (a fused product and
+      // difference is off by up to 2^-24 of the logit, which past 2^31 leaves no
+      // weight or an infinite one).
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[nt][i] *= a.scale_log2;
       if (masked) {
         const int n = here ? end[nt] - (base + 16 * g) : 0;
 #pragma unroll
@@ -356,7 +371,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, s[nt][i][e]);
-      top = fmaxf(mx[nt], xor16_32_max(top) * a.scale_log2);
+      top = fmaxf(mx[nt], xor16_32_max(top));
       if (__any(top > mx[nt])) {
         const float f = __builtin_amdgcn_exp2f(mx[nt] - top);
         mx[nt] = top;
@@ -369,7 +384,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
         float x8[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x8[e] = __builtin_amdgcn_exp2f(fmaf(s[nt][2 * u + (e >> 2)][e & 3], a.scale_log2, -mx[nt]));
+          x8[e] = __builtin_amdgcn_exp2f(minus(s[nt][2 * u + (e >> 2)][e & 3], mx[nt]));
           sum[nt] += x8[e];
         }
         split8<PP>(x8, w[nt][u]);

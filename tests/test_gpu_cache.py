@@ -856,3 +856,57 @@ def test_prompt_then_decode(adaptive):
     for l in range(L):
         m.check_values(l)
     assert c.bacon_cache_errors() == 0
+
+
+# ------------------------------------------------- ends of the numbers' range
+
+def _equal_keys(m, sign, power, rows):
+    """Keys that are 1.375 x 2^a in the first dimension (1.5 x 2^a in every third
+    row) and 0 elsewhere, and queries of their own value x 2^b there, a + b =
+    power: every logit is the same product in every row of its kind, so the
+    softmax is the mean over the kind that `sign` makes the larger, exactly.
+    Returns queries and the kinds."""
+    import torch
+    a = power // 2
+    kind = np.arange(rows) % 3 == 2
+    key = np.where(kind, 1.5, 1.375) * 2.0 ** a
+    q = m.tokens(1, m.hq)
+    first = (1.0 + q[..., 0].abs() % 1.0) * sign * 2.0 ** (power - a)
+    q.zero_()
+    q[..., 0] = first
+    k = torch.zeros(rows, m.H, m.d, dtype=q.dtype, device="cuda")
+    k[..., 0] = torch.from_numpy(key).cuda()[:, None].to(q.dtype)
+    return q, k, kind if sign > 0 else ~kind
+
+
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("fp32", 64, 1), ("fp32", 128, 17), ("bf16", 64, 20)])
+@pytest.mark.parametrize("rows", [1, 2, 300, 5000])
+def test_attend_of_logits_as_large_as_floats(dtype, d, G, rows):
+    """Logits of either sign up to 2^120: finite ones never count as no row, and
+    the largest has weight 1 whatever its size.  Weights are 0 and 1 exactly, so the
+    bound is that of the sums (n / 16 + 64 terms a chain, as in cache_ref) and of the
+    output's rounding; lse comes of at most eight roundings (of the sum over the query's
+    parts two, the scale, the product, log2 l and its sum, ln 2, the product)."""
+    from paper_2606_14782_amd import bacon
+    for power in (40, 70, 104, 120):
+        for sign in (1, -1):
+            m = Model([[1]], G, d, 32, dtype)
+            q, k, kind = _equal_keys(m, sign, power, rows)
+            v = _rand(m.rng, rows, 1, d, dtype=dtype)
+            m.c = _cache(1, G, 1, d, 1, 32, 1, rows, rows // 32 + 2, dtype)
+            batch = bacon.BatchLayout([0, rows], [max(1, rows - 1)])
+            m.c.bacon_cache_tables(batch)
+            m.c.bacon_cache_store(batch, [k], [v])
+            for kv, x in ((0, k), (1, v)):
+                m.rows[0][0][0][kv].store(_np(x)[:, 0])
+            m.check_values()
+            out, lse = m.c.bacon_cache_attend(0, q, want_lse=True)
+            held, key = m.rows[0][0][0][1].x, m.rows[0][0][0][0].x[:, 0]
+            won = held[kind] if kind.any() else held
+            s = _np(q)[0, 0, :, 0] * (key[kind].max() if kind.any() else key[0]) / math.sqrt(d)
+            h = 2.0 ** -24
+            tol = R.HALF[dtype] * np.abs(won.mean(0)) + (2 * (rows / 16 + 64) + 4) * h * np.abs(won).mean(0) * 1.01
+            assert np.all(np.abs(_np(out)[0, 0] - won.mean(0)) <= tol), (power, sign)
+            want = s + math.log(len(won))
+            assert np.all(np.abs(_np(lse)[0, 0] - want) <= 8 * h * np.abs(want)), (power, sign)
+            assert m.c.bacon_cache_errors() == 0
