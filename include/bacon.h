@@ -491,7 +491,11 @@ bacon_status bacon_cache_append(bacon_cache *cache, int32_t layer, int32_t first
  * d_k above, with Hq heads; d_out [num_seqs, tokens, Hq, d] in the cache's
  * dtype; d_lse (optional) [num_seqs, tokens, Hq] float32, the natural log of
  * the normaliser.  A query that sees no row, and a query j >= c (a padded
- * batch), gives zeros and -infinity.  G * tokens <= 64, G = Hq / Hkv.
+ * batch), gives zeros and -infinity.  Logits are sums in 32 bits: a query with
+ * one that is NaN or +infinity (it is not finite itself, or the sum passes the
+ * largest float), or with none above -infinity, gives NaN throughout, and sums of
+ * weighted values past the largest float are infinite or NaN.
+ * G * tokens <= 64, G = Hq / Hkv.
  * max_tokens: the longest length to expect (0: the table's), which settles
  * how the work is divided; longer pairs are right, only slower.  d_work: scratch of
  * bacon_cache_work_bytes (0: may be NULL), 256-byte aligned, of this call

@@ -133,6 +133,10 @@ constexpr int max_waves(bool bf16, int d, int nt) { return nt == 2 && !bf16 && d
 // bits is scaled by log2(e) / sqrt(d) < 1/5.
 constexpr float kFloor = -3.402823466e38f;
 
+// A query's maximum over no row at all, in what waves, parts and groups hand on:
+// what tells "sees no row" from logits that fell below all floats.
+constexpr float kNoRow = -INFINITY;
+
 // a - b of two values rounded before (a product and a subtraction joined into
 // one rounding would not give 0 for equal ones).
 __device__ __forceinline__ float minus(float a, float b) {
@@ -178,16 +182,18 @@ __device__ __forceinline__ void raw_floats(const QRaw<BF16> &r, float (&x)[8]) {
   }
 }
 
-// Four dimensions of a query's output from their weighted sums, and its normaliser.
+// Four dimensions of a query's output from their weighted sums (zeros where it
+// sees no row), its normaliser and its maximum.  A query that sees rows has a
+// normaliser of 1 at least, unless its logits are no numbers (a NaN or an
+// infinite one, or none above the least float): then all of it is NaN.
 template <bool BF16, int D>
-__device__ __forceinline__ void store_out(const CacheStepArgs &a, int64_t at, int dim, f32x4 acc, float l, float top,
-                                          bool none) {
-  const float inv = none ? 0.f : 1.f / l;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) acc[e] = none ? 0.f : acc[e] * inv;
+__device__ __forceinline__ void store_out(const CacheStepArgs &a, int64_t at, int dim, f32x4 acc, float l, float top) {
+  const bool none = top == kNoRow;
+  l = none ? 1.f : l > 0.f ? l : __builtin_nanf("");
+  acc *= 1.f / l;
   if constexpr (BF16) {
-    const u32x2 u = {float_bf16(acc[0]) | float_bf16(acc[1]) << 16, float_bf16(acc[2]) | float_bf16(acc[3]) << 16};
-    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + at * D + dim) = u;
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(a.out) + at * D + dim) = __builtin_convertvector(acc, bf16x4);
   } else {
     *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at * D + dim) = acc;
   }
@@ -310,9 +316,11 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
 
   f32x4 o[NT][D / 16];
   float mx[NT], sum[NT];
+  int seen[NT];                        // whether this lane's rows held one that the query sees
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     mx[nt] = kFloor;
+    seen[nt] = 0;
     sum[nt] = 0.f;
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) o[nt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -352,20 +360,23 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     bf16x8 w[NT][2][PP];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      if (masked) {
+        const int n = here ? end[nt] - (base + 16 * g) : 0;
+        seen[nt] |= n > 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (4 * i + e >= n) s[nt][i][e] = -INFINITY;
+      } else {
+        seen[nt] = 1;
+      }
       // In units of log2, rounded before the maximum is taken from them: the
       // largest logit's weight is then 1 whatever its size (a fused product and
       // difference is off by up to 2^-24 of the logit, which past 2^31 leaves no
       // weight or an infinite one).
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[nt][i] *= a.scale_log2;
-      if (masked) {
-        const int n = here ? end[nt] - (base + 16 * g) : 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (4 * i + e >= n) s[nt][i][e] = -INFINITY;
-      }
       float top = s[nt][0][0];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -426,9 +437,10 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   for (int nt = 0; nt < NT; ++nt) {
     float l = sum[nt] + __shfl_xor(sum[nt], 16);
     l += __shfl_xor(l, 32);
+    const bool any = (__ballot(seen[nt]) >> m & 0x0001000100010001ull) != 0;
     const int n = nt * 16 + m, at = wave * NT * 16 + n;
     if (row0 + n >= R) continue;
-    if (g == 0) *reinterpret_cast<float2 *>(ml + at * 2) = make_float2(mx[nt], l);
+    if (g == 0) *reinterpret_cast<float2 *>(ml + at * 2) = make_float2(any ? mx[nt] : kNoRow, l);
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4 *>(oo + at * P + 16 * e + 4 * g) = o[nt][e];
   }
@@ -446,24 +458,29 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
         part[w] = *reinterpret_cast<const float2 *>(ml + (w * NT * 16 + n) * 2);
         x[w] = *reinterpret_cast<const f32x4 *>(oo + (w * NT * 16 + n) * P + dim);
       }
-      float top = kFloor, l = 0.f;
+      float top = kNoRow, l = 0.f;
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) top = fmaxf(top, part[w].x);
+      const float most = fmaxf(top, kFloor);
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
-        const float f = __builtin_amdgcn_exp2f(part[w].x - top);
+        const float f = __builtin_amdgcn_exp2f(part[w].x - most);
         l += f * part[w].y;
         acc += f * x[w];
       }
       const int j = token_of(a, r);
-      const bool none = j >= count || !(l > 0.f);
+      if (j >= count) {                                      // padding sees no row, whatever its query is
+        top = kNoRow;
+        l = 0.f;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
       if (a.splits > 1) {
         const int64_t at = ((int64_t)bh * a.splits + split) * R + r;
-        if (dim == 0) a.part_ml[at] = make_float2(top, none ? 0.f : l);
-        *reinterpret_cast<f32x4 *>(a.part_o + at * D + dim) = acc;   // finite, also where there is none
+        if (dim == 0) a.part_ml[at] = make_float2(top, l);
+        *reinterpret_cast<f32x4 *>(a.part_o + at * D + dim) = acc;   // zeros where no row is seen
       } else {
-        store_out<BF16, D>(a, ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G), dim, acc, l, top, none);
+        store_out<BF16, D>(a, ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G), dim, acc, l, top);
       }
     }
   };
@@ -485,7 +502,7 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
   const int r = blockIdx.x, h = blockIdx.y, b = blockIdx.z, bh = b * c.Hkv + h, j = token_of(a, r);
   const float2 *ml = a.part_ml + (int64_t)bh * a.splits * R + r;
   const f32x4 *o = reinterpret_cast<const f32x4 *>(a.part_o) + ((int64_t)bh * a.splits * R + r) * TR + dim;
-  float top = kFloor, l = 0.f;
+  float top = kNoRow, most = kFloor, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int i = group; i < a.splits; i += 4 * SP) {
     float2 x[4];
@@ -495,16 +512,16 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
       const int64_t at = (int64_t)min(i + u * SP, a.splits - 1) * R;
       x[u] = ml[at];
       y[u] = o[at * TR];
-      if (i + u * SP >= a.splits) x[u] = make_float2(kFloor, 0.f);
+      if (i + u * SP >= a.splits) x[u] = make_float2(kNoRow, 0.f);   // (the last part's sums, times 0)
     }
-    const float m = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), top);
-    const float f = __builtin_amdgcn_exp2f(top - m);
+    top = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), top);
+    const float m = fmaxf(top, kFloor), f = __builtin_amdgcn_exp2f(most - m);
     l *= f;
     acc *= f;
-    top = m;
+    most = m;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float g = x[u].y > 0.f ? __builtin_amdgcn_exp2f(x[u].x - m) : 0.f;
+      const float g = __builtin_amdgcn_exp2f(x[u].x - m);
       l += g * x[u].y;
       acc += g * y[u];
     }
@@ -529,15 +546,16 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheStepArgs a) {
   top = x[0].x;
 #pragma unroll
   for (int i = 1; i < SP; ++i) top = fmaxf(top, x[i].x);
+  most = fmaxf(top, kFloor);
   l = 0.f;
   acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < SP; ++i) {
-    const float g = __builtin_amdgcn_exp2f(x[i].x - top);
+    const float g = __builtin_amdgcn_exp2f(x[i].x - most);
     l += g * x[i].y;
     acc += g * y[i];
   }
-  store_out<BF16, D>(a, ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G), t * 4, acc, l, top, !(l > 0.f));
+  store_out<BF16, D>(a, ((int64_t)b * a.tokens + j) * c.Hq + h * G + (r - j * G), t * 4, acc, l, top);
 }
 
 template <bool BF16, int D, int NT>

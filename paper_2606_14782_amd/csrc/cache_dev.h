@@ -19,12 +19,6 @@ constexpr float kLn2f = 0.69314718055994531f;
 
 __device__ __forceinline__ float bf16_float(unsigned bits) { return __uint_as_float(bits << 16); }
 
-// bfloat16 bits of x, rounded to nearest, ties to even (x finite).
-__device__ __forceinline__ unsigned float_bf16(float x) {
-  const unsigned u = __float_as_uint(x);
-  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-}
-
 // 2^e as a float, -126 <= e <= 127.
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 

@@ -910,3 +910,67 @@ def test_attend_of_logits_as_large_as_floats(dtype, d, G, rows):
             want = s + math.log(len(won))
             assert np.all(np.abs(_np(lse)[0, 0] - want) <= 8 * h * np.abs(want)), (power, sign)
             assert m.c.bacon_cache_errors() == 0
+
+
+@pytest.mark.parametrize("dtype,d,G,n", [("bf16", 128, 4, 1), ("fp32", 64, 7, 3), ("bf16", 64, 7, 4), ("fp32", 128, 5, 5)])
+@pytest.mark.parametrize("lens", [[[40, 1], [300, 65]], [[4100, 2000], [3, 1000]]])
+def test_a_query_that_is_not_finite_is_nan_alone(dtype, d, G, n, lens):
+    """All of its output and its lse, however the rows are divided; the other
+    queries of its workgroup as without it, bit for bit."""
+    import torch
+    m = Model(lens, 2 * G, d, 64, dtype)
+    q = m.tokens(n, 2 * G, 1.5)
+    out, lse = m.c.bacon_cache_attend(0, q, want_lse=True)
+    m.check_attend(q, out, lse)
+    bad = torch.zeros(lse.shape, dtype=torch.bool, device="cuda")
+    for i, (b, h, x) in enumerate(((0, 0, math.nan), (0, 2 * G - 1, math.inf), (1, 1, -math.inf), (1, G, math.nan))):
+        q[b, n - 1 - i % n, h, 7 * i] = x
+        bad[b, n - 1 - i % n, h] = True
+    bad &= ~torch.isneginf(lse)                       # (a query that sees no row stays one)
+    got, glse = m.c.bacon_cache_attend(0, q, want_lse=True)
+    assert got[bad].isnan().all() and glse[bad].isnan().all()
+    assert torch.equal(got[~bad], out[~bad]) and torch.equal(glse[~bad], lse[~bad])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 64)])
+@pytest.mark.parametrize("rows", [1, 128, 5000])
+def test_logits_past_the_largest_float(dtype, d, rows):
+    """Infinite logits: upward NaN, downward no weight, and NaN where that leaves none.
+    The first half's logits are 0: their weights are equal."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    half = rows // 128 * 64
+    m = Model([[1]], 4, d, 32, dtype)
+    q, v = m.tokens(1, 4) * 0, _rand(m.rng, rows, 1, d, dtype=dtype)
+    q[0, 0, :, 0] = torch.tensor([2.0 ** 20, -2.0 ** 20, -2.0 ** 60, 0.0])
+    for low in (half, 0):                             # rows whose logits are 0
+        k = torch.zeros(rows, 1, d, dtype=q.dtype, device="cuda")
+        k[low:, 0, 0] = 2.0 ** 127
+        c = _cache(1, 4, 1, d, 1, 32, 1, rows, rows // 32 + 2, dtype)
+        batch = bacon.BatchLayout([0, rows], [max(1, rows - 1)])
+        c.bacon_cache_tables(batch)
+        c.bacon_cache_store(batch, [k], [v])
+        m.rows[0][0][0][1].store(_np(v)[:, 0])
+        held, h = m.rows[0][0][0][1].x, 2.0 ** -24
+        out, lse = c.bacon_cache_attend(0, q, want_lse=True)
+        on, ln = _np(out)[0, 0], _np(lse)[0, 0]
+        for i, seen in enumerate((0, low, low, rows)):
+            if not seen:
+                assert np.isnan(on[i]).all() and np.isnan(ln[i]), (low, i)
+                continue
+            won = held[:seen]
+            tol = R.HALF[dtype] * np.abs(won.mean(0)) + (2 * (rows / 16 + 64) + 4) * h * np.abs(won).mean(0) * 1.01
+            assert np.all(np.abs(on[i] - won.mean(0)) <= tol), (low, i)
+            assert abs(ln[i] - math.log(seen)) <= (rows / 16 + 64 + 8) * h * (1 + math.log(seen)), (low, i)
+
+
+@pytest.mark.parametrize("lens", [[[200, 130], [70, 300]], [[2500, 130], [70, 4000]]])
+def test_padding_may_hold_anything(lens):
+    """Padding queries over whole tiles of rows: zeros and -infinity, whatever they hold."""
+    import torch
+    m = Model(lens, 6, 64, 32, "bf16")
+    counts = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    q = m.tokens(4, 6)
+    q[0, 1:], q[1] = math.nan, math.inf
+    out, lse = m.c.bacon_cache_attend(0, q, counts, want_lse=True)
+    m.check_attend(q, out, lse, [1, 0])
