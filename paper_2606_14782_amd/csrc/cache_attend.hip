@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "allow_lds.h"
 #include "cache_dev.h"
 
 namespace bacon {
@@ -564,18 +565,6 @@ constexpr int attend_lds(int waves) {
   return q > o ? q : o;
 }
 
-// Allows a kernel more dynamic LDS than the default 64 KB, once per instance.
-template <bool BF16, int D, int NT>
-void allow_lds() {
-  static const bool done = [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_cache_attend<BF16, D, NT>),
-                              hipFuncAttributeMaxDynamicSharedMemorySize,
-                              attend_lds<BF16, D, NT>(max_waves(BF16, D, NT)));
-    return true;
-  }();
-  (void)done;
-}
-
 template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const int units = a.num_seqs * a.c.Hkv * a.splits;
@@ -585,7 +574,7 @@ hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   // sequences of four drafted tokens 18.5 us, with four 19.1).  Elsewhere eight
   // are slower (64 sequences over 300 to 993 rows 22.6 us, with four 17.2).
   const int waves = NT == 2 && a.groups == 1 && a.chunk > 256 && max_waves(BF16, D, NT) == 8 ? 8 : 4;
-  allow_lds<BF16, D, NT>();
+  if (hipError_t e = allow_lds<k_cache_attend<BF16, D, NT>>(attend_lds<BF16, D, NT>(waves))) return e;
   const dim3 grid = a.groups == 1 ? dim3(a.splits, a.c.Hkv, a.num_seqs) : dim3((units + 7) / 8 * 8 * a.groups);
   hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), grid, dim3(64 * waves), (attend_lds<BF16, D, NT>(waves)), s,
                      a);
