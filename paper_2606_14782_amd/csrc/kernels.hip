@@ -28,10 +28,10 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <math.h>
 #include <stdint.h>
 
+#include "allow_lds.h"
 #include "internal.h"
 
 namespace bacon {
@@ -204,17 +204,6 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-}
-
-// Dynamic LDS above 64 KiB has to be allowed per kernel before launch.
-template <auto Kern>
-static void allow_lds(size_t bytes) {
-  static std::atomic<size_t> granted{0};
-  if (bytes > 64 * 1024 && bytes > granted) {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(Kern),
-                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    granted = bytes;
-  }
 }
 
 // ---------------------------------------------------------------- passes
@@ -568,7 +557,7 @@ static hipError_t launch_pass_dual_t(const PassArgs &a2, const PassArgs &a1, con
                            pass_lds_bytes(PASS_LSE, BF16, D, a1.Rpad, a1.chunk));
   if (lds > kLdsBytes || a1.Rpad != a2.Rpad || a1.chunk != a2.chunk) return hipErrorInvalidValue;
   dim3 grid(2 * st.total_chunks, a2.Hkv), block(64 * nw);
-  allow_lds<k_pass_dual<BF16, D, W32>>(lds);
+  if (hipError_t e = allow_lds<k_pass_dual<BF16, D, W32>>(lds)) return e;
   hipLaunchKernelGGL((k_pass_dual<BF16, D, W32>), grid, block, lds, s, a2, a1, st);
   return hipGetLastError();
 }
@@ -593,7 +582,7 @@ static hipError_t launch_pass_t(const PassArgs &a, const SeqTable &st, hipStream
   const int lds = pass_lds_bytes(MODE, BF16, D, a.Rpad, a.chunk);
   if (lds > kLdsBytes) return hipErrorInvalidValue;
   dim3 grid(st.total_chunks, a.Hkv), block(64 * nw);
-  allow_lds<k_pass<MODE, BF16, D, W32>>(lds);
+  if (hipError_t e = allow_lds<k_pass<MODE, BF16, D, W32>>(lds)) return e;
   hipLaunchKernelGGL((k_pass<MODE, BF16, D, W32>), grid, block, lds, s, a, st);
   return hipGetLastError();
 }
@@ -1074,7 +1063,7 @@ static hipError_t launch_dual_t(const PassArgs &a2, const PassArgs &a1, const Se
   const int lds = kr_lds_bytes(true, D, a2.Rpad);
   if (lds > kLdsBytes) return hipErrorInvalidValue;
   constexpr auto kern = k_krdual<D, W32, NRT>;
-  allow_lds<kern>(lds);
+  if (hipError_t e = allow_lds<kern>(lds)) return e;
   hipLaunchKernelGGL(kern, dim3(2 * st.total_chunks, a2.Hkv), dim3(64 * kKrWaves), lds, s, a2, a1,
                      st);
   return hipGetLastError();
@@ -1093,7 +1082,7 @@ static hipError_t launch_kr_t(const PassArgs &a, const SeqTable &st, hipStream_t
   const int lds = kr_lds_bytes(true, D, a.Rpad);
   if (lds > kLdsBytes) return hipErrorInvalidValue;
   constexpr auto kern = k_krpass<MODE, D, W32, NRT>;
-  allow_lds<kern>(lds);
+  if (hipError_t e = allow_lds<kern>(lds)) return e;
   hipLaunchKernelGGL(kern, dim3(st.total_chunks, a.Hkv), dim3(64 * kKrWaves), lds, s, a, st);
   return hipGetLastError();
 }
@@ -2124,7 +2113,7 @@ static hipError_t launch_single_t(const PassArgs &a, const SeqTable &st, hipStre
   const int lds = single_lds_bytes(D, a.Rpad);
   if (lds > kLdsBytes / 2) return hipErrorInvalidValue;
   constexpr auto kern = k_single<D, W32, NRT>;
-  allow_lds<kern>(lds);
+  if (hipError_t e = allow_lds<kern>(lds)) return e;
   hipLaunchKernelGGL(kern, dim3(st.total_chunks * a.Hkv), dim3(64 * kKrWaves), lds, s, a, st);
   return hipGetLastError();
 }
@@ -2817,7 +2806,7 @@ size_t select_lds_bytes() {
 hipError_t launch_select(const SelArgs &a, const SeqTable &st, hipStream_t s) {
   const size_t lds = select_lds_bytes() - sizeof(SelShared);
   if (lds + sizeof(SelShared) > kLdsBytes) return hipErrorInvalidValue;
-  allow_lds<k_select>(lds);
+  if (hipError_t e = allow_lds<k_select>(lds)) return e;
   hipLaunchKernelGGL(k_select, dim3(st.batch, a.Hkv), dim3(kSelThreads), lds, s, a, st);
   return hipGetLastError();
 }
@@ -4436,7 +4425,7 @@ size_t final_lds_bytes(int max_budget, int window) {
 
 template <int JOB>
 static hipError_t launch_sel_one(const SegArgs &a, const SeqTable &st, int jobs, size_t lds, hipStream_t s) {
-  allow_lds<k_sel_one<JOB>>(lds);
+  if (hipError_t e = allow_lds<k_sel_one<JOB>>(lds)) return e;
   hipLaunchKernelGGL(k_sel_one<JOB>, dim3(jobs, a.Hkv), dim3(kSegThreads), lds, s, a, st);
   return hipGetLastError();
 }
@@ -4480,11 +4469,11 @@ hipError_t launch_sel(const SelJobs &j, const SeqTable &st, hipStream_t s) {
     return hipGetLastError();
   };
   if (adapt) {
-    allow_lds<k_sel<true>>(lds);
+    if (hipError_t e = allow_lds<k_sel<true>>(lds)) return e;
     const AllocSet<true> as = alloc_set(j, st);
     return go(k_sel<true>, as.npool + as.nlist + as.npick, as);
   }
-  allow_lds<k_sel<false>>(lds);
+  if (hipError_t e = allow_lds<k_sel<false>>(lds)) return e;
   return go(k_sel<false>, 0, AllocSet<false>{});
 }
 
@@ -4492,13 +4481,13 @@ hipError_t launch_alloc(int stage, const AllocArgs &a, const SeqTable &st, hipSt
   if (!alloc_ok(&a)) return hipErrorInvalidValue;
   const size_t lds = stage == 0 ? sizeof(AllocPoolLds) : stage == 1 ? sizeof(AllocListLds) : alloc_pick_lds(a.Hkv);
   if (stage == 0) {
-    allow_lds<k_alloc<JOB_POOL>>(lds);
+    if (hipError_t e = allow_lds<k_alloc<JOB_POOL>>(lds)) return e;
     hipLaunchKernelGGL(k_alloc<JOB_POOL>, dim3(a.Hkv, st.total_segs), dim3(kSegThreads), lds, s, a, st);
   } else if (stage == 1) {
-    allow_lds<k_alloc<JOB_LIST>>(lds);
+    if (hipError_t e = allow_lds<k_alloc<JOB_LIST>>(lds)) return e;
     hipLaunchKernelGGL(k_alloc<JOB_LIST>, dim3(a.Hkv, st.total_segs), dim3(kSegThreads), lds, s, a, st);
   } else {
-    allow_lds<k_alloc<JOB_PICK>>(lds);
+    if (hipError_t e = allow_lds<k_alloc<JOB_PICK>>(lds)) return e;
     hipLaunchKernelGGL(k_alloc<JOB_PICK>, dim3(st.batch), dim3(kSegThreads), lds, s, a, st);
   }
   return hipGetLastError();
@@ -4557,10 +4546,10 @@ static hipError_t launch_wide_t(int mode, const PassArgs &a, const SeqTable &st,
   const int lds = wide_lds_bytes(BF16, D, a.Rpad, 1 << a.wide_split_log);
   const dim3 grid(a.Hkv, a.wide_jobs), block(kSegThreads);
   if (mode == PASS_LSE) {
-    allow_lds<k_wide<PASS_LSE, BF16, D>>(lds);
+    if (hipError_t e = allow_lds<k_wide<PASS_LSE, BF16, D>>(lds)) return e;
     hipLaunchKernelGGL((k_wide<PASS_LSE, BF16, D>), grid, block, lds, s, a, st);
   } else {
-    allow_lds<k_wide<PASS_FUSED, BF16, D>>(lds);
+    if (hipError_t e = allow_lds<k_wide<PASS_FUSED, BF16, D>>(lds)) return e;
     hipLaunchKernelGGL((k_wide<PASS_FUSED, BF16, D>), grid, block, lds, s, a, st);
   }
   return hipGetLastError();
@@ -4617,11 +4606,11 @@ static hipError_t launch_mega_t(const SelJobs &j, const PassArgs *p2, const Pass
     return hipGetLastError();
   };
   if (adapt) {
-    allow_lds<k_mega<BF16, D, true>>(lds);
+    if (hipError_t e = allow_lds<k_mega<BF16, D, true>>(lds)) return e;
     const AllocSet<true> as = alloc_set(j, st);
     return go(k_mega<BF16, D, true>, as.npool + as.nlist + as.npick, as);
   }
-  allow_lds<k_mega<BF16, D, false>>(lds);
+  if (hipError_t e = allow_lds<k_mega<BF16, D, false>>(lds)) return e;
   return go(k_mega<BF16, D, false>, 0, AllocSet<false>{});
 }
 hipError_t launch_mega(bool bf16, int head_dim, const SelJobs &j, const PassArgs *p2, const PassArgs *p1,

@@ -53,3 +53,15 @@ def test_grants_are_by_device(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-Wall", "-pthread", "-I", CSRC, "-o", exe, str(src)], check=True)
     res = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert res.returncode == 0, res.stdout
+
+
+def test_kernels_are_granted_by_no_other_way():
+    """Every launch of the library takes its grant from there, and looks at its status."""
+    for name in os.listdir(CSRC):
+        with open(os.path.join(CSRC, name)) as f:
+            text = f.read()
+        if name != "allow_lds.h":
+            assert "hipFuncSetAttribute" not in text, name
+        for line in text.splitlines():
+            if "allow_lds<" in line:
+                assert "hipError_t e = allow_lds<" in line, (name, line)
