@@ -368,7 +368,7 @@ int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
  *
  * Every pair has a length (rows held), a row of the block table (max_blocks
  * block ids, -1 where it has none) and the offset of its entries in the
- * layer's idx.  They lie in device memory with the codes: lengths that only the
+ * layer's idx (-1 past 2^31 - 1).  They lie in device memory with the codes: lengths that only the
  * device knows (BACON_ALLOC_ADAPTIVE) never pass through the host.  Row p of a
  * pair is row p % block_tokens of block table[p / block_tokens].
  *
@@ -457,8 +457,8 @@ bacon_status bacon_cache_tables(bacon_cache *cache, const bacon_batch *batch, in
  * bacon_compact reads them; d_idx: such an array of their idx, idx_count
  * entries each.  The pair's rows are its kept positions in ascending order,
  * then the window's; d_idx NULL stands for idx entries 0, 1, 2, ... (every row,
- * where the budget is N_b - W).  An entry past idx_count, or outside the
- * candidates, gives a zero row (BAD_INDEX). */
+ * where the budget is N_b - W).  An entry past idx_count or 2^31 - 1, or outside
+ * the candidates, gives a zero row (BAD_INDEX). */
 bacon_status bacon_cache_store(bacon_cache *cache, const bacon_batch *batch, int32_t first_seq,
                                int32_t first_layer, int32_t num_layers, const void *const *d_k,
                                const void *const *d_v, const int32_t *const *d_idx, int64_t idx_count,

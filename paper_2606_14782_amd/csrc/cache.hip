@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kTabThreads) void k_cache_tables(CacheTablesArgs a,
       s_need[lane] = fits ? n.need : 0;
       s_row[lane] = pair * c.max_blocks;
       c.lens[pair] = fits ? n.rows : 0;
-      c.starts[pair] = (int)start;
+      c.starts[pair] = start > 0x7FFFFFFF ? -1 : (int)start;   // -1: the store finds no entry there
       if (a.used && p == pairs - 1) *a.used = first + n.need;
     }
   }

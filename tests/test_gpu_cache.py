@@ -974,3 +974,28 @@ def test_padding_may_hold_anything(lens):
     q[0, 1:], q[1] = math.nan, math.inf
     out, lse = m.c.bacon_cache_attend(0, q, counts, want_lse=True)
     m.check_attend(q, out, lse, [1, 0])
+
+
+@pytest.mark.parametrize("device", [False, True])
+def test_budgets_whose_sum_passes_32_bits(device):
+    """Offsets into idx past 2^31 - 1 name no entry, also where they are small
+    numbers again past 2^32: the rows are zero, no other pair's."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(31)
+    H, W, N, big = 8, 2, 12, 1 << 30
+    c = _cache(2, H, H, 64, W, 16, 1, 16, 40, "fp32")
+    batch = bacon.BatchLayout([0, N], [big])
+    bud = torch.full((2, 1, H), big, dtype=torch.int32, device="cuda")
+    c.bacon_cache_tables(batch, bud if device else None)
+    assert (c.lens == N).all()
+    starts = c.starts[:, 0].cpu().numpy()
+    assert (starts == [0, big] + [-1] * (H - 2)).all()
+    k, v = (_rand(rng, 2, N, H, 64, dtype="fp32") for _ in range(2))
+    idx = torch.arange(N - W, dtype=torch.int32, device="cuda").expand(2, N - W).contiguous()
+    c.bacon_cache_store(batch, k, v, idx)
+    got = c.bacon_cache_load(N)
+    for x in got:
+        assert x[:, 0, 0].any(-1).all()                           # entries 0 .. 9
+        assert not x[:, 0, 1:, :N - W].any() and x[:, 0, :, N - W:].any(-1).all()
+    assert c.bacon_cache_errors() == bacon.CACHE_BAD_INDEX
