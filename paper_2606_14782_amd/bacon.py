@@ -554,9 +554,12 @@ class Cache:
             if budgets.dim() != 3 or budgets.shape[0] != s.num_layers or budgets.shape[2] != s.num_kv_heads:
                 raise BaconError(ERR_INVALID, f"budgets have shape {tuple(budgets.shape)}")
             nb = budgets.shape[1]
+        ids = self._whole(free, "free", self._torch.int32)
+        if free is not None and not ids:              # an empty tensor's address is NULL, which stands for every id
+            ids = self.memory.data_ptr()
         self._call(self._L.bacon_cache_tables, C.byref(batch.c), first_seq,
                    self._whole(budgets, "budgets", self._torch.int32), nb, reserve,
-                   self._whole(free, "free", self._torch.int32), 0 if free is None else free.numel(),
+                   ids, 0 if free is None else free.numel(),
                    self._whole(used, "used", self._torch.int64, (1,)))
         return used
 

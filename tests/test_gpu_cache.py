@@ -999,3 +999,19 @@ def test_budgets_whose_sum_passes_32_bits(device):
         assert x[:, 0, 0].any(-1).all()                           # entries 0 .. 9
         assert not x[:, 0, 1:, :N - W].any() and x[:, 0, :, N - W:].any(-1).all()
     assert c.bacon_cache_errors() == bacon.CACHE_BAD_INDEX
+
+
+def test_an_empty_list_of_free_ids_gives_no_blocks():
+    """A pool without a free block: no pair takes the ids that others hold."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    c = _cache(1, 2, 2, 64, 4, 16, 2, 64, 10, "bf16")
+    c.bacon_cache_tables(bacon.BatchLayout([0, 40], [30]), None, 10)
+    table = c.table.clone()
+    for free in (torch.empty(0, dtype=torch.int32, device="cuda"), torch.arange(9, dtype=torch.int32, device="cuda")[9:]):
+        c.bacon_cache_clear(1, 1)
+        used = c.bacon_cache_tables(bacon.BatchLayout([0, 40], [30]), None, 10, free, first_seq=1)
+        assert int(used) == 6
+        assert torch.equal(c.table[:, 0], table[:, 0]) and (c.table[:, 1] == -1).all()
+        assert (c.lens[:, 0] == 34).all() and not c.lens[:, 1].any()
+        assert c.bacon_cache_errors() == bacon.CACHE_NO_BLOCKS
