@@ -102,6 +102,9 @@ hipError_t launch_cache_clear(const CacheDev &c, int first_seq, int num_seqs, bo
 hipError_t launch_cache_tables(CacheTablesArgs a, hipStream_t s);
 // most_rows: upper bound of a pair's rows.
 hipError_t launch_cache_store(const CacheStoreArgs &a, bool bf16, int head_dim, int most_rows, hipStream_t s);
+// Workgroups of 256 threads that a load takes; a launch holds fewer than 2^32 threads.
+int64_t cache_load_groups(int64_t pairs, int count, int head_dim);
+constexpr int64_t kCacheMaxGroups = (1 << 24) - 1;
 hipError_t launch_cache_load(const CacheLoadArgs &a, bool bf16, int head_dim, hipStream_t s);
 hipError_t launch_cache_append(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s);
 // Whether an attend of q_rows query rows per pair also appends a's new rows

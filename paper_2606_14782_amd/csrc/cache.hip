@@ -520,13 +520,19 @@ hipError_t launch_cache_store(const CacheStoreArgs &a, bool bf16, int head_dim, 
   return hipGetLastError();
 }
 
+static int64_t load_groups_of_pair(int count, int head_dim) {
+  const int rows = 16 * 256 / (head_dim / 2);                // a workgroup's; the first may lie anywhere in a group of 16
+  return (((int64_t)count + 15) / 16 * 16 + 16 + rows - 1) / rows;
+}
+
+int64_t cache_load_groups(int64_t pairs, int count, int head_dim) {
+  return pairs * load_groups_of_pair(count, head_dim);
+}
+
 hipError_t launch_cache_load(const CacheLoadArgs &a, bool bf16, int head_dim, hipStream_t s) {
   const int64_t pairs = (int64_t)a.layers * a.num_seqs * a.c.Hkv;
-  const int groups = 256 / (head_dim / 2);                   // of 16 rows, a workgroup's
-  const unsigned per_pair = (unsigned)((((int64_t)a.count + 15) / 16 + 1 + groups - 1) / groups);
-  if (pairs * per_pair > 0x7FFFFFFF) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(pairs * per_pair));
-  CACHE_LAUNCH(k_cache_load, grid, 256, s, a, per_pair);
+  const dim3 grid((unsigned)cache_load_groups(pairs, a.count, head_dim));
+  CACHE_LAUNCH(k_cache_load, grid, 256, s, a, (unsigned)load_groups_of_pair(a.count, head_dim));
   return hipGetLastError();
 }
 

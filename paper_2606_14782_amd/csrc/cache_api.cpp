@@ -373,7 +373,8 @@ bacon_status bacon_cache_load(bacon_cache *c, int32_t first_layer, int32_t num_l
     return fail(BACON_ERR_INVALID, "first_token %d outside [-2^30, 2^30]", first_token);
   TRY(check_ptr(d_k_out, "k_out", 16));
   TRY(check_ptr(d_v_out, "v_out", 16));
-  if ((double)num_layers * num_seqs * c->shape.num_kv_heads * ((double)count / 16 + 8) > (double)0x7FFFFFFF)
+  const int64_t pairs = (int64_t)num_layers * num_seqs * c->shape.num_kv_heads;
+  if (cache_load_groups(pairs, count, c->shape.head_dim) > kCacheMaxGroups)
     return fail(BACON_ERR_UNSUPPORTED, "a load of %d rows of %d layers and %d sequences is too large", count,
                 num_layers, num_seqs);
   TRY(check_cleared(c, first_seq, num_seqs));

@@ -189,3 +189,17 @@ def test_reference_rounding():
     r.append(np.full((1, 2), 1000.0))
     assert len(r) == 7 and r.e[0] == R.exponent(1.0) and r.e[1] == R.exponent(1000.0)
     assert np.allclose(r.x[4:6], 1.0) and np.allclose(r.x[6], 1024.0)
+
+
+def test_a_load_of_more_threads_than_a_launch_holds_is_refused():
+    """2^24 workgroups of 256 threads are one launch too large; one fewer goes on
+    to the next check."""
+    f = C.c_void_p(FAKE)
+    kw = dict(num_q_heads=1024, num_kv_heads=1024, max_batch=64, max_blocks=1, num_blocks=1, block_tokens=16)
+    for d, layers, count, status in ((64, 256, 1, bacon.ERR_UNSUPPORTED), (64, 255, 1, bacon.ERR_ORDER),
+                                     (64, 255, 112, bacon.ERR_ORDER), (64, 255, 113, bacon.ERR_UNSUPPORTED),
+                                     (128, 256, 48, bacon.ERR_UNSUPPORTED), (128, 255, 48, bacon.ERR_ORDER),
+                                     (128, 255, 49, bacon.ERR_UNSUPPORTED), (128, 1, 1 << 30, bacon.ERR_UNSUPPORTED)):
+        h = _cache(num_layers=layers, head_dim=d, **kw)
+        assert bacon.lib().bacon_cache_load(h, 0, layers, 0, 64, 0, count, f, f, None) == status, (d, layers, count)
+        bacon.lib().bacon_cache_free(h)
