@@ -508,7 +508,8 @@ size_t bacon_cache_work_bytes(const bacon_cache *cache, int32_t num_seqs, int32_
                               int32_t max_tokens);
 
 /* A decode step of one layer: bacon_cache_append, then bacon_cache_attend over
- * the grown cache, with the same results. */
+ * the grown cache.  The cache ends the same; outputs and lse are the same but for
+ * the order of their sums (a step may divide the rows otherwise). */
 bacon_status bacon_cache_step(bacon_cache *cache, int32_t layer, int32_t first_seq, int32_t num_seqs,
                               int32_t tokens, const int32_t *d_counts, const void *d_q, int64_t q_stride,
                               const void *d_k, int64_t k_stride, const void *d_v, int64_t v_stride,
