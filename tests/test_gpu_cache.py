@@ -1015,3 +1015,91 @@ def test_an_empty_list_of_free_ids_gives_no_blocks():
         assert torch.equal(c.table[:, 0], table[:, 0]) and (c.table[:, 1] == -1).all()
         assert (c.lens[:, 0] == 34).all() and not c.lens[:, 1].any()
         assert c.bacon_cache_errors() == bacon.CACHE_NO_BLOCKS
+
+
+# --------------------------------------------- appends into divided pairs
+
+@pytest.mark.parametrize("dtype,d,bt,G,n,part", [
+    ("bf16", 128, 64, 4, 4, 64), ("bf16", 64, 16, 1, 16, 64), ("bf16", 128, 32, 7, 2, 64), ("bf16", 128, 16, 8, 1, 64),
+    ("fp32", 64, 32, 5, 3, 64), ("fp32", 128, 16, 1, 13, 64), ("bf16", 128, 64, 5, 6, 256), ("bf16", 64, 16, 1, 32, 256),
+    ("fp32", 128, 32, 8, 4, 256), ("fp32", 64, 64, 3, 9, 256)])
+def test_step_over_the_borders_of_parts(dtype, d, bt, G, n, part):
+    """Pairs divided along their rows, lengths just below the border of two parts:
+    two workgroups put some of the new rows in place each, and the join moves the
+    lengths.  Parts are 64 rows for up to 16 query rows, else 256."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    parts = 20 if part == 64 else 10
+    lens = [[4 * part - 1, 2 * part - n // 2], [(parts - 1) * part - n, 5 * part - n - (n + 1) // 2]]
+    most = parts * part
+    m = Model(lens, 2 * G, d, bt, dtype, reserve=part + n)
+    assert bacon.lib().bacon_cache_work_bytes(m.c._h, 2, n, most) >= 4 * parts * G * n * (8 + 4 * d)   # divided so
+    counts = torch.tensor([n, (n + 1) // 2], dtype=torch.int32, device="cuda")
+    for i, cnt in enumerate((None, counts, None)):
+        q, k, v = m.tokens(n, 2 * G, 1.5), m.tokens(n, 2, 3.0 ** i), m.tokens(n, 2, 3.0 ** i)
+        out, lse = m.c.bacon_cache_step(0, q, k, v, cnt, max_tokens=most, want_lse=True)
+        cl = None if cnt is None else cnt.tolist()
+        m.append(k, v, cl)
+        m.check_values()
+        m.check_attend(q, out, lse, cl)
+    assert m.c.bacon_cache_errors() == 0
+
+
+@pytest.mark.parametrize("dtype,G,n", [("bf16", 4, 3), ("bf16", 5, 6), ("fp32", 1, 2)])
+def test_divided_step_without_room_attends_over_what_is_there(dtype, G, n):
+    """Two of four pairs have no block left: they stay, the others grow."""
+    from paper_2606_14782_amd import bacon
+    m = Model([[1024, 1000], [777, 2048]], 2 * G, 64, 32, dtype, reserve=0)
+    q, k, v = m.tokens(n, 2 * G), m.tokens(n, 2), m.tokens(n, 2)
+    assert bacon.lib().bacon_cache_work_bytes(m.c._h, 2, n, 2048) > 0
+    out, lse = m.c.bacon_cache_step(0, q, k, v, max_tokens=2048, want_lse=True)
+    kn, vn = _np(k), _np(v)
+    for b, h in ((0, 1), (1, 0)):
+        m.rows[0][b][h][0].append(kn[b, :, h])
+        m.rows[0][b][h][1].append(vn[b, :, h])
+    m.check_values()
+    m.check_attend(q, out, lse)
+    assert m.c.bacon_cache_errors() == bacon.CACHE_NO_BLOCKS
+
+
+@pytest.mark.parametrize("dtype,append", [("bf16", False), ("bf16", True), ("fp32", True)])
+def test_magnitudes_of_the_whole_range(dtype, append):
+    """Zeros, the least and the largest magnitudes, ties and subnormal codes,
+    stored or appended: the values held are the nearest, exactly."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(6)
+    bt, d = 16, 64
+    n = bt * 9
+    x = rng.standard_normal((n, 1, d))
+    x[:bt] = 0
+    x[bt:2 * bt] *= 2.0 ** -128
+    x[2 * bt:3 * bt] = np.clip(x[2 * bt:3 * bt], -1, 1) * 2.0 ** 127
+    x[3 * bt:4 * bt] = rng.integers(-448, 449, (bt, 1, d))
+    x[4 * bt:5 * bt] = rng.integers(-64, 65, (bt, 1, d)) * 2.0 ** -11
+    x[4 * bt, 0, 0] = 448
+    x[5 * bt, 0, 0] = 450
+    x[6 * bt:7 * bt] *= 2.0 ** -107                       # about the least scale
+    x[7 * bt + 3] *= 2.0 ** 100                           # rows whose scale leaves nothing of the others
+    t = torch.from_numpy(x).cuda().to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    c = _cache(1, 1, 1, d, 1, bt, 1, n, 10, dtype)
+    held = R.Rows(bt, d)
+    if append:
+        c.bacon_cache_tables(bacon.BatchLayout([0, 1], [1]), None, n - 1)
+        c.bacon_cache_store(bacon.BatchLayout([0, 1], [1]), [t[:1]], [t[:1]])
+        held.store(_np(t)[:1, 0])
+        at = 1
+        while at < n:
+            new = t[at:at + int(rng.integers(1, 30))]
+            c.bacon_cache_append(0, new[None], new[None])
+            held.append(_np(new)[:, 0])
+            at += len(new)
+    else:
+        c.bacon_cache_tables(bacon.BatchLayout([0, n], [n - 1]))
+        c.bacon_cache_store(bacon.BatchLayout([0, n], [n - 1]), [t], [t])
+        held.store(_np(t)[:, 0])
+    scales = c.scales.cpu().numpy()[c.table[0, 0, 0, :9].cpu().numpy()]
+    np.testing.assert_array_equal(scales, np.exp2(np.array(held.e, np.float64))[:, None].repeat(2, 1))
+    for got in c.bacon_cache_load(n):
+        np.testing.assert_array_equal(_np(got)[0, 0, 0], held.x)
+    assert c.bacon_cache_errors() == 0
