@@ -215,7 +215,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   // The workgroups of a unit's further query rows follow the first's eight
   // apart: on the same die (workgroups go to the eight in turn), whose L2 then
   // still holds the codes (it took 512 pairs of 64 query rows over 1K rows from
-  // 66 us to 58; they take 42 now).
+  // 66 us to 58; they take 44 now).
   int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z, row0 = 0;
   if (a.groups > 1) {
     const int eights = blockIdx.x >> 3, unit = eights / a.groups * 8 + (blockIdx.x & 7);
@@ -569,11 +569,16 @@ template <bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const int units = a.num_seqs * a.c.Hkv * a.splits;
   // Four waves, also where some have no tile (they share the queries and the
-  // join: one sequence over 1K rows in parts of 64 takes 7.4 us with four and
-  // with one); eight where one holds all of 17 to 32 query rows (a step of 64
-  // sequences of four drafted tokens 18.5 us, with four 19.1).  Elsewhere eight
-  // are slower (64 sequences over 300 to 993 rows 22.6 us, with four 17.2).
-  const int waves = NT == 2 && a.groups == 1 && a.chunk > 256 && max_waves(BF16, D, NT) == 8 ? 8 : 4;
+  // join: one sequence over 1K rows in parts of 64 takes 7.3 us with four and
+  // with one).  Eight for a step of 17 to 32 query rows over parts of more than
+  // 256, whose appending wave is late, as long as every workgroup has a compute
+  // unit of its own: 64 sequences of four drafted tokens, 256 pairs, take 18.5 us
+  // with eight and 19.2 with four; but 512 pairs of 700 rows 33.5 and 25.8 (a
+  // unit holds two workgroups of four waves), one of 400 rows 13.6 and 13.3.  Attends
+  // gain nothing (four sequences over 8K rows, 28 query rows, 15.7 and 14.6, eight
+  // over 16K 47.9 and 48.9; one query row, 64 over 300 to 993 rows, 22.8 and 17.2).
+  const bool late = a.k && NT == 2 && a.chunk > 256 && units <= 256;
+  const int waves = late && max_waves(BF16, D, NT) == 8 ? 8 : 4;
   if (hipError_t e = allow_lds<k_cache_attend<BF16, D, NT>>(attend_lds<BF16, D, NT>(waves))) return e;
   const dim3 grid = a.groups == 1 ? dim3(a.splits, a.c.Hkv, a.num_seqs) : dim3((units + 7) / 8 * 8 * a.groups);
   hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), grid, dim3(64 * waves), (attend_lds<BF16, D, NT>(waves)), s,
@@ -613,13 +618,13 @@ hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStre
   a.R = R;
   a.group_magic = (65536 + G - 1) / G;
   // 16 query rows a workgroup or 32: 32 share the codes' conversion, 16 are
-  // sooner done with a tile.  bf16, us with 16 and with 32: three sequences up
-  // to 70K rows (28/4 heads, five tokens) 56 and 49, four over 4K (64/8, eight
-  // tokens) 25 and 20, eight over 16K (32 query rows) 54 and 48; but 64 over 300
-  // to 993 rows (28) 15.0 and 16.2, one over 64 rows 5.5 and 6.9.  fp32, whose
-  // parts fill the registers: five tokens of four sequences 12.8 and 14.4.  A
-  // step of 17 to 32 query rows keeps them in the one workgroup that appends:
-  // two would not see each other's rows.
+  // sooner done with a tile.  Attends in bf16, us with 16 and with 32: three
+  // sequences up to 70K rows (28/4 heads, five tokens) 55.8 and 49.6, four over 4K
+  // (64/8, eight tokens) 25.3 and 20.4, eight over 16K (32 query rows) 56.1 and
+  // 48.9; but 64 over 300 to 993 rows (28 query rows) 15.4 and 16.1, one over 64 rows
+  // 5.5 and 7.0.  fp32, whose parts fill the registers: five tokens of four
+  // sequences 13.1 and 14.8.  A step of 17 to 32 query rows keeps them in the one
+  // workgroup that appends: two would not see each other's rows.
   const bool shared = bf16 && a.chunk > 256 && (R > 32 || a.chunk > 1024);
   const bool one = R <= 16 || !(a.k || shared);
   a.groups = (R + (one ? 15 : 31)) / (one ? 16 : 32);
