@@ -521,7 +521,7 @@ hipError_t launch_cache_store(const CacheStoreArgs &a, bool bf16, int head_dim, 
 }
 
 static int64_t load_groups_of_pair(int count, int head_dim) {
-  const int rows = 16 * 256 / (head_dim / 2);                // a workgroup's; the first may lie anywhere in a group of 16
+  const int rows = 16 * 256 / (head_dim / 2);                // a workgroup's; the first lies anywhere in a group of 16
   return (((int64_t)count + 15) / 16 * 16 + 16 + rows - 1) / rows;
 }
 

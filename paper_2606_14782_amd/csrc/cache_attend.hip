@@ -204,7 +204,7 @@ __device__ __forceinline__ void store_out(const CacheStepArgs &a, int64_t at, in
 template <bool BF16, int D, int NT>
 __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(CacheStepArgs a) {
   constexpr int QP = BF16 ? 1 : 3;     // parts of a query: bf16 is one; fp32 needs three for its 24 bits
-  constexpr int PP = BF16 ? 2 : 3;     // parts of a weight: one would add 2^-9 to a bf16 output's own 2^-9
+  constexpr int PP = BF16 ? 2 : 3;     // parts of a weight: one would add 2^-8 to a bf16 output's own 2^-8, two 2^-16
   constexpr int KS = D / 32;
   extern __shared__ __align__(16) char lds[];
   bf16x8 *q_lds = reinterpret_cast<bf16x8 *>(lds);           // [NT][KS][QP][64]
