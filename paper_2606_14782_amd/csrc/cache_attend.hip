@@ -185,8 +185,8 @@ __device__ __forceinline__ void raw_floats(const QRaw<BF16> &r, float (&x)[8]) {
 
 // Four dimensions of a query's output from their weighted sums (zeros where it
 // sees no row), its normaliser and its maximum.  A query that sees rows has a
-// normaliser of 1 at least, unless its logits are no numbers (a NaN or an
-// infinite one, or none above the least float): then all of it is NaN.
+// normaliser of 1 at least, unless its logits are no numbers (one NaN or
+// +infinity, or all -infinity): then all of it is NaN.
 template <bool BF16, int D>
 __device__ __forceinline__ void store_out(const CacheStepArgs &a, int64_t at, int dim, f32x4 acc, float l, float top) {
   const bool none = top == kNoRow;
