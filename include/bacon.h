@@ -348,18 +348,26 @@ typedef struct {
 bacon_status bacon_profile_enable(bacon_ctx *ctx, int32_t enable);
 int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
 
-/* ---- Decoding over the kept rows: a cache held in 8 bits -----------------
+/* ---- Decoding over the kept rows: a cache held in 8 or 4 bits ------------
  *
  * The rows that a prompt's compression keeps (bacon_select_topk, the fused
  * calls) move into blocks of block_tokens tokens of one (layer, sequence, KV
- * head) -- a pair below -- each with K and V in e4m3 and one scale for its K
- * and one for its V.  New tokens are appended there, and decoding attends over
- * them.
+ * head) -- a pair below.  New tokens are appended there, and decoding attends
+ * over them.  The format of a cache:
  *
+ * BACON_CACHE_E4M3: K and V in e4m3, one scale for a block's K and one for its V.
  *   scale of a block of rows X:  2^e, e the smallest integer with
  *       max |X| <= 448 2^e, held to -100 <= e <= 120 (max |X| = 0: e = -100)
  *   code of x:   x 2^-e rounded to the nearest e4m3 value, ties to even
  *   value held:  code 2^e
+ *
+ * BACON_CACHE_E2M1: K and V in e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their
+ * negatives), a scale for every 32 values of a row: 17 bytes for 32 values.
+ *   scale of 32 values X:  2^e, e the smallest integer with max |X| <= 6 2^e,
+ *       held to -100 <= e <= 125 (max |X| = 0: e = -100)
+ *   code of x:   x 2^-e rounded to the nearest e2m1 value, ties to even
+ *   value held:  code 2^e
+ * A row's codes depend on that row alone: an append rounds no old row again.
  *
  * A power of two changes no value's relative precision (e4m3 keeps 4 bits
  * whatever the scale, down to 2^-6 of it), its products are exact, the value
@@ -375,10 +383,17 @@ int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
  * Memory of a cache, at the byte offsets of bacon_cache_layout:
  *   lens, starts  [num_layers, max_batch, Hkv] int32
  *   table         [num_layers, max_batch, Hkv, max_blocks] int32
+ *   E4M3:
  *   scales        [num_blocks, 2] float32, K then V
  *   codes         [num_blocks, 2, block_tokens * d] e4m3 bytes: K as
  *                 [block_tokens, d], V in groups of 16 tokens, each
  *                 transposed: [block_tokens / 16, d, 16]
+ *   E2M1:
+ *   scales        [num_blocks, 2, block_tokens / 16, d / 32, 16] bytes e + 127,
+ *                 K then V: of 16 tokens for every 32 dimensions
+ *   codes         [num_blocks, 2, block_tokens * d / 2] bytes, byte i of a row
+ *                 the codes of dimensions 2 i (low half) and 2 i + 1: K as
+ *                 [block_tokens, d / 2], V as [block_tokens / 16, d / 2, 16]
  *   errors        one uint32 word
  *
  * Calls name the sequences first_seq .. first_seq + num_seqs - 1 (or + batch
@@ -392,6 +407,9 @@ int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
  * blocks, an append beyond the table, an id outside the pool (its rows count
  * as absent), an idx entry outside the candidates (its row is zero). */
 
+/* What a cache holds its K and V in. */
+typedef enum { BACON_CACHE_E4M3 = 0, BACON_CACHE_E2M1 = 1 } bacon_cache_format;
+
 typedef struct {
   int32_t num_layers;
   int32_t num_q_heads;
@@ -403,6 +421,7 @@ typedef struct {
   int32_t max_blocks;        /* table entries of a pair, >= 1                */
   int64_t num_blocks;        /* blocks of the pool, 1..2^31 - 1              */
   bacon_dtype dtype;         /* of K and V rows, queries and outputs         */
+  int32_t format;            /* BACON_CACHE_E4M3 (0) or BACON_CACHE_E2M1     */
 } bacon_cache_shape;
 
 typedef struct {
@@ -477,7 +496,7 @@ bacon_status bacon_cache_load(bacon_cache *cache, int32_t first_layer, int32_t n
  * apart (>= Hkv d, a multiple of 16 bytes; a view of a fused projection's
  * output will do).  d_counts [num_seqs] (int32, device, optional; held to
  * 0..tokens) gives each sequence's own number of new tokens.  Every pair's
- * length grows by that number.  In each block touched, e is the larger of the
+ * length grows by that number.  In E4M3, e of each block touched is the larger of the
  * old rows' (if the block has any) and of the one the new rows need; where it
  * grows the old codes are rounded again at it.  A pair without room (in its
  * table's blocks) is left as it is (NO_BLOCKS).  1 <= tokens <= 64. */
@@ -519,13 +538,127 @@ bacon_status bacon_cache_step(bacon_cache *cache, int32_t layer, int32_t first_s
 /* Moves lengths: every pair of the named layers and sequences by d_delta[b]
  * (int32, device, optional) or by delta, held to 0 .. max_blocks *
  * block_tokens.  A negative move takes back drafted tokens that were rejected
- * (a scale that grew for them stays). */
+ * (an E4M3 scale that grew for them stays). */
 bacon_status bacon_cache_advance(bacon_cache *cache, int32_t first_layer, int32_t num_layers,
                                  int32_t first_seq, int32_t num_seqs, int32_t delta, const int32_t *d_delta,
                                  void *stream);
 
 /* Waits for the device and returns the error word (-1 if it cannot be read). */
 int32_t bacon_cache_errors(bacon_cache *cache);
+
+/* ---- Positions ------------------------------------------------------------
+ *
+ * Rotary positions of queries and keys, as every other call here takes them.
+ * With r = rotary_dim, pair i < r / 2 of a head is (x_i, x_{i + r/2}) in
+ * BACON_ROTARY_HALF and (x_{2i}, x_{2i+1}) in BACON_ROTARY_PAIRS; dimensions
+ * past r pass as they are.  A token at position p turns its pair (a, b) by
+ * t = p f_i into m (a cos t - b sin t), m (b cos t + a sin t).
+ *
+ * Frequencies f_i and magnitude m, from w_i = base^(-2 i / r) and s = factor:
+ *   PLAIN   f_i = w_i, m = 1
+ *   LINEAR  f_i = w_i / s, m = 1 (positions interpolated)
+ *   NTK     f_i = w_i of the base base * s^(r / (r - 2)), m = 1 (r > 2)
+ *   YARN    f_i = (1 - g) w_i / s + g w_i, g = (n - beta_slow) / (beta_fast -
+ *           beta_slow) held to [0, 1], n = trained_tokens w_i / (2 pi) the turns
+ *           that the pair made in training; m = 0.1 ln s + 1 (Peng et al. 2023,
+ *           "YaRN: Efficient Context Window Extension of Large Language Models")
+ *   GIVEN   f_i = frequencies[i] (within +-1e6), m = 1
+ * magnitude > 0 replaces m.
+ *
+ * Angles are formed in 64 bits (a far position has no bits left in 32), the
+ * products in 32 bits, each output rounded once.  Positions are any int32;
+ * keys that are kept may so be moved by the difference of two positions.
+ *
+ * sections: all 0 for one row of positions [tokens]; otherwise they sum to r / 2
+ * and d_positions has three rows [3, tokens] (frame, row and column of an
+ * image's or video's token, alike for text): the first sections[0] pairs turn by
+ * the first row, the next sections[1] by the second, the others by the third.
+ *
+ * d_q_norm, d_k_norm (each optional, [d] of the dtype): heads are first
+ * normalised, x <- x / sqrt(mean x^2 + norm_eps) * weight. */
+typedef enum { BACON_ROTARY_HALF = 0, BACON_ROTARY_PAIRS = 1 } bacon_rotary_layout;
+typedef enum {
+  BACON_ROTARY_PLAIN = 0,
+  BACON_ROTARY_LINEAR = 1,
+  BACON_ROTARY_NTK = 2,
+  BACON_ROTARY_YARN = 3,
+  BACON_ROTARY_GIVEN = 4
+} bacon_rotary_scaling;
+
+typedef struct {
+  int32_t num_q_heads;       /* 1..4096 (of q, where it is given)            */
+  int32_t num_kv_heads;      /* 1..4096 (of k)                               */
+  int32_t head_dim;          /* 64 or 128                                    */
+  int32_t rotary_dim;        /* even, 2..head_dim                            */
+  int32_t layout;            /* bacon_rotary_layout                          */
+  int32_t sections[3];       /* each >= 0                                    */
+  int32_t scaling;           /* bacon_rotary_scaling                         */
+  int32_t trained_tokens;    /* YARN: >= 1                                   */
+  double base;               /* > 1                                          */
+  double factor;             /* >= 1; 1 in PLAIN                             */
+  double beta_fast;          /* YARN: > beta_slow > 0                        */
+  double beta_slow;
+  double magnitude;          /* 0: as above                                  */
+  double norm_eps;           /* >= 0                                         */
+  const double *frequencies; /* GIVEN: [rotary_dim / 2], host memory         */
+  bacon_dtype dtype;
+} bacon_rotary;
+
+/* Fills *r: one head of 128 dimensions in bfloat16, all of them turned, HALF,
+ * one row of positions, PLAIN, base 10000, factor 1, beta_fast 32, beta_slow 1,
+ * magnitude 0, norm_eps 1e-6. */
+void bacon_default_rotary(bacon_rotary *r);
+
+/* The frequencies f_i (radians a token, [rotary_dim / 2]) and the magnitude m
+ * that bacon_rotate uses; host work. */
+bacon_status bacon_rotary_frequencies(const bacon_rotary *r, double *frequencies, double *magnitude);
+
+/* Turns q and k of `tokens` tokens (0: nothing to do; at most 2^25).  d_q [tokens, Hq, d], its tokens q_stride
+ * elements apart (>= Hq d, a multiple of 16 bytes; a view of a fused projection's
+ * output will do), to d_q_out, q_out_stride apart; k likewise.  q or k may be
+ * NULL (then its output is too); an output may be its input (the same pointer
+ * and distance) and otherwise overlaps neither input. */
+bacon_status bacon_rotate(const bacon_rotary *r, int64_t tokens, const int32_t *d_positions, const void *d_q,
+                          int64_t q_stride, const void *d_k, int64_t k_stride, const void *d_q_norm,
+                          const void *d_k_norm, void *d_q_out, int64_t q_out_stride, void *d_k_out,
+                          int64_t k_out_stride, void *stream);
+
+/* ---- The prompt's attention -----------------------------------------------
+ *
+ * Causal attention of a ragged batch of prompts, or of their next chunks, with
+ * the window rows' normalisers that bacon_compress_layer_lse takes.  Of `shape`
+ * the heads, head_dim, window, max_batch (1..64), max_total_tokens (of the keys)
+ * and dtype count, without the compression's limit on G W.
+ * Sequence b has the N_b = cu_seqlens[b+1] - cu_seqlens[b] >= 0 keys of rows
+ * cu_seqlens[b] .. of d_k and d_v, and the M_b queries of rows cu_queries[b] .. of
+ * d_q: its last M_b tokens (cu_queries: host array [batch + 1] from 0, or NULL:
+ * cu_seqlens, every token a query).  Query j sees the keys i <= N_b - M_b + j:
+ *
+ *   out = softmax(q . k / sqrt(d)) v
+ *   lse = natural log of sum exp(q . k / sqrt(d)) over the keys seen
+ *
+ * A query that sees no key (M_b > N_b) gives zeros and -infinity.  Rows behind
+ * the last sequence are neither read nor written.  Rows are q_stride (k_stride,
+ * v_stride) elements apart (>= heads x d, a multiple of 16 bytes).  d_out
+ * [cu_queries[batch], Hq, d]; d_lse (optional) [cu_queries[batch], Hq] float32;
+ * d_window_lse (optional) [batch, Hq, W] float32: the lse of the queries that are
+ * the window's tokens (token N_b - W + w is entry w); entries whose token is not
+ * a query of this call are left as they were, so that chunks fill them in turn.
+ *
+ * Logits, maxima, sums and outputs are held in 32 bits.  In bfloat16 a weight
+ * enters the second product rounded to bfloat16 (2^-9 of itself at most, as much as
+ * the output's own rounding, and independent from key to key).  A query one of
+ * whose logits is NaN or +infinity, or whose logits are all -infinity, gives NaN;
+ * where K or V of a key that is seen is not finite, so are its queries' outputs.
+ * What lies in rows that no query sees reaches nothing.
+ * d_work: scratch of bacon_prompt_work_bytes (0: may be NULL), 256-byte aligned,
+ * of this call alone until its work is done.  The arrays of `batch` and
+ * cu_queries are read during the call.  budgets are not read (may be NULL). */
+bacon_status bacon_prompt_attend(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries,
+                                 const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride,
+                                 const void *d_v, int64_t v_stride, void *d_out, float *d_lse, float *d_window_lse,
+                                 void *d_work, size_t work_bytes, void *stream);
+size_t bacon_prompt_work_bytes(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries);
 
 const char *bacon_status_string(bacon_status s);
 const char *bacon_last_error(void);

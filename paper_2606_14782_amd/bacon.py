@@ -31,6 +31,8 @@ ENTRY_POINTS = [
     "bacon_cache_tables", "bacon_cache_store", "bacon_cache_load", "bacon_cache_append",
     "bacon_cache_attend", "bacon_cache_work_bytes", "bacon_cache_step", "bacon_cache_advance",
     "bacon_cache_errors",
+    "bacon_default_rotary", "bacon_rotary_frequencies", "bacon_rotate",
+    "bacon_prompt_attend", "bacon_prompt_work_bytes",
 ]
 
 
@@ -66,7 +68,7 @@ class CacheShape(C.Structure):
     _fields_ = [("num_layers", C.c_int32), ("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("window", C.c_int32), ("block_tokens", C.c_int32),
                 ("max_batch", C.c_int32), ("max_blocks", C.c_int32), ("num_blocks", C.c_int64),
-                ("dtype", C.c_int)]
+                ("dtype", C.c_int), ("format", C.c_int32)]
 
 
 class CacheOffsets(C.Structure):
@@ -75,6 +77,20 @@ class CacheOffsets(C.Structure):
                 ("total", C.c_size_t)]
 
 
+class RotaryParams(C.Structure):
+    _fields_ = [("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("sections", C.c_int32 * 3),
+                ("scaling", C.c_int32), ("trained_tokens", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("beta_fast", C.c_double), ("beta_slow", C.c_double),
+                ("magnitude", C.c_double), ("norm_eps", C.c_double),
+                ("frequencies", C.POINTER(C.c_double)), ("dtype", C.c_int)]
+
+
+# which dimensions are a pair (bacon_rotary_layout), and the frequencies (bacon_rotary_scaling)
+ROTARY_HALF, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_NTK, ROTARY_YARN, ROTARY_GIVEN = range(5)
+# what a cache holds its K and V in (bacon_cache_format)
+CACHE_E4M3, CACHE_E2M1 = 0, 1
 # bits of a cache's error word
 CACHE_NO_BLOCKS, CACHE_BAD_BLOCK, CACHE_BAD_INDEX = 1, 2, 4
 
@@ -144,6 +160,16 @@ def lib() -> C.CDLL:
         L.bacon_cache_advance.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp]
         L.bacon_cache_errors.argtypes = [vp]
         L.bacon_cache_errors.restype = i32
+        rot = C.POINTER(RotaryParams)
+        L.bacon_default_rotary.argtypes = [rot]
+        L.bacon_default_rotary.restype = None
+        L.bacon_rotary_frequencies.argtypes = [rot, vp, vp]
+        L.bacon_rotate.argtypes = [rot, i64, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+        L.bacon_prompt_attend.argtypes = [C.POINTER(Shape), cap, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, sz, vp]
+        L.bacon_prompt_work_bytes.argtypes = [C.POINTER(Shape), cap, vp]
+        L.bacon_prompt_work_bytes.restype = sz
+        for name in ("rotary_frequencies", "rotate", "prompt_attend"):
+            getattr(L, "bacon_" + name).restype = C.c_int
         for name in ("layout", "init", "free", "clear", "tables", "store", "load", "append", "attend",
                      "step", "advance"):
             getattr(L, "bacon_cache_" + name).restype = C.c_int
@@ -431,13 +457,194 @@ def bacon_window_lse(ctx: Context, batch, q_win, k, out=None):
     return ctx.bacon_window_lse(batch, q_win, k, out)
 
 
+def _tokens_at(t):
+    """Pointer, tokens and token distance of heads [.., H, d] that lie together,
+    or None where they do not, or the tokens are not evenly spaced."""
+    *lead, h, d = t.shape
+    *steps, sh, sd = t.stride()
+    n = 1
+    for x in lead:
+        n *= x
+    if n == 0:
+        return t.data_ptr(), 0, h * d
+    if d > 1 and sd != 1 or h > 1 and sh != d:
+        return None
+    step = run = None                             # the distance of tokens, and of a whole leading index
+    for size, stride in zip(reversed(lead), reversed(steps)):
+        if size == 1:
+            continue
+        if step is None:
+            step, run = stride, stride * size
+        elif stride != run:
+            return None
+        else:
+            run *= size
+    return t.data_ptr(), n, h * d if step is None else step
+
+
+class _Given:
+    """Checks and pointers of the tensors of one call, all on the first one's device."""
+
+    def __init__(self, like, dtype=None):
+        import torch
+        if not isinstance(like, torch.Tensor) or like.device.type != "cuda":
+            raise BaconError(ERR_INVALID, "tensors on a GPU are needed")
+        self.torch, self.device, self.dtype = torch, like.device, dtype or like.dtype
+
+    def rows(self, t, name, heads, head_dim, lead=None):
+        """Pointer, tokens and token distance of [.., heads, head_dim]."""
+        if t.dtype != self.dtype or t.device != self.device or t.dim() < 3 or t.shape[-2:] != (heads, head_dim):
+            raise BaconError(ERR_INVALID, f"{name} must be {self.dtype} [.., {heads}, {head_dim}] on {self.device}, "
+                                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if lead is not None and t.shape[:-2] != lead:
+            raise BaconError(ERR_INVALID, f"{name} has shape {tuple(t.shape)}, tokens {tuple(lead)} expected")
+        at = _tokens_at(t)
+        if at is None:
+            raise BaconError(ERR_INVALID, f"{name} has strides {t.stride()}: a token's heads lie together, tokens "
+                                          "evenly spaced")
+        return at
+
+    def whole(self, t, name, shape, dtype=None):
+        """The pointer of a contiguous tensor (None: NULL)."""
+        if t is None:
+            return None
+        dtype = dtype or self.dtype
+        if t.dtype != dtype or t.device != self.device or not t.is_contiguous() or shape is not None and t.shape != shape:
+            raise BaconError(ERR_INVALID, f"{name} must be a contiguous {dtype} tensor {shape and tuple(shape)} on "
+                                          f"{self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def call(self, fn, *args):
+        """fn on the tensors' device and that device's current stream."""
+        cuda = self.torch.cuda
+        if cuda.current_device() == self.device.index:
+            status = fn(*args, self.torch._C._cuda_getCurrentRawStream(self.device.index))
+        else:
+            with cuda.device(self.device):
+                status = fn(*args, self.torch._C._cuda_getCurrentRawStream(self.device.index))
+        if status:
+            _check(status)
+
+
+class Rotary:
+    """A bacon_rotary: how a model's queries and keys turn with their positions.
+
+    sections: three numbers of pairs for three rows of positions (None: one row);
+    frequencies: radians a token of every pair (with scaling ROTARY_GIVEN)."""
+
+    def __init__(self, num_q_heads, num_kv_heads, head_dim, dtype, rotary_dim=None, layout=ROTARY_HALF, sections=None,
+                 base=10000.0, scaling=ROTARY_PLAIN, factor=1.0, trained_tokens=0, beta_fast=32.0, beta_slow=1.0,
+                 magnitude=0.0, frequencies=None, norm_eps=1e-6):
+        import torch
+        if dtype not in ("bf16", "fp32", BF16, FP32, torch.bfloat16, torch.float32):
+            raise BaconError(ERR_UNSUPPORTED, f"dtype {dtype} is not supported (bf16 or fp32)")
+        self.torch_dtype = torch.bfloat16 if dtype in ("bf16", BF16, torch.bfloat16) else torch.float32
+        c = self.c = RotaryParams()
+        lib().bacon_default_rotary(C.byref(c))
+        c.num_q_heads, c.num_kv_heads, c.head_dim = num_q_heads, num_kv_heads, head_dim
+        c.rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        c.layout, c.scaling, c.trained_tokens = layout, scaling, trained_tokens
+        if sections is not None:
+            if len(sections) != 3:
+                raise BaconError(ERR_INVALID, f"three sections are needed, {len(sections)} given")
+            c.sections[:] = sections
+        c.base, c.factor, c.beta_fast, c.beta_slow = base, factor, beta_fast, beta_slow
+        c.magnitude, c.norm_eps = magnitude, norm_eps
+        c.dtype = BF16 if self.torch_dtype == torch.bfloat16 else FP32
+        self._given = None
+        if frequencies is not None:
+            self._given = np.ascontiguousarray(frequencies, dtype=np.float64)
+            if self._given.shape != (c.rotary_dim // 2,):
+                raise BaconError(ERR_INVALID, f"{self._given.shape} frequencies for {c.rotary_dim // 2} pairs")
+            c.frequencies = self._given.ctypes.data_as(C.POINTER(C.c_double))
+        self.sectioned = sections is not None and any(sections)
+        f = np.empty(max(c.rotary_dim // 2, 1), dtype=np.float64)
+        m = C.c_double()
+        _check(lib().bacon_rotary_frequencies(C.byref(c), f.ctypes.data, C.byref(m)))
+        self.frequencies, self.magnitude = f, m.value
+
+
+def bacon_rotate(rotary: Rotary, positions, q=None, k=None, q_norm=None, k_norm=None, q_out=None, k_out=None):
+    """Turns q [.., Hq, d] and k [.., Hkv, d] (either may be None), whose leading
+    dimensions are the tokens, by positions (int32, [..], or [3, ..] with
+    sections); heads are normalised first where a weight [d] is given.  Outputs
+    may be the inputs.  Returns (q_out, k_out)."""
+    first = q if q is not None else k
+    if first is None:
+        raise BaconError(ERR_INVALID, "q and k are None")
+    g, c = _Given(first, rotary.torch_dtype), rotary.c
+    lead = first.shape[:-2]
+    args, outs, n = [], [], 0
+    for x, y, heads, name in ((q, q_out, c.num_q_heads, "q"), (k, k_out, c.num_kv_heads, "k")):
+        if x is None:
+            if y is not None:
+                raise BaconError(ERR_INVALID, f"{name}_out without {name}")
+            args.append((None, 0, None, 0))
+        else:
+            p, n, step = g.rows(x, name, heads, c.head_dim, lead)
+            if y is None:
+                y = x.new_empty(x.shape)
+            to, _, to_step = g.rows(y, name + "_out", heads, c.head_dim, lead)
+            args.append((p, step, to, to_step))
+        outs.append(y)
+    d = (c.head_dim,)
+    pos = g.whole(positions, "positions", (3, *lead) if rotary.sectioned else lead, g.torch.int32)
+    (qp, qs, qo, qos), (kp, ks, ko, kos) = args
+    g.call(lib().bacon_rotate, C.byref(c), n, pos, qp, qs, kp, ks, g.whole(q_norm, "q_norm", d),
+           g.whole(k_norm, "k_norm", d), qo, qos, ko, kos)
+    return tuple(outs)
+
+
+def bacon_prompt_attend(shape: Shape, batch: BatchLayout, q, k, v, queries=None, want_lse=False,
+                        want_window_lse=False, out=None, lse=None, window_lse=None, work=None):
+    """Causal attention of a ragged batch of prompts: q [Tq, Hq, d] over k, v [T,
+    Hkv, d] (views of one projection's output will do).  queries: the cumulative
+    numbers of queries [batch + 1] where they are the prompts' last tokens only.
+    Returns (out [Tq, Hq, d], lse [Tq, Hq] or None, window_lse [batch, Hq, W] or
+    None); entries of a given window_lse whose token is no query stay."""
+    g = _Given(q)
+    torch, hq, hkv, d = g.torch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim
+    g.dtype = torch.bfloat16 if shape.dtype == BF16 else torch.float32
+    cuq = None
+    if queries is not None:
+        cuq = np.ascontiguousarray(queries, dtype=np.int32)
+        if cuq.shape != batch.cu.shape:
+            raise BaconError(ERR_INVALID, f"queries has shape {cuq.shape}, {batch.cu.shape} expected")
+    n, total = int(batch.cu[-1] if cuq is None else cuq[-1]), int(batch.cu[-1])
+    qp, qn, qs = g.rows(q, "q", hq, d)
+    kp, kn, ks = g.rows(k, "k", hkv, d)
+    vp, vn, vs = g.rows(v, "v", hkv, d)
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or qn < n or kn < total or vn < total:
+        raise BaconError(ERR_INVALID, f"q, k, v have shapes {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)} for "
+                                      f"{n} queries of {total} tokens")
+    if out is None:
+        out = q.new_empty((n, hq, d))
+    if lse is None and want_lse:
+        lse = q.new_empty((n, hq), dtype=torch.float32)
+    seqs = len(batch.cu) - 1
+    if window_lse is None and want_window_lse:
+        window_lse = q.new_empty((seqs, hq, shape.window), dtype=torch.float32)
+    outp = g.whole(out, "out", (n, hq, d))
+    lsep = g.whole(lse, "lse", (n, hq), torch.float32)
+    winp = g.whole(window_lse, "window_lse", (seqs, hq, shape.window), torch.float32)
+    cup = None if cuq is None else cuq.ctypes.data
+    need = lib().bacon_prompt_work_bytes(C.byref(shape), C.byref(batch.c), cup)
+    if need and work is None:
+        work = q.new_empty(need, dtype=torch.uint8)
+    workp = g.whole(work, "work", None, torch.uint8)
+    g.call(lib().bacon_prompt_attend, C.byref(shape), C.byref(batch.c), cup, qp, qs, kp, ks, vp, vs, outp, lsep, winp,
+           workp, 0 if work is None else work.numel())
+    return out, lse, window_lse
+
+
 class Cache:
-    """A bacon_cache: the kept rows of a model's layers in 8 bits, with its
+    """A bacon_cache: the kept rows of a model's layers in 8 or 4 bits, with its
     memory on `device`.
 
     lens, starts [num_layers, max_batch, Hkv] and table [.., max_blocks]
-    (int32), scales [num_blocks, 2] (float32) and codes [num_blocks, 2,
-    block_tokens * d] (uint8, e4m3) are views of that memory.  max_tokens: the
+    (int32), scales and codes are views of that memory: for format "e4m3" [num_blocks, 2]
+    (float32) and [num_blocks, 2, block_tokens * d] (uint8), for "e2m1" [num_blocks, 2,
+    block_tokens / 16, d / 32, 16] and [num_blocks, 2, block_tokens * d / 2] (both uint8).  max_tokens: the
     longest a pair may become.  Tensors given to the calls are on the cache's
     device; every call runs on that device's current stream.  New tokens and
     queries may be views of one projection's output: only the heads of a token
@@ -445,8 +652,11 @@ class Cache:
     """
 
     def __init__(self, num_layers, num_q_heads, num_kv_heads, head_dim, window, block_tokens, max_batch,
-                 max_tokens, num_blocks, dtype, device="cuda"):
+                 max_tokens, num_blocks, dtype, device="cuda", format="e4m3"):
         import torch
+        formats = {"e4m3": CACHE_E4M3, CACHE_E4M3: CACHE_E4M3, "e2m1": CACHE_E2M1, CACHE_E2M1: CACHE_E2M1}
+        if format not in formats:
+            raise BaconError(ERR_UNSUPPORTED, f"format {format} is not supported (e4m3 or e2m1)")
         if block_tokens < 1:
             raise BaconError(ERR_INVALID, "block_tokens must be >= 1")
         if dtype not in ("bf16", "fp32", BF16, FP32, torch.bfloat16, torch.float32):
@@ -454,7 +664,7 @@ class Cache:
         bf16 = dtype in ("bf16", BF16, torch.bfloat16)
         blocks = (max_tokens + block_tokens - 1) // block_tokens
         self.shape = CacheShape(num_layers, num_q_heads, num_kv_heads, head_dim, window, block_tokens,
-                                max_batch, blocks, num_blocks, BF16 if bf16 else FP32)
+                                max_batch, blocks, num_blocks, BF16 if bf16 else FP32, formats[format])
         off = CacheOffsets()
         _check(lib().bacon_cache_layout(C.byref(self.shape), C.byref(off)))
         self._torch, self._L = torch, lib()
@@ -479,8 +689,12 @@ class Cache:
         self.lens = part(off.lens, torch.int32, *pairs)
         self.starts = part(off.starts, torch.int32, *pairs)
         self.table = part(off.table, torch.int32, *pairs, blocks)
-        self.scales = part(off.scales, torch.float32, num_blocks, 2)
-        self.codes = part(off.codes, torch.uint8, num_blocks, 2, block_tokens * head_dim)
+        if self.shape.format == CACHE_E2M1:
+            self.scales = part(off.scales, torch.uint8, num_blocks, 2, block_tokens // 16, head_dim // 32, 16)
+            self.codes = part(off.codes, torch.uint8, num_blocks, 2, block_tokens * head_dim // 2)
+        else:
+            self.scales = part(off.scales, torch.float32, num_blocks, 2)
+            self.codes = part(off.codes, torch.uint8, num_blocks, 2, block_tokens * head_dim)
 
     def __del__(self):
         h = getattr(self, "_h", None)

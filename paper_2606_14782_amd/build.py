@@ -10,7 +10,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbacon.so")
-SOURCES = ["kernels.hip", "noalloc.hip", "cache.hip", "cache_attend.hip", "api.cpp", "cache_api.cpp"]
+SOURCES = ["kernels.hip", "noalloc.hip", "cache.hip", "cache4.hip", "cache_attend.hip", "prompt.hip", "rotary.hip",
+           "api.cpp", "cache_api.cpp", "prompt_api.cpp", "rotary_api.cpp"]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -21,8 +22,9 @@ HIP_FLAGS = [
     "-fno-honor-nans",
     "-Wall", "-Wno-unused-result",
 ]
-# attention over the cache hands a NaN on to the outputs of its query
-SOURCE_FLAGS = {"cache_attend.hip": ["-fhonor-nans"]}
+# attention hands a NaN on to the outputs of its query, a rotation passes one as it is
+# (and its host side refuses NaN in its numbers)
+SOURCE_FLAGS = {s: ["-fhonor-nans"] for s in ("cache_attend.hip", "prompt.hip", "rotary.hip", "rotary_api.cpp")}
 
 
 def hipcc() -> str:

@@ -1,4 +1,4 @@
-// Declarations shared by the kernels of the 8-bit cache and its host API.
+// Declarations shared by the kernels of the cache (8 or 4 bits) and its host API.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -7,6 +7,7 @@
 namespace bacon {
 
 constexpr int kCacheLow = -100, kCacheHigh = 120;   // exponents a block's scale may take
+constexpr int kCache4High = 125;                    // in e2m1 (from kCacheLow on)
 constexpr int kCacheMaxBatch = 64;
 constexpr int kCacheMaxHeads = 1024;               // KV heads
 constexpr int kCacheMaxTokens = 64;                 // new tokens of one call
@@ -19,8 +20,10 @@ struct CacheDev {
   int bt_log;              // log2 of the tokens of a block
   int max_blocks;
   int num_blocks;
+  int format;              // BACON_CACHE_E4M3 or _E2M1
   int32_t *lens, *starts, *table;
-  float *scales;
+  float *scales;           // e4m3
+  uint8_t *scales4;        // e2m1, at the same place
   uint8_t *codes;
   unsigned *err;
 };
@@ -111,6 +114,11 @@ hipError_t launch_cache_append(const CacheStepArgs &a, bool bf16, int head_dim, 
 // (a.k not NULL); otherwise one workgroup would read rows that another writes.
 bool cache_appends(int q_rows);
 hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStream_t s);
+// The same calls' kernels for e2m1 (the divisions are the same).
+hipError_t launch_cache4_store(const CacheStoreArgs &a, bool bf16, int head_dim, dim3 grid, hipStream_t s);
+hipError_t launch_cache4_load(const CacheLoadArgs &a, bool bf16, int head_dim, dim3 grid, unsigned per_pair,
+                              hipStream_t s);
+hipError_t launch_cache4_append(const CacheStepArgs &a, bool bf16, int head_dim, hipStream_t s);
 hipError_t launch_cache_advance(const CacheMoveArgs &a, hipStream_t s);
 
 }  // namespace bacon

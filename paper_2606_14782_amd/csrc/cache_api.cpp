@@ -1,4 +1,4 @@
-// Host side of the 8-bit cache declared in include/bacon.h: argument checks,
+// Host side of the cache declared in include/bacon.h: argument checks,
 // the layout of its memory and launches.
 #include <hip/hip_runtime.h>
 
@@ -58,6 +58,8 @@ bacon_status check_shape(const bacon_cache_shape *s) {
                 kCacheMaxQRows);
   if (s->num_kv_heads > kCacheMaxHeads)
     return fail(BACON_ERR_UNSUPPORTED, "%d KV heads exceed %d", s->num_kv_heads, kCacheMaxHeads);
+  if (s->format != BACON_CACHE_E4M3 && s->format != BACON_CACHE_E2M1)
+    return fail(BACON_ERR_UNSUPPORTED, "format %d is not supported", s->format);
   if (s->num_blocks > 0x7FFFFFFF) return fail(BACON_ERR_UNSUPPORTED, "num_blocks too large");
   if ((int64_t)s->max_blocks * s->block_tokens > (1 << 30))
     return fail(BACON_ERR_UNSUPPORTED, "a pair's %d blocks of %d tokens exceed 2^30 tokens", s->max_blocks,
@@ -71,7 +73,13 @@ int64_t pairs_of(const bacon_cache_shape *s) {
   return (int64_t)s->num_layers * s->max_batch * s->num_kv_heads;
 }
 
-int64_t block_bytes(const bacon_cache_shape *s) { return 2LL * s->block_tokens * s->head_dim; }
+// Bytes of a block's codes and of its scales.
+int64_t block_bytes(const bacon_cache_shape *s) {
+  return 2LL * s->block_tokens * s->head_dim / (s->format == BACON_CACHE_E2M1 ? 2 : 1);
+}
+int64_t scale_bytes(const bacon_cache_shape *s) {
+  return s->format == BACON_CACHE_E2M1 ? 2LL * s->block_tokens * s->head_dim / 32 : 8;
+}
 
 bacon_cache_offsets layout_of(const bacon_cache_shape *s) {
   bacon_cache_offsets o{};
@@ -81,7 +89,7 @@ bacon_cache_offsets layout_of(const bacon_cache_shape *s) {
   o.lens = at;   at += align256(pairs * 4);
   o.starts = at; at += align256(pairs * 4);
   o.table = at;  at += align256(pairs * s->max_blocks * 4);
-  o.scales = at; at += align256((size_t)s->num_blocks * 8);
+  o.scales = at; at += align256((size_t)(s->num_blocks * scale_bytes(s)));
   o.codes = at;  at += align256((size_t)(s->num_blocks * block_bytes(s)));
   o.total = at;
   return o;
@@ -98,10 +106,12 @@ CacheDev device_of(const bacon_cache *c) {
   d.bt_log = s.block_tokens == 16 ? 4 : s.block_tokens == 32 ? 5 : 6;
   d.max_blocks = s.max_blocks;
   d.num_blocks = (int)s.num_blocks;
+  d.format = s.format;
   d.lens = reinterpret_cast<int32_t *>(c->mem + c->off.lens);
   d.starts = reinterpret_cast<int32_t *>(c->mem + c->off.starts);
   d.table = reinterpret_cast<int32_t *>(c->mem + c->off.table);
   d.scales = reinterpret_cast<float *>(c->mem + c->off.scales);
+  d.scales4 = reinterpret_cast<uint8_t *>(c->mem + c->off.scales);
   d.codes = reinterpret_cast<uint8_t *>(c->mem + c->off.codes);
   d.err = reinterpret_cast<unsigned *>(c->mem + c->off.errors);
   return d;

@@ -1,4 +1,4 @@
-// Attention over the 8-bit cache on gfx950.
+// Attention over the cache on gfx950.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -26,15 +26,30 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // second product, without an exchange between lanes, and V's 16-byte groups
 // are read in that order.  The codes become bf16 in registers, exactly, the
 // block's scale applied by the conversion.
-template <int D>
+//
+// In e2m1 row 16 g + 4 i + t of the tile is M index 4 g + i of step t, so that
+// the four rows a lane loads K of are neighbours and their scales a word; a
+// 16-byte load of a K row is 32 dimensions (of d 64, 8 bytes are 16), one scale;
+// V's bytes are two dimensions of a row, and are paired by rows after the
+// conversion, each row's scale applied in it.
+template <int FMT, int D>
 struct KTile {
   u32x4 w[4][D / 64];
   float scale;
 };
-template <int D>
+template <int FMT, int D>
 struct VTile {
   u32x4 w[D / 16];
   float scale;
+};
+template <int D>
+struct KTile<BACON_CACHE_E2M1, D> {
+  uint32_t w[4][D / 32];     // row, step of 32 dimensions
+  unsigned scales;           // of the four rows
+};
+template <int D>
+struct VTile<BACON_CACHE_E2M1, D> {
+  u32x4 w[D / 32], scales[D / 32];
 };
 
 // Block ids of a tile: of the rows this lane loads K of (group (lane & 15) >> 2)
@@ -56,27 +71,57 @@ __device__ __forceinline__ TileIds bound_ids(TileIds t, int base, int to) {
 }
 
 // (An absent block's rows are masked: any address of the pool will do.)
-template <int D>
-__device__ __forceinline__ void load_k(const CacheDev &c, int id, int base, KTile<D> &x) {
+template <int FMT, int D>
+__device__ __forceinline__ void load_k(const CacheDev &c, int id, int base, KTile<FMT, D> &x) {
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int i = (unsigned)id < (unsigned)c.num_blocks ? id : 0;
-  const int r = ((base + 16 * (m >> 2)) & ((1 << c.bt_log) - 1)) + (m & 3);
-  const uint8_t *p = block_codes<D>(c, i, 0) + r * D + 16 * g;
-  x.scale = c.scales[(int64_t)i * 2];
+  if constexpr (FMT == BACON_CACHE_E2M1) {
+    const int r = ((base + 16 * (m >> 2)) & ((1 << c.bt_log) - 1)) + 4 * (m & 3);
+    const uint8_t *p = block_codes<D / 2>(c, i, 0) + r * (D / 2) + g * (D / 8);
+    const int group = D == 128 ? g : g >> 1;
+    x.scales = *reinterpret_cast<const unsigned *>(block_scales4<D>(c, i, 0, r >> 4, group) + (r & 15));
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t) {
+      if constexpr (D == 128) {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(p + t * (D / 2));
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) x.w[t][j] = *reinterpret_cast<const u32x4 *>(p + 4 * t * D + 64 * j);
+        for (int j = 0; j < 4; ++j) x.w[t][j] = w[j];
+      } else {
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(p + t * (D / 2));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) x.w[t][j] = w[j];
+      }
+    }
+  } else {
+    const int r = ((base + 16 * (m >> 2)) & ((1 << c.bt_log) - 1)) + (m & 3);
+    const uint8_t *p = block_codes<D>(c, i, 0) + r * D + 16 * g;
+    x.scale = c.scales[(int64_t)i * 2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j) x.w[t][j] = *reinterpret_cast<const u32x4 *>(p + 4 * t * D + 64 * j);
+  }
 }
 
-template <int D>
-__device__ __forceinline__ void load_v(const CacheDev &c, int id, int base, VTile<D> &x) {
+template <int FMT, int D>
+__device__ __forceinline__ void load_v(const CacheDev &c, int id, int base, VTile<FMT, D> &x) {
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int i = (unsigned)id < (unsigned)c.num_blocks ? id : 0;
-  const uint8_t *p = block_codes<D>(c, i, 1) + ((base + 16 * g) & ((1 << c.bt_log) - 1)) * D + 16 * m;
-  x.scale = c.scales[(int64_t)i * 2 + 1];
+  if constexpr (FMT == BACON_CACHE_E2M1) {
+    const int r = (base + 16 * g) & ((1 << c.bt_log) - 1);
+    const uint8_t *p = block_codes<D / 2>(c, i, 1) + r * (D / 2) + 16 * m;
+    const uint8_t *s = block_scales4<D>(c, i, 1, r >> 4, 0);
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) x.w[e] = *reinterpret_cast<const u32x4 *>(p + 256 * e);
+    for (int e = 0; e < D / 32; ++e) {
+      x.w[e] = *reinterpret_cast<const u32x4 *>(p + 256 * e);
+      x.scales[e] = *reinterpret_cast<const u32x4 *>(s + 16 * e);
+    }
+  } else {
+    const uint8_t *p = block_codes<D>(c, i, 1) + ((base + 16 * g) & ((1 << c.bt_log) - 1)) * D + 16 * m;
+    x.scale = c.scales[(int64_t)i * 2 + 1];
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) x.w[e] = *reinterpret_cast<const u32x4 *>(p + 256 * e);
+  }
 }
 
 // Eight codes as bf16 values times the scale (exact).
@@ -89,6 +134,37 @@ __device__ __forceinline__ bf16x8 dequant(unsigned lo, unsigned hi, float scale)
   r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1];
   r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
   return r;
+}
+
+// The same of eight e2m1 codes of one row.
+__device__ __forceinline__ bf16x8 dequant4(unsigned w, float scale) {
+  bf16x8 r;
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1];
+  r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
+  return r;
+}
+
+// Eight rows' bytes of two neighbouring dimensions, each row with its own
+// scale: the even dimension's and the odd one's bf16 values.
+__device__ __forceinline__ void dequant_rows4(const unsigned *w, const unsigned *s, bf16x8 (&v)[2]) {
+  u32x4 even, odd;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const unsigned r0 = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], scale4(s[i], 0), 0));
+    const unsigned r1 = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], scale4(s[i], 1), 1));
+    const unsigned r2 = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], scale4(s[i], 2), 2));
+    const unsigned r3 = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], scale4(s[i], 3), 3));
+    even[2 * i] = __builtin_amdgcn_perm(r1, r0, 0x05040100);
+    odd[2 * i] = __builtin_amdgcn_perm(r1, r0, 0x07060302);
+    even[2 * i + 1] = __builtin_amdgcn_perm(r3, r2, 0x05040100);
+    odd[2 * i + 1] = __builtin_amdgcn_perm(r3, r2, 0x07060302);
+  }
+  v[0] = __builtin_bit_cast(bf16x8, even);
+  v[1] = __builtin_bit_cast(bf16x8, odd);
 }
 
 // Eight floats as NP bf16 parts whose sum they are, to 8 bits more a part: all
@@ -201,7 +277,14 @@ __device__ __forceinline__ void store_out(const CacheStepArgs &a, int64_t at, in
   if (dim == 0 && a.lse) a.lse[at] = none ? -INFINITY : (top + __log2f(l)) * kLn2f;
 }
 
-template <bool BF16, int D, int NT>
+// The dimension of a query's element e of step s (of 32) and group g: as K's
+// codes lie in their loads.
+template <int FMT, int D>
+__device__ __forceinline__ int q_dim(int s, int g) {
+  return FMT == BACON_CACHE_E2M1 ? g * (D / 4) + 8 * s : 64 * (s >> 1) + 16 * g + 8 * (s & 1);
+}
+
+template <int FMT, bool BF16, int D, int NT>
 __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(CacheStepArgs a) {
   constexpr int QP = BF16 ? 1 : 3;     // parts of a query: bf16 is one; fp32 needs three for its 24 bits
   constexpr int PP = BF16 ? 2 : 3;     // parts of a weight: one would add 2^-8 to a bf16 output's own 2^-8, two 2^-16
@@ -234,7 +317,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
 #pragma unroll
   for (int u = 0; u < QI; ++u) {
     const int i = wave + u * waves, nt = i / KS, s = i - nt * KS, r = row0 + nt * 16 + m;
-    const int j = token_of(a, r), dim = 64 * (s >> 1) + 16 * g + 8 * (s & 1);
+    const int j = token_of(a, r), dim = q_dim<FMT, D>(s, g);
     q_raw[u] = QRaw<BF16>{};
     if (i < NT * KS && r < R)
       q_raw[u] = load_raw<BF16>(a.q, ((int64_t)b * a.tokens + j) * a.q_stride + (h * G + r - j * G) * D + dim);
@@ -265,8 +348,8 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
 
   // the first tile's codes, asked for before the queries are formed
   int base = from + 64 * wave;
-  KTile<D> kt;
-  VTile<D> vt;
+  KTile<FMT, D> kt;
+  VTile<FMT, D> vt;
   if (base != guess) {
     id0 = any_ids(c, row, base);
     id1 = any_ids(c, row, base + step);
@@ -275,8 +358,8 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   TileIds ids = bound_ids(id0, base, to);
   const bool late = grow && base + 64 > fresh.b0 << c.bt_log;
   if (base < to && !late) {
-    load_k<D>(c, ids.k, base, kt);
-    load_v<D>(c, ids.v, base, vt);
+    load_k<FMT, D>(c, ids.k, base, kt);
+    load_v<FMT, D>(c, ids.v, base, vt);
   }
   // (taken to be waited for here: nothing in the loop then waits for them)
   asm volatile("" : "+v"(id1.k), "+v"(id1.v));
@@ -304,15 +387,20 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
   if (grow) {
     for (int i = fresh.b0; i <= fresh.b1; ++i) {
       const int at = (i << c.bt_log & ~63) - from;
-      if (at >= 0 && at < to - from && (at >> 6) % waves == wave) append_block<BF16, D>(a, pair, fresh, i);
+      if (at >= 0 && at < to - from && (at >> 6) % waves == wave) {
+        if constexpr (FMT == BACON_CACHE_E2M1)
+          append_block4<BF16, D>(a, pair, fresh, i);
+        else
+          append_block<BF16, D>(a, pair, fresh, i);
+      }
     }
     // (a wave's loads follow its stores through the unit's L1 in order: the
     // fence keeps the compiler to that and waits for nothing)
     __threadfence_block();
   }
   if (base < to && late) {
-    load_k<D>(c, ids.k, base, kt);
-    load_v<D>(c, ids.v, base, vt);
+    load_k<FMT, D>(c, ids.k, base, kt);
+    load_v<FMT, D>(c, ids.v, base, vt);
   }
 
   f32x4 o[NT][D / 16];
@@ -344,8 +432,12 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     for (int k = 0; k < KS; ++k) {
       bf16x8 kk[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        kk[i] = dequant(kt.w[i][k >> 1][2 * (k & 1)], kt.w[i][k >> 1][2 * (k & 1) + 1], kt.scale);
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (FMT == BACON_CACHE_E2M1)
+          kk[i] = dequant4(kt.w[i][k], scale4(kt.scales, i));
+        else
+          kk[i] = dequant(kt.w[i][k >> 1][2 * (k & 1)], kt.w[i][k >> 1][2 * (k & 1) + 1], kt.scale);
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -357,7 +449,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     }
     const TileIds next = bound_ids(id1, base + step, to);
     id1 = any_ids(c, row, base + 2 * step);
-    load_k<D>(c, next.k, base + step, kt);
+    load_k<FMT, D>(c, next.k, base + step, kt);
     bf16x8 w[NT][2][PP];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -368,7 +460,7 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (4 * i + e >= n) s[nt][i][e] = -INFINITY;
+            if ((FMT == BACON_CACHE_E2M1 ? 4 * e + i : 4 * i + e) >= n) s[nt][i][e] = -INFINITY;
       } else {
         seen[nt] = 1;
       }
@@ -396,7 +488,8 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
         float x8[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x8[e] = __builtin_amdgcn_exp2f(minus(s[nt][2 * u + (e >> 2)][e & 3], mx[nt]));
+          const int hi = 2 * u + (e >> 2), lo = e & 3;       // row 8 u + e of the lane's 16
+          x8[e] = __builtin_amdgcn_exp2f(minus(FMT == BACON_CACHE_E2M1 ? s[nt][lo][hi] : s[nt][hi][lo], mx[nt]));
           sum[nt] += x8[e];
         }
         split8<PP>(x8, w[nt][u]);
@@ -406,27 +499,56 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
       // rows that hold nothing: their codes may be any bytes
       const int n = here ? total - (base + 16 * g) : 0;
       if (!here && base + 16 * g < total) atomicOr(c.err, (unsigned)BACON_CACHE_BAD_BLOCK);
-      if (n <= 0) vt.scale = 1.f;
+      if constexpr (FMT != BACON_CACHE_E2M1) {
+        if (n <= 0) vt.scale = 1.f;
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int left = n - 4 * i;
         const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+        if constexpr (FMT == BACON_CACHE_E2M1) {
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) vt.w[e][i] &= keep;
+          for (int e = 0; e < D / 32; ++e) {
+            vt.w[e][i] &= keep;
+            vt.scales[e][i] = (vt.scales[e][i] & keep) | (0x7F7F7F7Fu & ~keep);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < D / 16; ++e) vt.w[e][i] &= keep;
+        }
       }
     }
+    if constexpr (FMT == BACON_CACHE_E2M1) {
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e)
+      for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bf16x8 vv = dequant(vt.w[e][2 * u], vt.w[e][2 * u + 1], vt.scale);
+        for (int u = 0; u < 2; ++u) {
+          const unsigned codes[2] = {vt.w[e][2 * u], vt.w[e][2 * u + 1]};
+          const unsigned scales[2] = {vt.scales[e][2 * u], vt.scales[e][2 * u + 1]};
+          bf16x8 vv[2];
+          dequant_rows4(codes, scales, vv);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int p = 0; p < PP; ++p) o[nt][e] = mfma(vv, w[nt][u][p], o[nt][e]);
-      }
+            for (int p = 0; p < PP; ++p) {
+              o[nt][2 * e] = mfma(vv[0], w[nt][u][p], o[nt][2 * e]);
+              o[nt][2 * e + 1] = mfma(vv[1], w[nt][u][p], o[nt][2 * e + 1]);
+            }
+        }
+    } else {
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 vv = dequant(vt.w[e][2 * u], vt.w[e][2 * u + 1], vt.scale);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int p = 0; p < PP; ++p) o[nt][e] = mfma(vv, w[nt][u][p], o[nt][e]);
+        }
+    }
     ids = next;
-    load_v<D>(c, ids.v, base + step, vt);
+    load_v<FMT, D>(c, ids.v, base + step, vt);
   }
 
   // Join the waves through LDS, all query rows at once.
@@ -443,7 +565,16 @@ __global__ __launch_bounds__(64 * max_waves(BF16, D, NT)) void k_cache_attend(Ca
     if (row0 + n >= R) continue;
     if (g == 0) *reinterpret_cast<float2 *>(ml + at * 2) = make_float2(any ? mx[nt] : kNoRow, l);
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4 *>(oo + at * P + 16 * e + 4 * g) = o[nt][e];
+    for (int e = 0; e < D / 16; ++e) {
+      if constexpr (FMT == BACON_CACHE_E2M1) {               // two tiles' dimensions in turn
+        const f32x4 a0 = o[nt][e & ~1], a1 = o[nt][e | 1];
+        const int i = 2 * (e & 1);
+        *reinterpret_cast<f32x4 *>(oo + at * P + 32 * (e >> 1) + 8 * g + 4 * (e & 1)) =
+            f32x4{a0[i], a1[i], a0[i + 1], a1[i + 1]};
+      } else {
+        *reinterpret_cast<f32x4 *>(oo + at * P + 16 * e + 4 * g) = o[nt][e];
+      }
+    }
   }
   lds_barrier();
   // every wave has read the old length
@@ -565,7 +696,7 @@ constexpr int attend_lds(int waves) {
   return q > o ? q : o;
 }
 
-template <bool BF16, int D, int NT>
+template <int FMT, bool BF16, int D, int NT>
 hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   const int units = a.num_seqs * a.c.Hkv * a.splits;
   // Four waves, also where some have no tile (they share the queries and the
@@ -579,9 +710,9 @@ hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   // over 16K 47.9 and 48.9; one query row, 64 over 300 to 993 rows, 22.8 and 17.2).
   const bool late = a.k && NT == 2 && a.chunk > 256 && units <= 256;
   const int waves = late && max_waves(BF16, D, NT) == 8 ? 8 : 4;
-  if (hipError_t e = allow_lds<k_cache_attend<BF16, D, NT>>(attend_lds<BF16, D, NT>(waves))) return e;
+  if (hipError_t e = allow_lds<k_cache_attend<FMT, BF16, D, NT>>(attend_lds<BF16, D, NT>(waves))) return e;
   const dim3 grid = a.groups == 1 ? dim3(a.splits, a.c.Hkv, a.num_seqs) : dim3((units + 7) / 8 * 8 * a.groups);
-  hipLaunchKernelGGL((k_cache_attend<BF16, D, NT>), grid, dim3(64 * waves), (attend_lds<BF16, D, NT>(waves)), s,
+  hipLaunchKernelGGL((k_cache_attend<FMT, BF16, D, NT>), grid, dim3(64 * waves), (attend_lds<BF16, D, NT>(waves)), s,
                      a);
   if (a.splits > 1) hipLaunchKernelGGL((k_cache_join<BF16, D>), dim3(a.R, a.c.Hkv, a.num_seqs), dim3(256), 0, s, a);
   return hipGetLastError();
@@ -628,11 +759,15 @@ hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStre
   const bool shared = bf16 && a.chunk > 256 && (R > 32 || a.chunk > 1024);
   const bool one = R <= 16 || !(a.k || shared);
   a.groups = (R + (one ? 15 : 31)) / (one ? 16 : 32);
-#define ATTEND(nt)                                                                                \
-  return bf16 ? (head_dim == 128 ? attend<true, 128, nt>(a, s) : attend<true, 64, nt>(a, s))      \
-              : (head_dim == 128 ? attend<false, 128, nt>(a, s) : attend<false, 64, nt>(a, s))
-  if (one) ATTEND(1);
-  ATTEND(2);
+#define ATTEND(f, nt)                                                                                    \
+  return bf16 ? (head_dim == 128 ? attend<f, true, 128, nt>(a, s) : attend<f, true, 64, nt>(a, s))       \
+              : (head_dim == 128 ? attend<f, false, 128, nt>(a, s) : attend<f, false, 64, nt>(a, s))
+  if (a.c.format == BACON_CACHE_E2M1) {
+    if (one) ATTEND(BACON_CACHE_E2M1, 1);
+    ATTEND(BACON_CACHE_E2M1, 2);
+  }
+  if (one) ATTEND(BACON_CACHE_E4M3, 1);
+  ATTEND(BACON_CACHE_E4M3, 2);
 #undef ATTEND
 }
 

@@ -1,4 +1,4 @@
-// Device helpers shared by the kernels of the 8-bit cache.
+// Device helpers shared by the kernels of the cache.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -57,6 +57,36 @@ __device__ __forceinline__ int pair_len(const CacheDev &c, int64_t pair) {
   return n < 0 ? 0 : n > cap ? cap : n;
 }
 
+// ---- e2m1: two codes a byte, a scale for 32 values of a row
+
+// The exponent of 32 values whose largest magnitude is a, plus 127: e the
+// smallest integer with a <= 6 2^e = 1.5 2^(e+2), within the bounds.
+__device__ __forceinline__ unsigned scale4_byte(float a) {
+  const unsigned u = __float_as_uint(a);
+  int e = (int)(u >> 23) - 127 - 2 + ((u & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+  e = e < kCacheLow ? kCacheLow : e > kCache4High ? kCache4High : e;
+  return (unsigned)(e + 127);
+}
+
+// 2^e of byte `i` of a word of scales.
+__device__ __forceinline__ float scale4(unsigned w, int i) { return __uint_as_float((w >> (8 * i) & 0xFFu) << 23); }
+
+// A block's scales of its rows 16 i .. 16 i + 15 and dimensions 32 j .. 32 j + 31.
+template <int D>
+__device__ __forceinline__ uint8_t *block_scales4(const CacheDev &c, int id, int kv, int i, int j) {
+  return c.scales4 + ((((int64_t)id * 2 + kv) << (c.bt_log - 4)) + i) * (D / 2) + j * 16;
+}
+
+// Eight values as codes: the conversion divides by the scale, a power of two,
+// and rounds to nearest even.
+__device__ __forceinline__ unsigned codes4(const float (&x)[8], float scale) {
+  unsigned w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+}
+
 // Id of the pair's block i, or -1 where the table holds none of the pool's.
 __device__ __forceinline__ int block_id(const CacheDev &c, int64_t pair, int i) {
   const int id = i < c.max_blocks ? c.table[pair * c.max_blocks + i] : -1;
@@ -65,7 +95,7 @@ __device__ __forceinline__ int block_id(const CacheDev &c, int64_t pair, int i) 
 
 template <int D>
 __device__ __forceinline__ uint8_t *block_codes(const CacheDev &c, int id, int kv) {
-  return c.codes + (((int64_t)id * 2 + kv) << c.bt_log) * D;
+  return c.codes + (((int64_t)id * 2 + kv) << c.bt_log) * D;     // (e2m1: D the bytes of a row)
 }
 
 // Byte of V's code (row r of its block, dimension dim): groups of 16 rows,
@@ -114,6 +144,44 @@ __device__ __forceinline__ NewRows new_rows(const CacheStepArgs &a, int64_t pair
   NewRows n{b, h, len, count, len >> a.c.bt_log, (len + count - 1) >> a.c.bt_log, true};
   for (int i = n.b0; i <= n.b1; ++i) n.room &= block_id(a.c, pair, i) >= 0;
   return n;
+}
+
+// The same in e2m1: four lanes hold the 32 values of a scale, and no row
+// touches another's.
+template <bool BF16, int D>
+__device__ void append_block4(const CacheStepArgs &a, int64_t pair, const NewRows &n, int i) {
+  constexpr int TR = D / 8, RP = 64 / TR;
+  const CacheDev &c = a.c;
+  const int lane = threadIdx.x & 63, base = i << c.bt_log, l = lane % TR;
+  const int id = block_id(c, pair, i);
+  const int from = max(n.len, base), old = from - base, m = min(n.len + n.count, base + (1 << c.bt_log)) - from;
+  const int64_t row0 = (int64_t)n.b * a.tokens + (from - n.len);
+  for (int r0 = 0; r0 < m; r0 += RP) {                       // (whole waves: the lanes of a scale stay together)
+    const int r = r0 + lane / TR, at = old + r;
+    float x[2][8] = {};
+    if (r < m)
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv)
+        load8<BF16>(kv ? a.v : a.k, (row0 + r) * (kv ? a.v_stride : a.k_stride) + n.h * D + l * 8, x[kv]);
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[kv][e]));
+      top = fmaxf(top, __shfl_xor(top, 1));
+      top = fmaxf(top, __shfl_xor(top, 2));
+      const unsigned byte = scale4_byte(top), w = codes4(x[kv], __uint_as_float(byte << 23));
+      if (r >= m) continue;
+      if (l % 4 == 0) block_scales4<D>(c, id, kv, at >> 4, l / 4)[at & 15] = (uint8_t)byte;
+      uint8_t *dst = block_codes<D / 2>(c, id, kv);
+      if (kv == 0) {
+        *reinterpret_cast<unsigned *>(dst + at * (D / 2) + l * 4) = w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dst[v_at<D / 2>(at, l * 4 + e)] = (uint8_t)(w >> (8 * e));
+      }
+    }
+  }
 }
 
 // One wave puts the new rows of the pair's block i in place: 8 elements a

@@ -1,0 +1,587 @@
+// The prompt's attention on gfx950; include/bacon.h states the formulas.
+//
+// A workgroup takes 128 query rows of one KV head: row r of a sequence is query
+// r / G of head h G + r % G, so the G heads that share K and V share its tiles.
+// Each of its four waves holds 32 of them and sees every tile of keys, which
+// come through LDS, read directly from memory into one of two buffers while the
+// other is computed on.  Both products have the query rows along N:
+//
+//   S^T = K Q^T    lane (n = lane & 31, g = lane >> 5) holds, of row n, the logits
+//                  of keys 8 t + 4 g + i (t < 4, i < 4) of every 32
+//   O^T = V^T P^T  takes them from there: a lane's own weights are its share of
+//                  the keys, so nothing passes between lanes but the row's
+//                  maximum, once a tile, and its sum, once at the end
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "prompt.h"
+
+namespace bacon {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+#define GLOBAL __attribute__((address_space(1)))
+#define LDS __attribute__((address_space(3)))
+
+constexpr int kWaves = 4;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+// The maximum before any logit; below every finite one that counts.
+constexpr float kFloor = -3.402823466e38f;
+// A row's maximum over no key at all, in what parts hand on.
+constexpr float kNoKey = -INFINITY;
+// How far (in powers of two) weights may grow past 1 before the maximum they are
+// taken from moves: sums in 32 bits are as exact, and most tiles then move none.
+constexpr float kSlack = 8.f;
+
+// A unit of work: 128 query rows of a KV head of a sequence, over keys from .. to.
+struct Unit {
+  PromptSeq s;
+  int h, tile, split, row0, rows;      // row0: the first query row, rows: the sequence's
+  int from, to;
+};
+
+__device__ __forceinline__ int division(int i, unsigned magic) {     // i / G for small i
+  return magic ? (int)__umulhi((unsigned)i, magic) : i;
+}
+
+__device__ __forceinline__ int seq_of(const PromptArgs &a, int unit) {
+  int lo = 0, hi = a.seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (unit >= a.s[mid].unit0) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// The keys that query i of a sequence sees.
+__device__ __forceinline__ int keys_seen(const PromptSeq &s, int i) {
+  return min(max(s.keys - s.queries + i + 1, 0), s.keys);
+}
+
+// The longest rows come first, the heads next to each other (and so on dies of
+// their own, whose L2 then serves one head's keys to all its workgroups).
+__device__ __forceinline__ Unit unit_of(const PromptArgs &a, int i) {
+  Unit u;
+  u.s = a.s[seq_of(a, i)];
+  const int local = i - u.s.unit0, rest = local / a.Hkv;
+  u.h = local - rest * a.Hkv;
+  const int from_last = rest / u.s.splits;
+  u.split = rest - from_last * u.s.splits;
+  u.tile = u.s.tiles - 1 - from_last;
+  u.row0 = u.tile * kPromptRows;
+  u.rows = u.s.queries * a.G;
+  const int most = keys_seen(u.s, (min(u.row0 + kPromptRows, u.rows) - 1) / a.G);
+  const int chunk = ((u.s.keys + u.s.splits - 1) / u.s.splits + 63) & ~63;
+  u.from = u.split * chunk;
+  u.to = min(most, u.from + chunk);
+  return u;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// The value of the lane 32 away.
+__device__ __forceinline__ float other_half(float x) {
+  const unsigned u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// (A product and a difference joined into one rounding would leave an
+// unbounded rest of a huge logit.)
+__device__ __forceinline__ float minus(float a, float b) {
+#pragma clang fp contract(off)
+  return a - b;
+}
+
+// One query row of a lane.
+struct Row {
+  int query, head, end;      // end: keys seen (0 past the rows)
+  bool valid;
+};
+
+__device__ __forceinline__ Row row_of(const PromptArgs &a, const Unit &u, int r) {
+  const int first = u.row0 / a.G, rem = u.row0 - first * a.G;
+  const int q = division(rem + r, a.group_magic);
+  Row x;
+  x.valid = u.row0 + r < u.rows;
+  x.query = first + q;
+  x.head = u.h * a.G + rem + r - q * a.G;
+  x.end = x.valid ? keys_seen(u.s, x.query) : 0;
+  return x;
+}
+
+// What a lane hands on of its row: four runs of four dimensions of every 32.
+template <bool BF16, int D>
+__device__ __forceinline__ void finish(const PromptArgs &a, const Unit &u, const Row &row, int r, const f32x16 (&o)[D / 32],
+                                       float m, float sum) {
+  const int g = (threadIdx.x & 63) >> 5;
+  sum += other_half(sum);
+  if (!row.valid) return;
+  const bool none = min(row.end, u.to) <= u.from;
+  if (u.s.splits > 1) {
+    const int64_t at = (int64_t)blockIdx.x * kPromptRows + r;
+    if (g == 0) a.part_ml[at] = make_float2(none ? kNoKey : m, none ? 0.f : sum);
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        f32x4 x = {o[e][4 * t], o[e][4 * t + 1], o[e][4 * t + 2], o[e][4 * t + 3]};
+        if (none) x = f32x4{0.f, 0.f, 0.f, 0.f};
+        *reinterpret_cast<f32x4 *>(a.part_o + at * D + 32 * e + 8 * t + 4 * g) = x;
+      }
+    return;
+  }
+  const float l = none ? 1.f : sum > 0.f ? sum : __builtin_nanf(""), inv = 1.f / l;
+  const int64_t token = u.s.q0 + row.query;
+  const int64_t at = (token * a.Hq + row.head) * D;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f32x4 x = {o[e][4 * t], o[e][4 * t + 1], o[e][4 * t + 2], o[e][4 * t + 3]};
+      x = none ? f32x4{0.f, 0.f, 0.f, 0.f} : x * inv;
+      const int64_t i = at + 32 * e + 8 * t + 4 * g;
+      if constexpr (BF16)
+        *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(a.out) + i) = __builtin_convertvector(x, bf16x4);
+      else
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + i) = x;
+    }
+  if (g == 0) {
+    const float lse = none ? -INFINITY : m * a.scale + __log2f(l) * kLn2;
+    if (a.lse) a.lse[token * a.Hq + row.head] = lse;
+    const int w = a.W - u.s.queries + row.query;
+    if (a.window && w >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + w] = lse;
+  }
+}
+
+// The running maximum of a row (in units of its logits), and its sum of weights.
+template <int N, int E>
+__device__ __forceinline__ void weigh(f32x16 (&s)[N], f32x16 (&o)[E], float &m, float &sum, float scale_log2) {
+  float top = max3(s[0][0], s[0][1], s[0][2]);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = i ? 0 : 3; e + 1 < 16; e += 2) top = max3(top, s[i][e], s[i][e + 1]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = fmaxf(top, s[i][15]);
+  top = fmaxf(top, other_half(top));
+  if (__any(minus(top, m) * scale_log2 > kSlack)) {
+    const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(minus(m, next) * scale_log2);
+    m = next;
+    sum *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= f;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[i][e] = __builtin_amdgcn_exp2f(minus(s[i][e], m) * scale_log2);
+      sum += s[i][e];
+    }
+}
+
+// Keys base + 32 i + 8 (e / 4) + 4 g + e % 4 from `end` on are not seen.
+template <int N>
+__device__ __forceinline__ void mask(f32x16 (&s)[N], int left) {
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (32 * i + 8 * (e >> 2) + 4 * g + (e & 3) >= left) s[i][e] = -INFINITY;
+}
+
+// Rows of a tile as 16-byte pieces in LDS, piece c of row r at place c ^ f(r):
+// a read of the same piece of 16 or 32 rows then meets every bank once.
+template <int PIECES>
+__device__ __forceinline__ int k_place(int row) { return PIECES == 32 ? row & 31 : PIECES == 16 ? row & 15 : row >> 1 & 7; }
+template <int PIECES>
+__device__ __forceinline__ int v_place(int row) {
+  return PIECES == 16 ? (row & 3) << 2 : (row >> 1 & 1) << 2;
+}
+
+// What this wave asked for is there, and every other wave's: its reads of the
+// other buffer are done too.
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_s_waitcnt(0x0070);                        // vmcnt 0, lgkmcnt 0
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Wave `wave` of the workgroup asks for its share of ROWS rows from row `base`
+// on (rows past the last stand for it: what they give is masked).
+template <int ROWS, int PIECES, class Place>
+__device__ __forceinline__ void stage(const char *p, int64_t stride_bytes, int base, int last, char *to, int wave,
+                                      Place place) {
+  constexpr int EACH = ROWS * PIECES / 64 / kWaves;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int at = (wave * EACH + i) * 64, row = (at + lane) / PIECES, c = (lane & (PIECES - 1)) ^ place(row);
+    const char *from = p + min(base + row, last) * stride_bytes + c * 16;
+    __builtin_amdgcn_global_load_lds((const GLOBAL void *)from, (LDS void *)(to + at * 16), 16, 0, 0);
+  }
+}
+
+// V of a tile, 16 keys of step j for the dimensions 32 e .. of a lane.
+template <int ROW>
+__device__ __forceinline__ bf16x8 v_piece(const char *vt, int v_at, int j, int e) {
+  const char *at = vt + (v_at ^ (e << 6)) + j * 16 * ROW;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS s16x4 *)at);
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS s16x4 *)(at + 8 * ROW));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Halves of a word that are infinite or NaN, as their top bits.
+__device__ __forceinline__ unsigned not_finite(unsigned w) {
+  return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+
+// Whether a tile's V holds values that are not finite.  A weight of 0 would make
+// NaN of them, in the outputs of queries that do not see their key.
+template <int D, int ROW>
+__device__ __noinline__ bool tile_spoilt(const char *vt, int v_at) {
+  unsigned bad = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+      const u32x4 x = __builtin_bit_cast(u32x4, v_piece<ROW>(vt, v_at, j, e));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad |= not_finite(x[i]);
+    }
+  return __any(bad != 0);
+}
+
+// The second product over such a tile where some keys are masked: values that
+// are not finite count as 0, and make NaN of the queries that see their key
+// (`left` keys of the tile).
+template <int D, int ROW>
+__device__ __noinline__ void spoilt_product(const char *vt, int v_at, int left, const f32x16 (&s)[2], f32x16 (&o)[D / 32]) {
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) {
+    f32x16 hit;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bf16x8 p, seen;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = 16 * j + 8 * (i >> 2) + 4 * g + (i & 3);
+        p[i] = (__bf16)s[j >> 1][8 * (j & 1) + i];
+        seen[i] = (__bf16)(key < left ? 1.f : 0.f);
+      }
+      const u32x4 x = __builtin_bit_cast(u32x4, v_piece<ROW>(vt, v_at, j, e));
+      u32x4 fine, ones;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned bad = not_finite(x[i]), halves = (bad >> 15) * 0xFFFFu;
+        fine[i] = x[i] & ~halves;
+        ones[i] = halves & 0x3F803F80u;
+      }
+      o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fine), p, o[e], 0, 0, 0);
+      hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ones), seen, hit, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (hit[i] > 0.f) o[e][i] = __builtin_nanf("");
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
+  constexpr int KEYS = 64, PIECES = D / 8, TILE = KEYS * D * 2, ROW = D * 2;
+  __shared__ __align__(16) char lds[4 * TILE];               // K, V of two tiles
+  const Unit u = unit_of(a, blockIdx.x);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, g = lane >> 5;
+  const Row row = row_of(a, u, wave * 32 + n);
+  const char *k = static_cast<const char *>(a.k) + ((int64_t)u.s.k0 * a.k_stride + u.h * D) * 2;
+  const char *v = static_cast<const char *>(a.v) + ((int64_t)u.s.k0 * a.v_stride + u.h * D) * 2;
+  const auto ask = [&](int base, int buffer) {
+    char *to = lds + buffer * 2 * TILE;
+    stage<KEYS, PIECES>(k, a.k_stride * 2, base, u.s.keys - 1, to, wave, k_place<PIECES>);
+    stage<KEYS, PIECES>(v, a.v_stride * 2, base, u.s.keys - 1, to + TILE, wave, v_place<PIECES>);
+  };
+  if (u.from < u.to) ask(u.from, 0);
+  bf16x8 q[D / 16];
+  {
+    const char *p = static_cast<const char *>(a.q) +
+                    (((int64_t)u.s.q0 + row.query) * a.q_stride + (int64_t)row.head * D) * 2 + g * 16;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      u32x4 w = {0, 0, 0, 0};
+      if (row.valid) w = *reinterpret_cast<const u32x4 *>(p + 32 * i);
+      q[i] = __builtin_bit_cast(bf16x8, w);
+    }
+  }
+  // below this key nothing of the wave's is masked
+  const int clear = __builtin_amdgcn_readfirstlane(row.valid ? row.end : u.s.keys);
+  const int far = __builtin_amdgcn_readfirstlane(
+      min(u.to, u.row0 + wave * 32 >= u.rows ? 0
+                                             : keys_seen(u.s, (min(u.row0 + wave * 32 + 32, u.rows) - 1) / a.G)));
+  const float scale_log2 = a.scale * kLog2e;
+  f32x16 o[D / 32];
+  float m = kFloor, sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
+  // this lane's places in a tile: K rows n (+ 32), V rows 4 g + n / 4 % 4 (+ 8 ..)
+  const int k_at = n * ROW + ((g ^ k_place<PIECES>(n)) << 4);
+  const int key = 4 * g + ((lane & 15) >> 2);
+  const int v_at = key * ROW + (((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ v_place<PIECES>(key)) << 4) + (lane & 1) * 8;
+  int buffer = 0;
+  for (int base = u.from; base < u.to; base += KEYS, buffer ^= 1) {
+    tile_barrier();
+    if (base + KEYS < u.to) ask(base + KEYS, buffer ^ 1);
+    if (base >= far) continue;
+    const char *kt = lds + buffer * 2 * TILE, *vt = kt + TILE;
+    f32x16 s[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        const bf16x8 x = *reinterpret_cast<const bf16x8 *>(kt + (k_at ^ (c << 5)) + i * 32 * ROW);
+        s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[c], s[i], 0, 0, 0);
+      }
+    }
+    const bool masked = base + KEYS > clear;
+    if (masked) mask(s, row.end - base);
+    weigh(s, o, m, sum, scale_log2);
+    if (masked && tile_spoilt<D, ROW>(vt, v_at)) {
+      spoilt_product<D, ROW>(vt, v_at, row.end - base, s, o);
+      continue;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {                            // 16 keys a step
+      bf16x8 p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[j >> 1][8 * (j & 1) + e];
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) {
+        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_piece<ROW>(vt, v_at, j, e), p, o[e], 0, 0, 0);
+      }
+    }
+  }
+  finish<true, D>(a, u, row, wave * 32 + n, o, m, sum);
+}
+
+// In full precision: 32x32x2 products of floats, tiles of 32 keys.
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
+  constexpr int KEYS = 32, PIECES = D / 4, TILE = KEYS * D * 4, ROW = D * 4;
+  __shared__ __align__(16) char lds[4 * TILE];
+  const Unit u = unit_of(a, blockIdx.x);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, g = lane >> 5;
+  const Row row = row_of(a, u, wave * 32 + n);
+  const char *k = static_cast<const char *>(a.k) + ((int64_t)u.s.k0 * a.k_stride + u.h * D) * 4;
+  const char *v = static_cast<const char *>(a.v) + ((int64_t)u.s.k0 * a.v_stride + u.h * D) * 4;
+  const auto k_swap = [](int r) { return r & (PIECES - 1); };
+  const auto v_swap = [](int r) { return r >> 2 & 1 ? 8 : 0; };      // rows 4 g + i of both halves: other banks
+  const auto ask = [&](int base, int buffer) {
+    char *to = lds + buffer * 2 * TILE;
+    stage<KEYS, PIECES>(k, a.k_stride * 4, base, u.s.keys - 1, to, wave, k_swap);
+    stage<KEYS, PIECES>(v, a.v_stride * 4, base, u.s.keys - 1, to + TILE, wave, v_swap);
+  };
+  if (u.from < u.to) ask(u.from, 0);
+  f32x4 q[D / 8];                                            // dimensions 8 i + 4 g .. + 3
+  {
+    const char *p = static_cast<const char *>(a.q) +
+                    (((int64_t)u.s.q0 + row.query) * a.q_stride + (int64_t)row.head * D) * 4 + g * 16;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      q[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (row.valid) q[i] = *reinterpret_cast<const f32x4 *>(p + 32 * i);
+    }
+  }
+  const int clear = __builtin_amdgcn_readfirstlane(row.valid ? row.end : u.s.keys);
+  const int far = __builtin_amdgcn_readfirstlane(
+      min(u.to, u.row0 + wave * 32 >= u.rows ? 0
+                                             : keys_seen(u.s, (min(u.row0 + wave * 32 + 32, u.rows) - 1) / a.G)));
+  const float scale_log2 = a.scale * kLog2e;
+  f32x16 o[D / 32];
+  float m = kFloor, sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
+  int buffer = 0;
+  for (int base = u.from; base < u.to; base += KEYS, buffer ^= 1) {
+    tile_barrier();
+    if (base + KEYS < u.to) ask(base + KEYS, buffer ^ 1);
+    if (base >= far) continue;
+    const char *kt = lds + buffer * 2 * TILE, *vt = kt + TILE;
+    f32x16 s[1];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(kt + n * ROW + (((2 * c + g) ^ k_swap(n)) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[c][e], s[0], 0, 0, 0);
+    }
+    const bool masked = base + KEYS > clear;
+    if (masked) mask(s, row.end - base);
+    weigh(s, o, m, sum, scale_log2);
+    const auto v_value = [&](int j, int e) {
+      const int r = 8 * (j >> 2) + 4 * g + (j & 3);
+      return *reinterpret_cast<const float *>(vt + r * ROW + ((32 * e + n) ^ (g ? 32 : 0)) * 4);
+    };
+    const auto spoilt = [](float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; };
+    if (masked) {                                            // as tile_spoilt and spoilt_product
+      bool bad = false;
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) bad |= spoilt(v_value(j, e));
+      if (__any(bad)) {
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+          f32x16 hit;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float x = v_value(j, e), seen = base + 8 * (j >> 2) + 4 * g + (j & 3) < row.end ? 1.f : 0.f;
+            o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(spoilt(x) ? 0.f : x, s[0][j], o[e], 0, 0, 0);
+            hit = __builtin_amdgcn_mfma_f32_32x32x2f32(spoilt(x) ? 1.f : 0.f, seen, hit, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (hit[i] > 0.f) o[e][i] = __builtin_nanf("");
+        }
+        continue;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+        o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_value(j, e), s[0][j], o[e], 0, 0, 0);
+  }
+  finish<false, D>(a, u, row, wave * 32 + n, o, m, sum);
+}
+
+// Joins the parts of 128 query rows: D / 4 threads a row.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
+  constexpr int TR = D / 4;
+  const Unit u = unit_of(a, blockIdx.x);
+  if (u.split != 0 || u.s.splits == 1) return;
+  const int dim = threadIdx.x % TR * 4;
+  for (int r = threadIdx.x / TR; r < min(kPromptRows, u.rows - u.row0); r += 256 / TR) {
+    const Row row = row_of(a, u, r);
+    float top = kNoKey, l = 0.f, most = kFloor;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < u.s.splits; ++i) {
+      const int64_t at = ((int64_t)blockIdx.x + i * a.Hkv) * kPromptRows + r;
+      const float2 x = a.part_ml[at];
+      const f32x4 y = *reinterpret_cast<const f32x4 *>(a.part_o + at * D + dim);
+      const float m = fmaxf(most, x.x);
+      const float f = __builtin_amdgcn_exp2f(minus(most, m) * a.scale * kLog2e);
+      const float w = x.x == kNoKey ? 0.f : __builtin_amdgcn_exp2f(minus(x.x, m) * a.scale * kLog2e);
+      l = l * f + x.y * w;
+      acc = acc * f + y * w;
+      most = m;
+      top = fmaxf(top, x.x);
+    }
+    const bool none = row.end <= 0;
+    const float sum = none ? 1.f : l > 0.f ? l : __builtin_nanf(""), inv = 1.f / sum;
+    acc = none ? f32x4{0.f, 0.f, 0.f, 0.f} : acc * inv;
+    const int64_t token = u.s.q0 + row.query, at = (token * a.Hq + row.head) * D + dim;
+    if constexpr (BF16)
+      *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(a.out) + at) = __builtin_convertvector(acc, bf16x4);
+    else
+      *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at) = acc;
+    if (dim == 0) {
+      const float lse = none ? -INFINITY : most * a.scale + __log2f(sum) * kLn2;
+      if (a.lse) a.lse[token * a.Hq + row.head] = lse;
+      const int w = a.W - u.s.queries + row.query;
+      if (a.window && w >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + w] = lse;
+    }
+  }
+}
+
+}  // namespace
+
+PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
+  PromptPlan p{};
+  double total = 0;
+  int longest = 0;
+  for (int i = 0; i < a->seqs; ++i) {
+    PromptSeq &s = a->s[i];
+    s.tiles = (int)(((int64_t)s.queries * a->G + kPromptRows - 1) / kPromptRows);
+    const double first = std::max(0, s.keys - s.queries);
+    total += 0.5 * (first + s.keys) * s.tiles * a->Hkv;
+    longest = std::max(longest, s.keys);
+  }
+  const double slots = 512, ideal = total / slots;
+  const int chunk = longest <= 2 * ideal ? 0 : std::max(256, ((int)ideal + 63) / 64 * 64);
+  int64_t units = 0;
+  bool parts = false;
+  std::sort(a->s, a->s + a->seqs, [](const PromptSeq &x, const PromptSeq &y) {
+    return x.keys != y.keys ? x.keys > y.keys : x.index < y.index;
+  });
+  for (int i = 0; i < a->seqs; ++i) {
+    PromptSeq &s = a->s[i];
+    s.splits = chunk ? std::max(1, (s.keys + chunk - 1) / chunk) : 1;
+    parts |= s.splits > 1;
+    s.unit0 = (int)std::min<int64_t>(units, 0x7FFFFFFF);
+    units += (int64_t)s.tiles * s.splits * a->Hkv;
+  }
+  a->units = (int)std::min<int64_t>(units, 0x7FFFFFFF);
+  if (parts) {
+    const size_t rows = (size_t)units * kPromptRows;
+    p.ml_bytes = rows * sizeof(float2);
+    p.bytes = p.ml_bytes + rows * head_dim * sizeof(float);
+  }
+  return p;
+}
+
+hipError_t launch_prompt(const PromptArgs &a, bool bf16, int head_dim, hipStream_t s) {
+  const dim3 grid((unsigned)a.units), threads(256);
+  if (bf16 && head_dim == 128)
+    hipLaunchKernelGGL((k_prompt_bf16<128>), grid, threads, 0, s, a);
+  else if (bf16)
+    hipLaunchKernelGGL((k_prompt_bf16<64>), grid, threads, 0, s, a);
+  else if (head_dim == 128)
+    hipLaunchKernelGGL((k_prompt_fp32<128>), grid, threads, 0, s, a);
+  else
+    hipLaunchKernelGGL((k_prompt_fp32<64>), grid, threads, 0, s, a);
+  bool parts = false;
+  for (int i = 0; i < a.seqs; ++i) parts |= a.s[i].splits > 1;
+  if (parts) {
+    if (bf16 && head_dim == 128)
+      hipLaunchKernelGGL((k_prompt_join<true, 128>), grid, threads, 0, s, a);
+    else if (bf16)
+      hipLaunchKernelGGL((k_prompt_join<true, 64>), grid, threads, 0, s, a);
+    else if (head_dim == 128)
+      hipLaunchKernelGGL((k_prompt_join<false, 128>), grid, threads, 0, s, a);
+    else
+      hipLaunchKernelGGL((k_prompt_join<false, 64>), grid, threads, 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace bacon
