@@ -639,7 +639,8 @@ bacon_status bacon_rotate(const bacon_rotary *r, int64_t tokens, const int32_t *
  *
  * A query that sees no key (M_b > N_b) gives zeros and -infinity.  Rows behind
  * the last sequence are neither read nor written.  Rows are q_stride (k_stride,
- * v_stride) elements apart (>= heads x d, a multiple of 16 bytes).  d_out
+ * v_stride) elements apart (>= heads x d, a multiple of 16 bytes; of K and V
+ * under 2^26 bytes).  d_out
  * [cu_queries[batch], Hq, d]; d_lse (optional) [cu_queries[batch], Hq] float32;
  * d_window_lse (optional) [batch, Hq, W] float32: the lse of the queries that are
  * the window's tokens (token N_b - W + w is entry w); entries whose token is not

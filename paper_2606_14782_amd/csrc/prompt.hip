@@ -34,7 +34,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-// The maximum before any logit; below every finite one that counts.
+// The maximum before any logit: below every finite one times log2(e) / sqrt(d).
 constexpr float kFloor = -3.402823466e38f;
 // A row's maximum over no key at all, in what parts hand on.
 constexpr float kNoKey = -INFINITY;
@@ -86,10 +86,9 @@ __device__ __forceinline__ Unit unit_of(const PromptArgs &a, int i) {
   return u;
 }
 
+// (NaN where one of them is: such a row gives NaN whatever its maximum.)
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
 // The value of the lane 32 away.
@@ -123,17 +122,28 @@ __device__ __forceinline__ Row row_of(const PromptArgs &a, const Unit &u, int r)
   return x;
 }
 
+// What a row's weights are taken from: 2^(logit log2(e) - at), `at` the maximum so
+// far in units of log2, rounded once.  A weight is then one product, subtracted in
+// the same rounding, since an error of `at` is every weight's alike; where `at` is
+// so large that the product's rest would count (`far`), the product is rounded first.
+struct Weighed {
+  float at = kFloor, sum = 0.f;
+  bool far = false;          // one of the wave's rows is
+};
+
+__device__ __forceinline__ bool is_far(float at) { return __builtin_fabsf(at) > 0x1p20f && at != kFloor; }
+
 // What a lane hands on of its row: four runs of four dimensions of every 32.
 template <bool BF16, int D>
 __device__ __forceinline__ void finish(const PromptArgs &a, const Unit &u, const Row &row, int r, const f32x16 (&o)[D / 32],
-                                       float m, float sum) {
+                                       const Weighed &w) {
   const int g = (threadIdx.x & 63) >> 5;
-  sum += other_half(sum);
+  const float sum = w.sum + other_half(w.sum);
   if (!row.valid) return;
   const bool none = min(row.end, u.to) <= u.from;
   if (u.s.splits > 1) {
     const int64_t at = (int64_t)blockIdx.x * kPromptRows + r;
-    if (g == 0) a.part_ml[at] = make_float2(none ? kNoKey : m, none ? 0.f : sum);
+    if (g == 0) a.part_ml[at] = make_float2(none ? kNoKey : w.at, none ? 0.f : sum);
 #pragma unroll
     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -160,38 +170,52 @@ __device__ __forceinline__ void finish(const PromptArgs &a, const Unit &u, const
         *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + i) = x;
     }
   if (g == 0) {
-    const float lse = none ? -INFINITY : m * a.scale + __log2f(l) * kLn2;
+    const float lse = none ? -INFINITY : (w.at + __log2f(l)) * kLn2;
     if (a.lse) a.lse[token * a.Hq + row.head] = lse;
-    const int w = a.W - u.s.queries + row.query;
-    if (a.window && w >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + w] = lse;
+    const int at_window = a.W - u.s.queries + row.query;
+    if (a.window && at_window >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + at_window] = lse;
   }
 }
 
-// The running maximum of a row (in units of its logits), and its sum of weights.
 template <int N, int E>
-__device__ __forceinline__ void weigh(f32x16 (&s)[N], f32x16 (&o)[E], float &m, float &sum, float scale_log2) {
+__device__ __forceinline__ void weigh(f32x16 (&s)[N], f32x16 (&o)[E], Weighed &w, float scale_log2) {
   float top = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int e = i ? 0 : 3; e + 1 < 16; e += 2) top = max3(top, s[i][e], s[i][e + 1]);
-#pragma unroll
-  for (int i = 0; i < N; ++i) top = fmaxf(top, s[i][15]);
-  top = fmaxf(top, other_half(top));
-  if (__any(minus(top, m) * scale_log2 > kSlack)) {
-    const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(minus(m, next) * scale_log2);
-    m = next;
-    sum *= f;
+  top = __builtin_elementwise_maximum(top, s[0][15]);
+  top = __builtin_elementwise_maximum(top, other_half(top)) * scale_log2;
+  const bool moves = top > w.at + kSlack;                    // (each row by itself: its results depend on no other)
+  if (__any(moves)) {
+    const float next = moves ? top : w.at, f = __builtin_amdgcn_exp2f(minus(w.at, next));
+    w.at = next;
+    w.far = __any(is_far(next));
+    w.sum *= f;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= f;
   }
+  if (__builtin_expect(w.far, 0)) {
+    const bool far = is_far(w.at);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = far ? minus(s[i][e] * scale_log2, w.at) : __builtin_fmaf(s[i][e], scale_log2, -w.at);
+        s[i][e] = __builtin_amdgcn_exp2f(x);
+      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], scale_log2, -w.at));
+  }
+  float part[4] = {0.f, 0.f, 0.f, 0.f};                      // (chains of their own)
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      s[i][e] = __builtin_amdgcn_exp2f(minus(s[i][e], m) * scale_log2);
-      sum += s[i][e];
-    }
+    for (int e = 0; e < 16; ++e) part[e & 3] += s[i][e];
+  w.sum += (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 // Keys base + 32 i + 8 (e / 4) + 4 g + e % 4 from `end` on are not seen.
@@ -223,20 +247,33 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// Wave `wave` of the workgroup asks for its share of ROWS rows from row `base`
-// on (rows past the last stand for it: what they give is masked).
-template <int ROWS, int PIECES, class Place>
-__device__ __forceinline__ void stage(const char *p, int64_t stride_bytes, int base, int last, char *to, int wave,
-                                      Place place) {
-  constexpr int EACH = ROWS * PIECES / 64 / kWaves;
-  const int lane = threadIdx.x & 63;
+// This wave's share of a tile's ROWS rows of K or V, in 16-byte pieces: where
+// each piece lies from the tile's first row on.
+template <int ROWS, int PIECES>
+struct Share {
+  static constexpr int kEach = ROWS * PIECES / 64 / kWaves;
+  unsigned at[kEach];
+
+  template <class Place>
+  __device__ __forceinline__ void find(unsigned stride_bytes, int rows, int wave, Place place) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int i = 0; i < EACH; ++i) {
-    const int at = (wave * EACH + i) * 64, row = (at + lane) / PIECES, c = (lane & (PIECES - 1)) ^ place(row);
-    const char *from = p + min(base + row, last) * stride_bytes + c * 16;
-    __builtin_amdgcn_global_load_lds((const GLOBAL void *)from, (LDS void *)(to + at * 16), 16, 0, 0);
+    for (int i = 0; i < kEach; ++i) {
+      const int row = ((wave * kEach + i) * 64 + lane) / PIECES, c = (lane & (PIECES - 1)) ^ place(row);
+      at[i] = (unsigned)min(row, rows - 1) * stride_bytes + c * 16;   // (rows past the last stand for it: they are masked)
+    }
   }
-}
+
+  // Asks for it, directly into LDS (a wave's 64 pieces one after the other).  The
+  // compiler does not see these: it would wait for them before it reads the other
+  // buffer.  tile_barrier waits.  (Nothing else here uses m0.)
+  __device__ __forceinline__ void ask(const char *tile, unsigned to, int wave) const {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                   :: "s"(to + (wave * kEach + i) * 1024), "v"(at[i]), "s"(tile) : "memory");
+  }
+};
 
 // V of a tile, 16 keys of step j for the dimensions 32 e .. of a lane.
 template <int ROW>
@@ -247,61 +284,35 @@ __device__ __forceinline__ bf16x8 v_piece(const char *vt, int v_at, int j, int e
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Halves of a word that are infinite or NaN, as their top bits.
-__device__ __forceinline__ unsigned not_finite(unsigned w) {
-  return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+// Where some keys of a tile are masked, V's values that are not finite count as
+// 0 (a weight of 0 would make NaN of them, in the outputs of queries that do not
+// see their key), and are noted: spoil() then finds who sees them.
+__device__ __forceinline__ unsigned finite_halves(unsigned w, unsigned &bad) {
+  const unsigned x = ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;      // top bits of those that are not
+  bad |= x;
+  return w & ~((x << 1) - (x >> 15));
 }
 
-// Whether a tile's V holds values that are not finite.  A weight of 0 would make
-// NaN of them, in the outputs of queries that do not see their key.
-template <int D, int ROW>
-__device__ __noinline__ bool tile_spoilt(const char *vt, int v_at) {
-  unsigned bad = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) {
-      const u32x4 x = __builtin_bit_cast(u32x4, v_piece<ROW>(vt, v_at, j, e));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= not_finite(x[i]);
-    }
-  return __any(bad != 0);
-}
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 
-// The second product over such a tile where some keys are masked: values that
-// are not finite count as 0, and make NaN of the queries that see their key
-// (`left` keys of the tile).
-template <int D, int ROW>
-__device__ __noinline__ void spoilt_product(const char *vt, int v_at, int left, const f32x16 (&s)[2], f32x16 (&o)[D / 32]) {
+// The outputs of a lane's row that a key from `from` on, which the row sees, holds
+// such a value for are NaN.  (Rare, and slow.)
+template <bool BF16, int D>
+__device__ __forceinline__ void spoil(const char *v, int64_t stride_bytes, int from, int end, f32x16 (&o)[D / 32]) {
   const int g = (threadIdx.x & 63) >> 5;
+  for (int key = from; key < end; ++key) {
+    const char *p = v + key * stride_bytes;
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e) {
-    f32x16 hit;
+    for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bf16x8 p, seen;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int key = 16 * j + 8 * (i >> 2) + 4 * g + (i & 3);
-        p[i] = (__bf16)s[j >> 1][8 * (j & 1) + i];
-        seen[i] = (__bf16)(key < left ? 1.f : 0.f);
-      }
-      const u32x4 x = __builtin_bit_cast(u32x4, v_piece<ROW>(vt, v_at, j, e));
-      u32x4 fine, ones;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const unsigned bad = not_finite(x[i]), halves = (bad >> 15) * 0xFFFFu;
-        fine[i] = x[i] & ~halves;
-        ones[i] = halves & 0x3F803F80u;
-      }
-      o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fine), p, o[e], 0, 0, 0);
-      hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ones), seen, hit, 0, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (hit[i] > 0.f) o[e][i] = __builtin_nanf("");
+        for (int i = 0; i < 4; ++i) {
+          const int dim = 32 * e + 8 * t + 4 * g + i;
+          const float x = BF16 ? __uint_as_float((unsigned)reinterpret_cast<const uint16_t *>(p)[dim] << 16)
+                               : reinterpret_cast<const float *>(p)[dim];
+          if (!finite(x)) o[e][4 * t + i] = __builtin_nanf("");
+        }
   }
 }
 
@@ -315,10 +326,18 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
   const Row row = row_of(a, u, wave * 32 + n);
   const char *k = static_cast<const char *>(a.k) + ((int64_t)u.s.k0 * a.k_stride + u.h * D) * 2;
   const char *v = static_cast<const char *>(a.v) + ((int64_t)u.s.k0 * a.v_stride + u.h * D) * 2;
+  const unsigned lds_at = (unsigned)(uintptr_t)(LDS char *)lds;
+  Share<KEYS, PIECES> ks, vs;
+  ks.find(a.k_stride * 2, KEYS, wave, k_place<PIECES>);
+  vs.find(a.v_stride * 2, KEYS, wave, v_place<PIECES>);
   const auto ask = [&](int base, int buffer) {
-    char *to = lds + buffer * 2 * TILE;
-    stage<KEYS, PIECES>(k, a.k_stride * 2, base, u.s.keys - 1, to, wave, k_place<PIECES>);
-    stage<KEYS, PIECES>(v, a.v_stride * 2, base, u.s.keys - 1, to + TILE, wave, v_place<PIECES>);
+    const unsigned to = lds_at + buffer * 2 * TILE;
+    if (u.s.keys - base < KEYS) {
+      ks.find(a.k_stride * 2, u.s.keys - base, wave, k_place<PIECES>);
+      vs.find(a.v_stride * 2, u.s.keys - base, wave, v_place<PIECES>);
+    }
+    ks.ask(k + base * a.k_stride * 2, to, wave);
+    vs.ask(v + base * a.v_stride * 2, to + TILE, wave);
   };
   if (u.from < u.to) ask(u.from, 0);
   bf16x8 q[D / 16];
@@ -339,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
                                              : keys_seen(u.s, (min(u.row0 + wave * 32 + 32, u.rows) - 1) / a.G)));
   const float scale_log2 = a.scale * kLog2e;
   f32x16 o[D / 32];
-  float m = kFloor, sum = 0.f;
+  Weighed w;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -349,6 +368,7 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
   const int key = 4 * g + ((lane & 15) >> 2);
   const int v_at = key * ROW + (((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ v_place<PIECES>(key)) << 4) + (lane & 1) * 8;
   int buffer = 0;
+  unsigned bad = 0;
   for (int base = u.from; base < u.to; base += KEYS, buffer ^= 1) {
     tile_barrier();
     if (base + KEYS < u.to) ask(base + KEYS, buffer ^ 1);
@@ -367,11 +387,7 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
     }
     const bool masked = base + KEYS > clear;
     if (masked) mask(s, row.end - base);
-    weigh(s, o, m, sum, scale_log2);
-    if (masked && tile_spoilt<D, ROW>(vt, v_at)) {
-      spoilt_product<D, ROW>(vt, v_at, row.end - base, s, o);
-      continue;
-    }
+    weigh(s, o, w, scale_log2);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {                            // 16 keys a step
       bf16x8 p;
@@ -379,11 +395,19 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
       for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[j >> 1][8 * (j & 1) + e];
 #pragma unroll
       for (int e = 0; e < D / 32; ++e) {
-        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_piece<ROW>(vt, v_at, j, e), p, o[e], 0, 0, 0);
+        bf16x8 x = v_piece<ROW>(vt, v_at, j, e);
+        if (masked) {
+          u32x4 y = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = finite_halves(y[i], bad);
+          x = __builtin_bit_cast(bf16x8, y);
+        }
+        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p, o[e], 0, 0, 0);
       }
     }
   }
-  finish<true, D>(a, u, row, wave * 32 + n, o, m, sum);
+  if (__any(bad != 0)) spoil<true, D>(v, a.v_stride * 2, max(u.from, clear & ~(KEYS - 1)), min(row.end, u.to), o);
+  finish<true, D>(a, u, row, wave * 32 + n, o, w);
 }
 
 // In full precision: 32x32x2 products of floats, tiles of 32 keys.
@@ -399,10 +423,18 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
   const char *v = static_cast<const char *>(a.v) + ((int64_t)u.s.k0 * a.v_stride + u.h * D) * 4;
   const auto k_swap = [](int r) { return r & (PIECES - 1); };
   const auto v_swap = [](int r) { return r >> 2 & 1 ? 8 : 0; };      // rows 4 g + i of both halves: other banks
+  const unsigned lds_at = (unsigned)(uintptr_t)(LDS char *)lds;
+  Share<KEYS, PIECES> ks, vs;
+  ks.find(a.k_stride * 4, KEYS, wave, k_swap);
+  vs.find(a.v_stride * 4, KEYS, wave, v_swap);
   const auto ask = [&](int base, int buffer) {
-    char *to = lds + buffer * 2 * TILE;
-    stage<KEYS, PIECES>(k, a.k_stride * 4, base, u.s.keys - 1, to, wave, k_swap);
-    stage<KEYS, PIECES>(v, a.v_stride * 4, base, u.s.keys - 1, to + TILE, wave, v_swap);
+    const unsigned to = lds_at + buffer * 2 * TILE;
+    if (u.s.keys - base < KEYS) {
+      ks.find(a.k_stride * 4, u.s.keys - base, wave, k_swap);
+      vs.find(a.v_stride * 4, u.s.keys - base, wave, v_swap);
+    }
+    ks.ask(k + base * a.k_stride * 4, to, wave);
+    vs.ask(v + base * a.v_stride * 4, to + TILE, wave);
   };
   if (u.from < u.to) ask(u.from, 0);
   f32x4 q[D / 8];                                            // dimensions 8 i + 4 g .. + 3
@@ -421,12 +453,13 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
                                              : keys_seen(u.s, (min(u.row0 + wave * 32 + 32, u.rows) - 1) / a.G)));
   const float scale_log2 = a.scale * kLog2e;
   f32x16 o[D / 32];
-  float m = kFloor, sum = 0.f;
+  Weighed w;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
   int buffer = 0;
+  unsigned bad = 0;
   for (int base = u.from; base < u.to; base += KEYS, buffer ^= 1) {
     tile_barrier();
     if (base + KEYS < u.to) ask(base + KEYS, buffer ^ 1);
@@ -443,44 +476,25 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
     }
     const bool masked = base + KEYS > clear;
     if (masked) mask(s, row.end - base);
-    weigh(s, o, m, sum, scale_log2);
+    weigh(s, o, w, scale_log2);
     const auto v_value = [&](int j, int e) {
       const int r = 8 * (j >> 2) + 4 * g + (j & 3);
       return *reinterpret_cast<const float *>(vt + r * ROW + ((32 * e + n) ^ (g ? 32 : 0)) * 4);
     };
-    const auto spoilt = [](float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; };
-    if (masked) {                                            // as tile_spoilt and spoilt_product
-      bool bad = false;
-#pragma unroll
-      for (int j = 0; j < 16; ++j)
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) bad |= spoilt(v_value(j, e));
-      if (__any(bad)) {
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) {
-          f32x16 hit;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) hit[i] = 0.f;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float x = v_value(j, e), seen = base + 8 * (j >> 2) + 4 * g + (j & 3) < row.end ? 1.f : 0.f;
-            o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(spoilt(x) ? 0.f : x, s[0][j], o[e], 0, 0, 0);
-            hit = __builtin_amdgcn_mfma_f32_32x32x2f32(spoilt(x) ? 1.f : 0.f, seen, hit, 0, 0, 0);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (hit[i] > 0.f) o[e][i] = __builtin_nanf("");
-        }
-        continue;
-      }
-    }
 #pragma unroll
     for (int j = 0; j < 16; ++j)
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e)
-        o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_value(j, e), s[0][j], o[e], 0, 0, 0);
+      for (int e = 0; e < D / 32; ++e) {
+        float x = v_value(j, e);
+        if (masked && !finite(x)) {
+          x = 0.f;
+          bad = 1;
+        }
+        o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[0][j], o[e], 0, 0, 0);
+      }
   }
-  finish<false, D>(a, u, row, wave * 32 + n, o, m, sum);
+  if (__any(bad != 0)) spoil<false, D>(v, a.v_stride * 4, max(u.from, clear & ~(KEYS - 1)), min(row.end, u.to), o);
+  finish<false, D>(a, u, row, wave * 32 + n, o, w);
 }
 
 // Joins the parts of 128 query rows: D / 4 threads a row.
@@ -492,19 +506,18 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
   const int dim = threadIdx.x % TR * 4;
   for (int r = threadIdx.x / TR; r < min(kPromptRows, u.rows - u.row0); r += 256 / TR) {
     const Row row = row_of(a, u, r);
-    float top = kNoKey, l = 0.f, most = kFloor;
+    float l = 0.f, most = kFloor;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < u.s.splits; ++i) {
       const int64_t at = ((int64_t)blockIdx.x + i * a.Hkv) * kPromptRows + r;
       const float2 x = a.part_ml[at];
       const f32x4 y = *reinterpret_cast<const f32x4 *>(a.part_o + at * D + dim);
       const float m = fmaxf(most, x.x);
-      const float f = __builtin_amdgcn_exp2f(minus(most, m) * a.scale * kLog2e);
-      const float w = x.x == kNoKey ? 0.f : __builtin_amdgcn_exp2f(minus(x.x, m) * a.scale * kLog2e);
+      const float f = __builtin_amdgcn_exp2f(minus(most, m));
+      const float w = x.x == kNoKey ? 0.f : __builtin_amdgcn_exp2f(minus(x.x, m));
       l = l * f + x.y * w;
       acc = acc * f + y * w;
       most = m;
-      top = fmaxf(top, x.x);
     }
     const bool none = row.end <= 0;
     const float sum = none ? 1.f : l > 0.f ? l : __builtin_nanf(""), inv = 1.f / sum;
@@ -515,7 +528,7 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
     else
       *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at) = acc;
     if (dim == 0) {
-      const float lse = none ? -INFINITY : most * a.scale + __log2f(sum) * kLn2;
+      const float lse = none ? -INFINITY : (most + __log2f(sum)) * kLn2;
       if (a.lse) a.lse[token * a.Hq + row.head] = lse;
       const int w = a.W - u.s.queries + row.query;
       if (a.window && w >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + w] = lse;

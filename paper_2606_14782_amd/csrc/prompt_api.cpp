@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kMaxGroup = 1024;            // query heads of a KV head
 constexpr int64_t kMaxTokens = 1 << 30;
+constexpr int64_t kMaxStride = 1 << 26;    // bytes between rows of K or V: 64 of them within 2^32
 constexpr int kMaxUnits = (1 << 24) - 1;   // workgroups of 256 threads: a launch holds fewer than 2^32
 
 bacon_status check_shape(const bacon_shape *s) {
@@ -106,6 +107,13 @@ bacon_status check_rows(const bacon_shape *s, const void *p, int64_t stride, int
   return BACON_OK;
 }
 
+// K's and V's tiles are found from their first rows in 32 bits.
+bacon_status check_tile(const bacon_shape *s, int64_t stride, const char *name) {
+  if (stride * (s->dtype == BACON_BF16 ? 2 : 4) >= kMaxStride)
+    return fail(BACON_ERR_UNSUPPORTED, "%s rows of %lld elements' distance are too far apart", name, (long long)stride);
+  return BACON_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -131,6 +139,8 @@ bacon_status bacon_prompt_attend(const bacon_shape *shape, const bacon_batch *ba
   if (batch->cu_seqlens[batch->batch]) {       // (queries of no keys at all need none)
     TRY(check_rows(shape, d_k, k_stride, a.Hkv, "k"));
     TRY(check_rows(shape, d_v, v_stride, a.Hkv, "v"));
+    TRY(check_tile(shape, k_stride, "k"));
+    TRY(check_tile(shape, v_stride, "v"));
   }
   if (p.bytes) {
     TRY(check_ptr(d_work, "work", 256));
