@@ -457,71 +457,73 @@ def bacon_window_lse(ctx: Context, batch, q_win, k, out=None):
     return ctx.bacon_window_lse(batch, q_win, k, out)
 
 
-def _tokens_at(t):
-    """Pointer, tokens and token distance of heads [.., H, d] that lie together,
-    or None where they do not, or the tokens are not evenly spaced."""
-    *lead, h, d = t.shape
-    *steps, sh, sd = t.stride()
-    n = 1
-    for x in lead:
-        n *= x
-    if n == 0:
-        return t.data_ptr(), 0, h * d
-    if d > 1 and sd != 1 or h > 1 and sh != d:
+def _tokens_at(t, heads, head_dim):
+    """Tokens and token distance of heads [.., heads, head_dim] that lie together,
+    tokens evenly spaced; None where t is not that."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) < 3 or shape[-1] != head_dim or shape[-2] != heads:
         return None
-    step = run = None                             # the distance of tokens, and of a whole leading index
-    for size, stride in zip(reversed(lead), reversed(steps)):
+    if strides[-1] != 1 or strides[-2] != head_dim and heads > 1:
+        return 0, heads * head_dim if 0 in shape else None
+    n, step, run = 1, None, None                  # run: the distance of a whole leading index
+    for size, stride in zip(shape[-3::-1], strides[-3::-1]):
+        n *= size
         if size == 1:
             continue
         if step is None:
-            step, run = stride, stride * size
-        elif stride != run:
+            step = stride
+        elif stride != run and n:
             return None
-        else:
-            run *= size
-    return t.data_ptr(), n, h * d if step is None else step
+        run = stride * size
+    return n, heads * head_dim if step is None or n == 0 else step
 
 
 class _Given:
     """Checks and pointers of the tensors of one call, all on the first one's device."""
 
-    def __init__(self, like, dtype=None):
-        import torch
-        if not isinstance(like, torch.Tensor) or like.device.type != "cuda":
-            raise BaconError(ERR_INVALID, "tensors on a GPU are needed")
-        self.torch, self.device, self.dtype = torch, like.device, dtype or like.dtype
+    __slots__ = ("torch", "device", "dtype")
 
-    def rows(self, t, name, heads, head_dim, lead=None):
-        """Pointer, tokens and token distance of [.., heads, head_dim]."""
-        if t.dtype != self.dtype or t.device != self.device or t.dim() < 3 or t.shape[-2:] != (heads, head_dim):
-            raise BaconError(ERR_INVALID, f"{name} must be {self.dtype} [.., {heads}, {head_dim}] on {self.device}, "
-                                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-        if lead is not None and t.shape[:-2] != lead:
-            raise BaconError(ERR_INVALID, f"{name} has shape {tuple(t.shape)}, tokens {tuple(lead)} expected")
-        at = _tokens_at(t)
-        if at is None:
-            raise BaconError(ERR_INVALID, f"{name} has strides {t.stride()}: a token's heads lie together, tokens "
-                                          "evenly spaced")
+    def __init__(self, like, dtype):
+        import torch
+        if not isinstance(like, torch.Tensor) or not like.is_cuda:
+            raise BaconError(ERR_INVALID, "tensors on a GPU are needed")
+        self.torch, self.device, self.dtype = torch, like.device, dtype
+
+    def rows(self, t, name, heads, head_dim):
+        """Tokens and token distance of [.., heads, head_dim]."""
+        shape, strides = t.shape, t.stride()
+        if (len(shape) == 3 and strides[2] == 1 and strides[1] == head_dim and shape[1] == heads and shape[2] == head_dim
+                and shape[0] > 1 and t.dtype == self.dtype and t.device == self.device):
+            return shape[0], strides[0]
+        at = _tokens_at(t, heads, head_dim) if t.dtype == self.dtype and t.device == self.device else None
+        if at is None or at[1] is None:
+            raise BaconError(ERR_INVALID, f"{name} must be {self.dtype} [.., {heads}, {head_dim}] on {self.device}, a "
+                                          f"token's heads together, tokens evenly spaced: got {t.dtype} {tuple(t.shape)} "
+                                          f"with strides {t.stride()} on {t.device}")
         return at
 
     def whole(self, t, name, shape, dtype=None):
         """The pointer of a contiguous tensor (None: NULL)."""
         if t is None:
             return None
-        dtype = dtype or self.dtype
-        if t.dtype != dtype or t.device != self.device or not t.is_contiguous() or shape is not None and t.shape != shape:
-            raise BaconError(ERR_INVALID, f"{name} must be a contiguous {dtype} tensor {shape and tuple(shape)} on "
-                                          f"{self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if (t.dtype != (dtype or self.dtype) or t.device != self.device or not t.is_contiguous()
+                or shape is not None and t.shape != shape):
+            raise BaconError(ERR_INVALID, f"{name} must be a contiguous {dtype or self.dtype} tensor "
+                                          f"{shape and tuple(shape)} on {self.device}, got {t.dtype} {tuple(t.shape)} "
+                                          f"on {t.device}")
         return t.data_ptr()
+
+    def like(self, t):
+        return self.torch.empty_like(t, memory_format=self.torch.contiguous_format)
 
     def call(self, fn, *args):
         """fn on the tensors' device and that device's current stream."""
-        cuda = self.torch.cuda
-        if cuda.current_device() == self.device.index:
-            status = fn(*args, self.torch._C._cuda_getCurrentRawStream(self.device.index))
+        at, C_ = self.device.index, self.torch._C
+        if C_._cuda_getDevice() == at:
+            status = fn(*args, C_._cuda_getCurrentRawStream(at))
         else:
-            with cuda.device(self.device):
-                status = fn(*args, self.torch._C._cuda_getCurrentRawStream(self.device.index))
+            with self.torch.cuda.device(self.device):
+                status = fn(*args, C_._cuda_getCurrentRawStream(at))
         if status:
             _check(status)
 
@@ -562,6 +564,8 @@ class Rotary:
         m = C.c_double()
         _check(lib().bacon_rotary_frequencies(C.byref(c), f.ctypes.data, C.byref(m)))
         self.frequencies, self.magnitude = f, m.value
+        self.num_q_heads, self.num_kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
+        self._rotate, self._c = lib().bacon_rotate, C.byref(c)
 
 
 def bacon_rotate(rotary: Rotary, positions, q=None, k=None, q_norm=None, k_norm=None, q_out=None, k_out=None):
@@ -572,27 +576,35 @@ def bacon_rotate(rotary: Rotary, positions, q=None, k=None, q_norm=None, k_norm=
     first = q if q is not None else k
     if first is None:
         raise BaconError(ERR_INVALID, "q and k are None")
-    g, c = _Given(first, rotary.torch_dtype), rotary.c
-    lead = first.shape[:-2]
-    args, outs, n = [], [], 0
-    for x, y, heads, name in ((q, q_out, c.num_q_heads, "q"), (k, k_out, c.num_kv_heads, "k")):
-        if x is None:
-            if y is not None:
-                raise BaconError(ERR_INVALID, f"{name}_out without {name}")
-            args.append((None, 0, None, 0))
+    g, c, lead, d = _Given(first, rotary.torch_dtype), rotary.c, first.shape[:-2], rotary.head_dim
+    qp = kp = qo = ko = None
+    qs = ks = qos = kos = n = 0
+    if q is not None:
+        n, qs = g.rows(q, "q", rotary.num_q_heads, d)
+        if q_out is None:
+            q_out = g.like(q)
+            qos = rotary.num_q_heads * d
         else:
-            p, n, step = g.rows(x, name, heads, c.head_dim, lead)
-            if y is None:
-                y = x.new_empty(x.shape)
-            to, _, to_step = g.rows(y, name + "_out", heads, c.head_dim, lead)
-            args.append((p, step, to, to_step))
-        outs.append(y)
-    d = (c.head_dim,)
+            qos = g.rows(q_out, "q_out", rotary.num_q_heads, d)[1]
+        qp, qo = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise BaconError(ERR_INVALID, "q_out without q")
+    if k is not None:
+        n, ks = g.rows(k, "k", rotary.num_kv_heads, d)
+        if k_out is None:
+            k_out = g.like(k)
+            kos = rotary.num_kv_heads * d
+        else:
+            kos = g.rows(k_out, "k_out", rotary.num_kv_heads, d)[1]
+        kp, ko = k.data_ptr(), k_out.data_ptr()
+    elif k_out is not None:
+        raise BaconError(ERR_INVALID, "k_out without k")
+    if q is not None and q_out.shape[:-2] != lead or k is not None and (k.shape[:-2] != lead or k_out.shape[:-2] != lead):
+        raise BaconError(ERR_INVALID, f"q, k and their outputs do not all have the tokens {tuple(lead)}")
     pos = g.whole(positions, "positions", (3, *lead) if rotary.sectioned else lead, g.torch.int32)
-    (qp, qs, qo, qos), (kp, ks, ko, kos) = args
-    g.call(lib().bacon_rotate, C.byref(c), n, pos, qp, qs, kp, ks, g.whole(q_norm, "q_norm", d),
-           g.whole(k_norm, "k_norm", d), qo, qos, ko, kos)
-    return tuple(outs)
+    g.call(rotary._rotate, rotary._c, n, pos, qp, qs, kp, ks, None if q_norm is None else g.whole(q_norm, "q_norm", (d,)),
+           None if k_norm is None else g.whole(k_norm, "k_norm", (d,)), qo, qos, ko, kos)
+    return q_out, k_out
 
 
 def bacon_prompt_attend(shape: Shape, batch: BatchLayout, q, k, v, queries=None, want_lse=False,
@@ -601,38 +613,42 @@ def bacon_prompt_attend(shape: Shape, batch: BatchLayout, q, k, v, queries=None,
     Hkv, d] (views of one projection's output will do).  queries: the cumulative
     numbers of queries [batch + 1] where they are the prompts' last tokens only.
     Returns (out [Tq, Hq, d], lse [Tq, Hq] or None, window_lse [batch, Hq, W] or
-    None); entries of a given window_lse whose token is no query stay."""
-    g = _Given(q)
-    torch, hq, hkv, d = g.torch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim
+    None); entries of window_lse whose token is no query stay (NaN, where it is
+    made here)."""
+    hq, hkv, d, W = shape.num_q_heads, shape.num_kv_heads, shape.head_dim, shape.window
+    g = _Given(q, None)
+    torch, L = g.torch, lib()
     g.dtype = torch.bfloat16 if shape.dtype == BF16 else torch.float32
-    cuq = None
+    cuq, cup = batch.cu, None
     if queries is not None:
         cuq = np.ascontiguousarray(queries, dtype=np.int32)
         if cuq.shape != batch.cu.shape:
             raise BaconError(ERR_INVALID, f"queries has shape {cuq.shape}, {batch.cu.shape} expected")
-    n, total = int(batch.cu[-1] if cuq is None else cuq[-1]), int(batch.cu[-1])
-    qp, qn, qs = g.rows(q, "q", hq, d)
-    kp, kn, ks = g.rows(k, "k", hkv, d)
-    vp, vn, vs = g.rows(v, "v", hkv, d)
-    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or qn < n or kn < total or vn < total:
+        cup = cuq.ctypes.data
+    n, total, seqs = int(cuq[-1]), int(batch.cu[-1]), len(batch.cu) - 1
+    qn, qs = g.rows(q, "q", hq, d)
+    kn, ks = g.rows(k, "k", hkv, d)
+    vn, vs = g.rows(v, "v", hkv, d)
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or qn < n or kn < total or vn < total or n < 0:
         raise BaconError(ERR_INVALID, f"q, k, v have shapes {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)} for "
                                       f"{n} queries of {total} tokens")
     if out is None:
         out = q.new_empty((n, hq, d))
+        outp = out.data_ptr()
+    else:
+        outp = g.whole(out, "out", (n, hq, d))
     if lse is None and want_lse:
         lse = q.new_empty((n, hq), dtype=torch.float32)
-    seqs = len(batch.cu) - 1
     if window_lse is None and want_window_lse:
-        window_lse = q.new_empty((seqs, hq, shape.window), dtype=torch.float32)
-    outp = g.whole(out, "out", (n, hq, d))
+        window_lse = q.new_full((seqs, hq, W), float("nan"), dtype=torch.float32)
     lsep = g.whole(lse, "lse", (n, hq), torch.float32)
-    winp = g.whole(window_lse, "window_lse", (seqs, hq, shape.window), torch.float32)
-    cup = None if cuq is None else cuq.ctypes.data
-    need = lib().bacon_prompt_work_bytes(C.byref(shape), C.byref(batch.c), cup)
+    winp = g.whole(window_lse, "window_lse", (seqs, hq, W), torch.float32)
+    sp, bp = C.byref(shape), C.byref(batch.c)
+    need = L.bacon_prompt_work_bytes(sp, bp, cup)
     if need and work is None:
         work = q.new_empty(need, dtype=torch.uint8)
     workp = g.whole(work, "work", None, torch.uint8)
-    g.call(lib().bacon_prompt_attend, C.byref(shape), C.byref(batch.c), cup, qp, qs, kp, ks, vp, vs, outp, lsep, winp,
+    g.call(L.bacon_prompt_attend, sp, bp, cup, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, outp, lsep, winp,
            workp, 0 if work is None else work.numel())
     return out, lse, window_lse
 

@@ -13,6 +13,7 @@ constexpr int kPromptMaxBatch = 64;
 struct PromptSeq {
   int k0, keys, q0, queries;
   int unit0, tiles, splits, index;
+  int join0;               // tiles of KV heads before it that are joined
 };
 
 struct PromptArgs {
@@ -24,6 +25,8 @@ struct PromptArgs {
   unsigned group_magic;    // 2^32 / G, rounded up (0 where G is 1)
   float scale;             // 1 / sqrt(d)
   int seqs, units;
+  int joined;              // tiles of KV heads whose parts are joined
+  int fold;                // the second 256 units in the other order
   float2 *part_ml;         // [unit rows] maximum and sum of every part
   float *part_o;           // [unit rows, d]
   PromptSeq s[kPromptMaxBatch];

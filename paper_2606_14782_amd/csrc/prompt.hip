@@ -14,7 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <type_traits>
+#include <cmath>
 
 #include "prompt.h"
 
@@ -70,6 +70,7 @@ __device__ __forceinline__ int keys_seen(const PromptSeq &s, int i) {
 // The longest rows come first, the heads next to each other (and so on dies of
 // their own, whose L2 then serves one head's keys to all its workgroups).
 __device__ __forceinline__ Unit unit_of(const PromptArgs &a, int i) {
+  if (a.fold && i >= 256) i = a.units - 1 - (i - 256);
   Unit u;
   u.s = a.s[seq_of(a, i)];
   const int local = i - u.s.unit0, rest = local / a.Hkv;
@@ -221,18 +222,19 @@ __device__ __forceinline__ void weigh(f32x16 (&s)[N], f32x16 (&o)[E], Weighed &w
 // Keys base + 32 i + 8 (e / 4) + 4 g + e % 4 from `end` on are not seen.
 template <int N>
 __device__ __forceinline__ void mask(f32x16 (&s)[N], int left) {
-  const int g = (threadIdx.x & 63) >> 5;
+  left -= 4 * ((threadIdx.x & 63) >> 5);
+  asm volatile("" : "+v"(left));                             // (else 32 registers hold the keys' numbers)
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-      if (32 * i + 8 * (e >> 2) + 4 * g + (e & 3) >= left) s[i][e] = -INFINITY;
+      if (32 * i + 8 * (e >> 2) + (e & 3) >= left) s[i][e] = -INFINITY;
 }
 
 // Rows of a tile as 16-byte pieces in LDS, piece c of row r at place c ^ f(r):
 // a read of the same piece of 16 or 32 rows then meets every bank once.
 template <int PIECES>
-__device__ __forceinline__ int k_place(int row) { return PIECES == 32 ? row & 31 : PIECES == 16 ? row & 15 : row >> 1 & 7; }
+__device__ __forceinline__ int k_place(int row) { return PIECES == 16 ? row & 15 : row >> 1 & 7; }
 template <int PIECES>
 __device__ __forceinline__ int v_place(int row) {
   return PIECES == 16 ? (row & 3) << 2 : (row >> 1 & 1) << 2;
@@ -242,6 +244,14 @@ __device__ __forceinline__ int v_place(int row) {
 // other buffer are done too.
 __device__ __forceinline__ void tile_barrier() {
   __builtin_amdgcn_s_waitcnt(0x0070);                        // vmcnt 0, lgkmcnt 0
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// The same for LDS traffic alone: loads into registers stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);                        // lgkmcnt 0
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -284,9 +294,9 @@ __device__ __forceinline__ bf16x8 v_piece(const char *vt, int v_at, int j, int e
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Where some keys of a tile are masked, V's values that are not finite count as
-// 0 (a weight of 0 would make NaN of them, in the outputs of queries that do not
-// see their key), and are noted: spoil() then finds who sees them.
+// V's values that are not finite count as 0 where a key may be masked (a weight of
+// 0 would make NaN of them, in the outputs of queries that do not see their key),
+// and are noted: spoil() then finds who sees them.
 __device__ __forceinline__ unsigned finite_halves(unsigned w, unsigned &bad) {
   const unsigned x = ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;      // top bits of those that are not
   bad |= x;
@@ -410,41 +420,79 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
   finish<true, D>(a, u, row, wave * 32 + n, o, w);
 }
 
-// In full precision: 32x32x2 products of floats, tiles of 32 keys.
+// Eight floats as three bf16 parts whose sum they are: two cut off (a mask, and the
+// rest is exact), the last one rounded.
+__device__ __forceinline__ void split8(float (&x)[8], bf16x8 (&part)[3]) {
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302);
+    part[p] = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] -= __uint_as_float(__float_as_uint(x[i]) & 0xFFFF0000u);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) part[2][i] = (__bf16)x[i];
+}
+
+// acc + a b of values in three parts: the six products that 24 bits of the whole
+// can tell, the smallest first.
+__device__ __forceinline__ f32x16 product(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f32x16 acc) {
+#pragma unroll
+  for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+    for (int i = 0; i <= sum; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[sum - i], acc, 0, 0, 0);
+  return acc;
+}
+
+// In full precision: the same products of values in three bf16 parts, six of
+// them for one, which takes three eighths of the time of the matrix
+// instructions for floats.  The workgroup splits a tile of 32 keys into LDS, each
+// thread its share, read into registers while the tile before was computed on.
+// V's values that are not finite count as 0 there and are noted (see spoil).
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
-  constexpr int KEYS = 32, PIECES = D / 4, TILE = KEYS * D * 4, ROW = D * 4;
-  __shared__ __align__(16) char lds[4 * TILE];
+  constexpr int KEYS = 32, PIECES = D / 8, ROW = D * 2, PART = KEYS * ROW, EACH = KEYS * PIECES / 256;
+  __shared__ __align__(16) char lds[6 * PART];               // K's parts, V's
+  __shared__ int noted;
   const Unit u = unit_of(a, blockIdx.x);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int n = lane & 31, g = lane >> 5;
   const Row row = row_of(a, u, wave * 32 + n);
   const char *k = static_cast<const char *>(a.k) + ((int64_t)u.s.k0 * a.k_stride + u.h * D) * 4;
   const char *v = static_cast<const char *>(a.v) + ((int64_t)u.s.k0 * a.v_stride + u.h * D) * 4;
-  const auto k_swap = [](int r) { return r & (PIECES - 1); };
-  const auto v_swap = [](int r) { return r >> 2 & 1 ? 8 : 0; };      // rows 4 g + i of both halves: other banks
-  const unsigned lds_at = (unsigned)(uintptr_t)(LDS char *)lds;
-  Share<KEYS, PIECES> ks, vs;
-  ks.find(a.k_stride * 4, KEYS, wave, k_swap);
-  vs.find(a.v_stride * 4, KEYS, wave, v_swap);
-  const auto ask = [&](int base, int buffer) {
-    const unsigned to = lds_at + buffer * 2 * TILE;
-    if (u.s.keys - base < KEYS) {
-      ks.find(a.k_stride * 4, u.s.keys - base, wave, k_swap);
-      vs.find(a.v_stride * 4, u.s.keys - base, wave, v_swap);
-    }
-    ks.ask(k + base * a.k_stride * 4, to, wave);
-    vs.ask(v + base * a.v_stride * 4, to + TILE, wave);
-  };
-  if (u.from < u.to) ask(u.from, 0);
-  f32x4 q[D / 8];                                            // dimensions 8 i + 4 g .. + 3
-  {
-    const char *p = static_cast<const char *>(a.q) +
-                    (((int64_t)u.s.q0 + row.query) * a.q_stride + (int64_t)row.head * D) * 4 + g * 16;
+  f32x4 kr[EACH][2], vr[EACH][2];
+  const auto ask = [&](int base) {                           // (rows past the last stand for it: they are masked)
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      q[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (row.valid) q[i] = *reinterpret_cast<const f32x4 *>(p + 32 * i);
+    for (int i = 0; i < EACH; ++i) {
+      const int at = i * 256 + t;
+      const int64_t r = min(base + at / PIECES, u.s.keys - 1);
+      const f32x4 *x = reinterpret_cast<const f32x4 *>(k + r * a.k_stride * 4) + at % PIECES * 2;
+      const f32x4 *y = reinterpret_cast<const f32x4 *>(v + r * a.v_stride * 4) + at % PIECES * 2;
+      kr[i][0] = x[0];
+      kr[i][1] = x[1];
+      vr[i][0] = y[0];
+      vr[i][1] = y[1];
+    }
+  };
+  if (u.from < u.to) ask(u.from);
+  if (t == 0) noted = 0;
+  bf16x8 q[D / 16][3];
+  {
+    const float *p = static_cast<const float *>(a.q) + ((int64_t)u.s.q0 + row.query) * a.q_stride + (int64_t)row.head * D + 8 * g;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        f32x4 w = {0.f, 0.f, 0.f, 0.f};
+        if (row.valid) w = *reinterpret_cast<const f32x4 *>(p + 16 * i + 4 * e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[4 * e + j] = w[j];
+      }
+      split8(x, q[i]);
     }
   }
   const int clear = __builtin_amdgcn_readfirstlane(row.valid ? row.end : u.s.keys);
@@ -458,116 +506,225 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
-  int buffer = 0;
-  unsigned bad = 0;
-  for (int base = u.from; base < u.to; base += KEYS, buffer ^= 1) {
-    tile_barrier();
-    if (base + KEYS < u.to) ask(base + KEYS, buffer ^ 1);
+  const int k_at = n * ROW + ((g ^ k_place<PIECES>(n)) << 4);
+  const int key = 4 * g + ((lane & 15) >> 2);
+  const int v_at = key * ROW + (((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ v_place<PIECES>(key)) << 4) + (lane & 1) * 8;
+  for (int base = u.from; base < u.to; base += KEYS) {
+    lds_barrier();                                           // the tile before has been read
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int at = i * 256 + t, r = at / PIECES, c = at % PIECES;
+      float x[8], y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = kr[i][e >> 2][e & 3];
+        y[e] = vr[i][e >> 2][e & 3];
+        if (!finite(y[e])) {
+          y[e] = 0.f;
+          bad = true;
+        }
+      }
+      bf16x8 xp[3], yp[3];
+      split8(x, xp);
+      split8(y, yp);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        *reinterpret_cast<bf16x8 *>(lds + p * PART + r * ROW + ((c ^ k_place<PIECES>(r)) << 4)) = xp[p];
+        *reinterpret_cast<bf16x8 *>(lds + (3 + p) * PART + r * ROW + ((c ^ v_place<PIECES>(r)) << 4)) = yp[p];
+      }
+    }
+    if (bad) noted = 1;
+    ask(base + KEYS);
+    lds_barrier();
     if (base >= far) continue;
-    const char *kt = lds + buffer * 2 * TILE, *vt = kt + TILE;
     f32x16 s[1];
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
 #pragma unroll
-    for (int c = 0; c < D / 8; ++c) {
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(kt + n * ROW + (((2 * c + g) ^ k_swap(n)) << 4));
+    for (int c = 0; c < D / 16; ++c) {
+      bf16x8 x[3];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[c][e], s[0], 0, 0, 0);
+      for (int p = 0; p < 3; ++p) x[p] = *reinterpret_cast<const bf16x8 *>(lds + p * PART + (k_at ^ (c << 5)));
+      s[0] = product(x, q[c], s[0]);
     }
-    const bool masked = base + KEYS > clear;
-    if (masked) mask(s, row.end - base);
+    if (base + KEYS > clear) mask(s, row.end - base);
     weigh(s, o, w, scale_log2);
-    const auto v_value = [&](int j, int e) {
-      const int r = 8 * (j >> 2) + 4 * g + (j & 3);
-      return *reinterpret_cast<const float *>(vt + r * ROW + ((32 * e + n) ^ (g ? 32 : 0)) * 4);
-    };
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
+    for (int j = 0; j < 2; ++j) {                            // 16 keys a step
+      float x[8];
+      bf16x8 p[3];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = s[0][8 * j + e];
+      split8(x, p);
 #pragma unroll
       for (int e = 0; e < D / 32; ++e) {
-        float x = v_value(j, e);
-        if (masked && !finite(x)) {
-          x = 0.f;
-          bad = 1;
-        }
-        o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[0][j], o[e], 0, 0, 0);
+        bf16x8 y[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) y[i] = v_piece<ROW>(lds + (3 + i) * PART, v_at, j, e);
+        o[e] = product(y, p, o[e]);
       }
+    }
   }
-  if (__any(bad != 0)) spoil<false, D>(v, a.v_stride * 4, max(u.from, clear & ~(KEYS - 1)), min(row.end, u.to), o);
+  lds_barrier();
+  if (noted) spoil<false, D>(v, a.v_stride * 4, u.from, min(row.end, u.to), o);
   finish<false, D>(a, u, row, wave * 32 + n, o, w);
 }
 
-// Joins the parts of 128 query rows: D / 4 threads a row.
+// Joins the parts of query rows: D / 4 threads a row, one row each.  Bytes bound
+// it; the parts of a row are asked for four at a time.
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
-  constexpr int TR = D / 4;
-  const Unit u = unit_of(a, blockIdx.x);
-  if (u.split != 0 || u.s.splits == 1) return;
-  const int dim = threadIdx.x % TR * 4;
-  for (int r = threadIdx.x / TR; r < min(kPromptRows, u.rows - u.row0); r += 256 / TR) {
-    const Row row = row_of(a, u, r);
-    float l = 0.f, most = kFloor;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < u.s.splits; ++i) {
-      const int64_t at = ((int64_t)blockIdx.x + i * a.Hkv) * kPromptRows + r;
-      const float2 x = a.part_ml[at];
-      const f32x4 y = *reinterpret_cast<const f32x4 *>(a.part_o + at * D + dim);
-      const float m = fmaxf(most, x.x);
-      const float f = __builtin_amdgcn_exp2f(minus(most, m));
-      const float w = x.x == kNoKey ? 0.f : __builtin_amdgcn_exp2f(minus(x.x, m));
-      l = l * f + x.y * w;
-      acc = acc * f + y * w;
-      most = m;
+  constexpr int TR = D / 4, ROWS = 256 / TR, GROUPS = kPromptRows / ROWS;
+  const int group = blockIdx.x % GROUPS;
+  int lo = 0, hi = a.seqs - 1;
+  const int i = blockIdx.x / GROUPS;                         // a tile of a KV head, of sequences that have parts
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (i >= a.s[mid].join0) lo = mid; else hi = mid - 1;
+  }
+  const PromptSeq &s = a.s[lo];
+  const int tile = (i - s.join0) / a.Hkv, h = (i - s.join0) - tile * a.Hkv;
+  const int first_unit = s.unit0 + tile * s.splits * a.Hkv + h;      // (tiles from the last one on, as in unit_of)
+  const Unit u = unit_of(a, first_unit);
+  const int r = group * ROWS + threadIdx.x / TR, dim = threadIdx.x % TR * 4;
+  const Row row = row_of(a, u, r);
+  if (!row.valid) return;
+  const float2 *ml = a.part_ml + (int64_t)first_unit * kPromptRows + r;
+  const float *po = a.part_o + ((int64_t)first_unit * kPromptRows + r) * D + dim;
+  const int64_t step = (int64_t)a.Hkv * kPromptRows;
+  float l = 0.f, most = kFloor;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < s.splits; p += 4) {
+    float2 x[4];
+    f32x4 y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t at = min(p + j, s.splits - 1) * step;
+      x[j] = ml[at];
+      y[j] = *reinterpret_cast<const f32x4 *>(po + at * D);
     }
-    const bool none = row.end <= 0;
-    const float sum = none ? 1.f : l > 0.f ? l : __builtin_nanf(""), inv = 1.f / sum;
-    acc = none ? f32x4{0.f, 0.f, 0.f, 0.f} : acc * inv;
-    const int64_t token = u.s.q0 + row.query, at = (token * a.Hq + row.head) * D + dim;
-    if constexpr (BF16)
-      *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(a.out) + at) = __builtin_convertvector(acc, bf16x4);
-    else
-      *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at) = acc;
-    if (dim == 0) {
-      const float lse = none ? -INFINITY : (most + __log2f(sum)) * kLn2;
-      if (a.lse) a.lse[token * a.Hq + row.head] = lse;
-      const int w = a.W - u.s.queries + row.query;
-      if (a.window && w >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + w] = lse;
+    float m = most;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (p + j >= s.splits) x[j] = make_float2(kNoKey, 0.f);
+      m = fmaxf(m, x[j].x);
     }
+    const float f = __builtin_amdgcn_exp2f(minus(most, m));
+    l *= f;
+    acc *= f;
+    most = m;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (x[j].x == kNoKey) continue;
+      const float w = __builtin_amdgcn_exp2f(minus(x[j].x, m));
+      l += x[j].y * w;
+      acc += y[j] * w;
+    }
+  }
+  const bool none = row.end <= 0;
+  const float sum = none ? 1.f : l > 0.f ? l : __builtin_nanf(""), inv = 1.f / sum;
+  acc = none ? f32x4{0.f, 0.f, 0.f, 0.f} : acc * inv;
+  const int64_t token = u.s.q0 + row.query, at = (token * a.Hq + row.head) * D + dim;
+  if constexpr (BF16)
+    *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(a.out) + at) = __builtin_convertvector(acc, bf16x4);
+  else
+    *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at) = acc;
+  if (dim == 0) {
+    const float lse = none ? -INFINITY : (most + __log2f(sum)) * kLn2;
+    if (a.lse) a.lse[token * a.Hq + row.head] = lse;
+    const int place = a.W - u.s.queries + row.query;
+    if (a.window && place >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + place] = lse;
   }
 }
 
 }  // namespace
 
+// Microseconds of a step (a tile of keys) of a workgroup that has a compute unit to
+// itself, of one of two that share it, and of the whole GPU for 256 steps.
+struct StepTimes {
+  double alone, shared, all;
+};
+
+static StepTimes step_times(int head_dim, bool bf16) {
+  if (bf16) return head_dim == 128 ? StepTimes{1.5, 2.0, 1.05} : StepTimes{0.95, 1.2, 0.85};
+  return head_dim == 128 ? StepTimes{3.3, 4.5, 3.4} : StepTimes{1.47, 1.9, 1.4};
+}
+
+// A batch takes what its longest workgroup does, or what all of them do together; a
+// workgroup costs five steps besides its own, and parts, alike in length, end in
+// rounds of 512 (us, forecast and measured: 1K tokens of 28 heads 31.5 and 31.9;
+// 512 queries over 8K keys 199 and 195, in four parts 74 and 75, in five 116 and
+// 99, in eight 84 and 81).
+static double forecast(const PromptArgs *a, const StepTimes &t, int keys_a_step, int chunk) {
+  double steps = 0, units = 0, longest = 0;
+  for (int i = 0; i < a->seqs; ++i) {
+    const PromptSeq &s = a->s[i];
+    const double seen = 0.5 * (std::max(0, s.keys - s.queries) + s.keys), n = (double)s.tiles * a->Hkv;
+    steps += n * seen / keys_a_step;
+    units += n * (chunk ? std::max(1.0, std::min(seen / chunk + 0.5, std::ceil((double)s.keys / chunk))) : 1.0);
+    longest = std::max(longest, (double)(chunk ? std::min(s.keys, chunk) : s.keys) / keys_a_step);
+  }
+  double last = (longest + 5) * t.alone;
+  if (chunk) {
+    const double full = std::floor(units / 512), rest = units - 512 * full;
+    last = (longest + 5) * (full * t.shared + (rest > 256 ? t.shared : rest > 0 ? t.alone : 0));
+  } else if (units > 256) {
+    last += (steps / units + 5) * (t.shared - t.alone);      // beside one of mean length
+  }
+  return std::max(last, (steps + 5 * units) / 256 * t.all);
+}
+
 PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
   PromptPlan p{};
-  double total = 0;
   int longest = 0;
+  int64_t rows = 0;
   for (int i = 0; i < a->seqs; ++i) {
     PromptSeq &s = a->s[i];
-    s.tiles = (int)(((int64_t)s.queries * a->G + kPromptRows - 1) / kPromptRows);
-    const double first = std::max(0, s.keys - s.queries);
-    total += 0.5 * (first + s.keys) * s.tiles * a->Hkv;
+    const int64_t r = (int64_t)s.queries * a->G;
+    s.tiles = (int)((r + kPromptRows - 1) / kPromptRows);
     longest = std::max(longest, s.keys);
+    rows += r * a->Hkv;
   }
-  const double slots = 512, ideal = total / slots;
-  const int chunk = longest <= 2 * ideal ? 0 : std::max(256, ((int)ideal + 63) / 64 * 64);
-  int64_t units = 0;
-  bool parts = false;
+  // The parts that the longest keys are divided into: as many as make the forecast
+  // least, with the joining launch's time: 5 us and what its parts' bytes take
+  // (512 parts of 128 rows of 128 dimensions 7.6 us, 1024 12.4).
+  const StepTimes times = step_times(head_dim, bf16);
+  const int keys_a_step = bf16 ? 64 : 32;
+  double best = forecast(a, times, keys_a_step, 0);
+  int chunk = 0;
+  for (int parts = 2; parts <= 64 && longest > 64; parts += std::max(1, parts / 4)) {
+    const int c = ((longest + parts - 1) / parts + 63) / 64 * 64;
+    const double time = forecast(a, times, keys_a_step, c) + 5 + 0.15 * parts + 7e-5 * head_dim / 128 * rows * parts;
+    if (time < best) {
+      best = time;
+      chunk = c;
+    }
+    if (c == 64) break;
+  }
+  int64_t units = 0, joined = 0;
   std::sort(a->s, a->s + a->seqs, [](const PromptSeq &x, const PromptSeq &y) {
     return x.keys != y.keys ? x.keys > y.keys : x.index < y.index;
   });
   for (int i = 0; i < a->seqs; ++i) {
     PromptSeq &s = a->s[i];
     s.splits = chunk ? std::max(1, (s.keys + chunk - 1) / chunk) : 1;
-    parts |= s.splits > 1;
     s.unit0 = (int)std::min<int64_t>(units, 0x7FFFFFFF);
+    s.join0 = (int)std::min<int64_t>(joined, 0x7FFFFFFF);
     units += (int64_t)s.tiles * s.splits * a->Hkv;
+    if (s.splits > 1) joined += (int64_t)s.tiles * a->Hkv;   // (the longest come first: those behind have one part)
   }
   a->units = (int)std::min<int64_t>(units, 0x7FFFFFFF);
-  if (parts) {
-    const size_t rows = (size_t)units * kPromptRows;
-    p.ml_bytes = rows * sizeof(float2);
-    p.bytes = p.ml_bytes + rows * head_dim * sizeof(float);
+  a->joined = (int)std::min<int64_t>(joined, 0x7FFFFFFF);
+  // Two workgroups a compute unit, all there at once: the second 256 in the other
+  // order, so that the longest have the shortest beside them (2K tokens of 32 heads
+  // 56 us, else 62; with more of them the longest first are best: 3500 tokens 119
+  // and 144).
+  a->fold = !joined && units > 256 && units <= 512;
+  if (joined) {
+    const size_t part_rows = (size_t)units * kPromptRows;
+    p.ml_bytes = part_rows * sizeof(float2);
+    p.bytes = p.ml_bytes + part_rows * head_dim * sizeof(float);
   }
   return p;
 }
@@ -582,17 +739,16 @@ hipError_t launch_prompt(const PromptArgs &a, bool bf16, int head_dim, hipStream
     hipLaunchKernelGGL((k_prompt_fp32<128>), grid, threads, 0, s, a);
   else
     hipLaunchKernelGGL((k_prompt_fp32<64>), grid, threads, 0, s, a);
-  bool parts = false;
-  for (int i = 0; i < a.seqs; ++i) parts |= a.s[i].splits > 1;
-  if (parts) {
+  if (a.joined) {
+    const dim3 join((unsigned)a.joined * (kPromptRows * head_dim / 4 / 256));
     if (bf16 && head_dim == 128)
-      hipLaunchKernelGGL((k_prompt_join<true, 128>), grid, threads, 0, s, a);
+      hipLaunchKernelGGL((k_prompt_join<true, 128>), join, threads, 0, s, a);
     else if (bf16)
-      hipLaunchKernelGGL((k_prompt_join<true, 64>), grid, threads, 0, s, a);
+      hipLaunchKernelGGL((k_prompt_join<true, 64>), join, threads, 0, s, a);
     else if (head_dim == 128)
-      hipLaunchKernelGGL((k_prompt_join<false, 128>), grid, threads, 0, s, a);
+      hipLaunchKernelGGL((k_prompt_join<false, 128>), join, threads, 0, s, a);
     else
-      hipLaunchKernelGGL((k_prompt_join<false, 64>), grid, threads, 0, s, a);
+      hipLaunchKernelGGL((k_prompt_join<false, 64>), join, threads, 0, s, a);
   }
   return hipGetLastError();
 }
