@@ -26,7 +26,6 @@ struct PromptArgs {
   float scale;             // 1 / sqrt(d)
   int seqs, units;
   int joined;              // tiles of KV heads whose parts are joined
-  int fold;                // the second 256 units in the other order
   float2 *part_ml;         // [unit rows] maximum and sum of every part
   float *part_o;           // [unit rows, d]
   PromptSeq s[kPromptMaxBatch];

@@ -70,7 +70,6 @@ __device__ __forceinline__ int keys_seen(const PromptSeq &s, int i) {
 // The longest rows come first, the heads next to each other (and so on dies of
 // their own, whose L2 then serves one head's keys to all its workgroups).
 __device__ __forceinline__ Unit unit_of(const PromptArgs &a, int i) {
-  if (a.fold && i >= 256) i = a.units - 1 - (i - 256);
   Unit u;
   u.s = a.s[seq_of(a, i)];
   const int local = i - u.s.unit0, rest = local / a.Hkv;
@@ -178,6 +177,8 @@ __device__ __forceinline__ void finish(const PromptArgs &a, const Unit &u, const
   }
 }
 
+// A tile's logits become weights.  A row's maximum moves where they pass it by more
+// than kSlack, each row's by itself: its results depend on no other.
 template <int N, int E>
 __device__ __forceinline__ void weigh(f32x16 (&s)[N], f32x16 (&o)[E], Weighed &w, float scale_log2) {
   float top = max3(s[0][0], s[0][1], s[0][2]);
@@ -187,7 +188,7 @@ __device__ __forceinline__ void weigh(f32x16 (&s)[N], f32x16 (&o)[E], Weighed &w
     for (int e = i ? 0 : 3; e + 1 < 16; e += 2) top = max3(top, s[i][e], s[i][e + 1]);
   top = __builtin_elementwise_maximum(top, s[0][15]);
   top = __builtin_elementwise_maximum(top, other_half(top)) * scale_log2;
-  const bool moves = top > w.at + kSlack;                    // (each row by itself: its results depend on no other)
+  const bool moves = top > w.at + kSlack;
   if (__any(moves)) {
     const float next = moves ? top : w.at, f = __builtin_amdgcn_exp2f(minus(w.at, next));
     w.at = next;
@@ -575,7 +576,8 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
 // it; the parts of a row are asked for four at a time.
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
-  constexpr int TR = D / 4, ROWS = 256 / TR, GROUPS = kPromptRows / ROWS;
+  constexpr int TR = D / 4, ROWS = 256 / TR;
+  constexpr int GROUPS = kPromptRows / ROWS;
   const int group = blockIdx.x % GROUPS;
   int lo = 0, hi = a.seqs - 1;
   const int i = blockIdx.x / GROUPS;                         // a tile of a KV head, of sequences that have parts
@@ -716,11 +718,6 @@ PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
   }
   a->units = (int)std::min<int64_t>(units, 0x7FFFFFFF);
   a->joined = (int)std::min<int64_t>(joined, 0x7FFFFFFF);
-  // Two workgroups a compute unit, all there at once: the second 256 in the other
-  // order, so that the longest have the shortest beside them (2K tokens of 32 heads
-  // 56 us, else 62; with more of them the longest first are best: 3500 tokens 119
-  // and 144).
-  a->fold = !joined && units > 256 && units <= 512;
   if (joined) {
     const size_t part_rows = (size_t)units * kPromptRows;
     p.ml_bytes = part_rows * sizeof(float2);
