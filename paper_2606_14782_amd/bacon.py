@@ -633,7 +633,7 @@ def bacon_prompt_attend(shape: Shape, batch: BatchLayout, q, k, v, queries=None,
         raise BaconError(ERR_INVALID, f"q, k, v have shapes {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)} for "
                                       f"{n} queries of {total} tokens")
     if out is None:
-        out = q.new_empty((n, hq, d))
+        out = g.like(q) if qn == n else q.new_empty((n, hq, d))
         outp = out.data_ptr()
     else:
         outp = g.whole(out, "out", (n, hq, d))
@@ -830,10 +830,9 @@ class Cache:
         if out is None:
             if min(shape) < 1:
                 raise BaconError(ERR_INVALID, f"a load of shape {shape}")
-            both = self.scales.new_empty((2, *shape), dtype=self.torch_dtype)
-            k, v = both.unbind(0)
-            kp = both.data_ptr()
-            vp = kp + both.nbytes // 2
+            k = self.scales.new_empty(shape, dtype=self.torch_dtype)
+            v = self._torch.empty_like(k)
+            kp, vp = k.data_ptr(), v.data_ptr()
         else:
             k, v = out
             kp, vp = (self._whole(k, "k_out", self.torch_dtype, shape), self._whole(v, "v_out", self.torch_dtype, shape))
@@ -850,7 +849,7 @@ class Cache:
         """Outputs and scratch of an attend, made where they are not given, and their pointers."""
         torch, shape = self._torch, (b, n, self._hq, self._d)
         if out is None:
-            out = q.new_empty(shape)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
             outp = out.data_ptr()
         else:
             outp = self._whole(out, "out", self.torch_dtype, shape)

@@ -173,3 +173,68 @@ def test_streams_and_graphs():
     T.test_two_streams_attend_beside_each_other()
     T.test_two_captured_graphs_replay_beside_each_other()
     T.test_tables_and_store_in_a_captured_graph()
+
+
+@pytest.mark.parametrize("lens", [[[40, 33], [100, 7]], [[4000, 2100], [9, 100]]])
+def test_captured_step_replays(lens):
+    T.test_captured_step_replays(lens)
+
+
+@pytest.mark.parametrize("dtype,d,bt,G,n,part", [
+    ("bf16", 128, 64, 4, 4, 64), ("bf16", 64, 16, 1, 16, 64), ("fp32", 64, 32, 5, 3, 64), ("bf16", 128, 64, 5, 6, 256),
+    ("fp32", 128, 32, 8, 4, 256)])
+def test_step_over_the_borders_of_parts(dtype, d, bt, G, n, part):
+    T.test_step_over_the_borders_of_parts(dtype, d, bt, G, n, part)
+
+
+@pytest.mark.parametrize("dtype,d,G,n", [("bf16", 128, 4, 1), ("fp32", 64, 7, 3)])
+@pytest.mark.parametrize("lens", [[[40, 1], [300, 65]], [[4100, 2000], [3, 1000]]])
+def test_a_query_that_is_not_finite_is_nan_alone(dtype, d, G, n, lens):
+    T.test_a_query_that_is_not_finite_is_nan_alone(dtype, d, G, n, lens)
+
+
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("fp32", 64, 1), ("bf16", 64, 20)])
+@pytest.mark.parametrize("rows", [1, 300, 5000])
+def test_attend_of_logits_as_large_as_floats(dtype, d, G, rows):
+    """Logits of either sign up to 2^120 of two kinds of key, 4 and 6 (exact in e2m1):
+    the larger ones' weights are 1, the others' 0.  The bounds are those of the
+    8-bit cache's test of the same: sums, and the output's rounding."""
+    import math
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(rows)
+    for power in (40, 104, 117):
+        for sign in (1, -1):
+            q = torch.zeros(1, 1, G, d, device="cuda")
+            q[..., 0] = sign * 2.0 ** (power - power // 2)
+            kind = rng.integers(0, 2, rows)
+            key = np.where(kind == 1, 6.0, 4.0) * 2.0 ** (power // 2)
+            k = torch.zeros(rows, 1, d, device="cuda")
+            k[:, 0, 0] = torch.from_numpy(key.astype(np.float32)).cuda()
+            v = torch.from_numpy(rng.standard_normal((rows, 1, d)).astype(np.float32)).cuda()
+            q, k, v = (x.to(torch.bfloat16 if dtype == "bf16" else torch.float32) for x in (q, k, v))
+            c = _cache4(1, G, 1, d, 1, 32, 1, rows, rows // 32 + 2, dtype)
+            batch = bacon.BatchLayout([0, rows], [max(1, rows - 1)])
+            c.bacon_cache_tables(batch)
+            c.bacon_cache_store(batch, [k], [v])
+            out, lse = c.bacon_cache_attend(0, q, want_lse=True)
+            s = sign * 2.0 ** (power - power // 2) * key / math.sqrt(d)
+            won = A.held(T._np(v)[:, 0])[s == s.max()]
+            tol = A.HALF[dtype] * np.abs(won.mean(0)) + (2 * (rows / 16 + 64) + 4) * A.h * np.abs(won).mean(0) * 1.01
+            assert np.all(np.abs(T._np(out)[0, 0] - won.mean(0)) <= tol), (power, sign)
+            want = s.max() + math.log(len(won))
+            assert np.all(np.abs(T._np(lse)[0, 0] - want) <= 8 * A.h * np.abs(want)), (power, sign)
+
+
+@pytest.mark.parametrize("dtype,G,n", [("bf16", 4, 1), ("fp32", 2, 3)])
+def test_divided_step_without_room_attends_over_what_is_there(dtype, G, n):
+    T.test_divided_step_without_room_attends_over_what_is_there(dtype, G, n)
+
+
+def test_rows_not_named_and_padding():
+    T.test_rows_that_are_not_named_stay()
+    T.test_padding_may_hold_anything([[40, 33], [100, 7]])
+
+
+def test_attend_over_the_longest():
+    T.test_attend_over_the_longest()
