@@ -53,13 +53,15 @@ __device__ __forceinline__ int division(int i, unsigned magic) {     // i / G fo
   return magic ? (int)__umulhi((unsigned)i, magic) : i;
 }
 
-__device__ __forceinline__ int seq_of(const PromptArgs &a, int unit) {
-  int lo = 0, hi = a.seqs - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (unit >= a.s[mid].unit0) lo = mid; else hi = mid - 1;
-  }
-  return lo;
+// The last sequence whose first unit (or joined tile) is not past i: the lanes look
+// at one each, in one round trip to the arguments (16 prompts of 100 tokens 17.1 us
+// -> 15.9).
+template <int PromptSeq::*FIRST>
+__device__ __forceinline__ int seq_of(const PromptArgs &a, int i) {
+  if (a.seqs == 1) return 0;
+  const int lane = threadIdx.x & 63;
+  const bool at = lane < a.seqs && i >= a.s[lane].*FIRST;
+  return __popcll(__ballot(at)) - 1;
 }
 
 // The keys that query i of a sequence sees.
@@ -71,7 +73,7 @@ __device__ __forceinline__ int keys_seen(const PromptSeq &s, int i) {
 // their own, whose L2 then serves one head's keys to all its workgroups).
 __device__ __forceinline__ Unit unit_of(const PromptArgs &a, int i) {
   Unit u;
-  u.s = a.s[seq_of(a, i)];
+  u.s = a.s[seq_of<&PromptSeq::unit0>(a, i)];
   const int local = i - u.s.unit0, rest = local / a.Hkv;
   u.h = local - rest * a.Hkv;
   const int from_last = rest / u.s.splits;
@@ -295,12 +297,9 @@ __device__ __forceinline__ bf16x8 v_piece(const char *vt, int v_at, int j, int e
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// V's values that are not finite count as 0 where a key may be masked (a weight of
-// 0 would make NaN of them, in the outputs of queries that do not see their key),
-// and are noted: spoil() then finds who sees them.
-__device__ __forceinline__ unsigned finite_halves(unsigned w, unsigned &bad) {
+// Halves of a word with those that are infinite or NaN as 0.
+__device__ __forceinline__ unsigned finite_halves(unsigned w) {
   const unsigned x = ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;      // top bits of those that are not
-  bad |= x;
   return w & ~((x << 1) - (x >> 15));
 }
 
@@ -327,12 +326,15 @@ __device__ __forceinline__ void spoil(const char *v, int64_t stride_bytes, int f
   }
 }
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
+// A unit's outputs; false where one came out that is not finite, and nothing is
+// handed on.  That may be by a masked key's value (0 times it): CAREFUL counts such
+// values as 0 in tiles that mask keys, and finds what sees them.  (Looking for them
+// at once took 1.5 us of a masked tile's 3.)
+template <int D, bool CAREFUL>
+__device__ __forceinline__ bool attend_unit(const PromptArgs &a, int unit, int t, char *lds) {
   constexpr int KEYS = 64, PIECES = D / 8, TILE = KEYS * D * 2, ROW = D * 2;
-  __shared__ __align__(16) char lds[4 * TILE];               // K, V of two tiles
-  const Unit u = unit_of(a, blockIdx.x);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Unit u = unit_of(a, unit);
+  const int lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int n = lane & 31, g = lane >> 5;
   const Row row = row_of(a, u, wave * 32 + n);
   const char *k = static_cast<const char *>(a.k) + ((int64_t)u.s.k0 * a.k_stride + u.h * D) * 2;
@@ -350,8 +352,8 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
     ks.ask(k + base * a.k_stride * 2, to, wave);
     vs.ask(v + base * a.v_stride * 2, to + TILE, wave);
   };
-  if (u.from < u.to) ask(u.from, 0);
   bf16x8 q[D / 16];
+  if (u.from < u.to) ask(u.from, 0);
   {
     const char *p = static_cast<const char *>(a.q) +
                     (((int64_t)u.s.q0 + row.query) * a.q_stride + (int64_t)row.head * D) * 2 + g * 16;
@@ -368,18 +370,17 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
       min(u.to, u.row0 + wave * 32 >= u.rows ? 0
                                              : keys_seen(u.s, (min(u.row0 + wave * 32 + 32, u.rows) - 1) / a.G)));
   const float scale_log2 = a.scale * kLog2e;
+  // this lane's places in a tile: K rows n (+ 32), V rows 4 g + n / 4 % 4 (+ 8 ..)
+  const int k_at = n * ROW + ((g ^ k_place<PIECES>(n)) << 4);
+  const int key = 4 * g + ((lane & 15) >> 2);
+  const int v_at = key * ROW + (((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ v_place<PIECES>(key)) << 4) + (lane & 1) * 8;
   f32x16 o[D / 32];
   Weighed w;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
-  // this lane's places in a tile: K rows n (+ 32), V rows 4 g + n / 4 % 4 (+ 8 ..)
-  const int k_at = n * ROW + ((g ^ k_place<PIECES>(n)) << 4);
-  const int key = 4 * g + ((lane & 15) >> 2);
-  const int v_at = key * ROW + (((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ v_place<PIECES>(key)) << 4) + (lane & 1) * 8;
   int buffer = 0;
-  unsigned bad = 0;
   for (int base = u.from; base < u.to; base += KEYS, buffer ^= 1) {
     tile_barrier();
     if (base + KEYS < u.to) ask(base + KEYS, buffer ^ 1);
@@ -399,26 +400,52 @@ __global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
     const bool masked = base + KEYS > clear;
     if (masked) mask(s, row.end - base);
     weigh(s, o, w, scale_log2);
+    const auto product = [&](auto value) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {                            // 16 keys a step
-      bf16x8 p;
+      for (int j = 0; j < 4; ++j) {                        // 16 keys a step
+        bf16x8 p;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[j >> 1][8 * (j & 1) + e];
+        for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[j >> 1][8 * (j & 1) + e];
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e) {
-        bf16x8 x = v_piece<ROW>(vt, v_at, j, e);
-        if (masked) {
-          u32x4 y = __builtin_bit_cast(u32x4, x);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = finite_halves(y[i], bad);
-          x = __builtin_bit_cast(bf16x8, y);
-        }
-        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p, o[e], 0, 0, 0);
+        for (int e = 0; e < D / 32; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(j, e), p, o[e], 0, 0, 0);
       }
-    }
+    };
+    if (CAREFUL && masked)
+      product([&](int j, int e) {
+        u32x4 y = __builtin_bit_cast(u32x4, v_piece<ROW>(vt, v_at, j, e));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = finite_halves(y[i]);
+        return __builtin_bit_cast(bf16x8, y);
+      });
+    else
+      product([&](int j, int e) { return v_piece<ROW>(vt, v_at, j, e); });
   }
-  if (__any(bad != 0)) spoil<true, D>(v, a.v_stride * 2, max(u.from, clear & ~(KEYS - 1)), min(row.end, u.to), o);
+  if constexpr (CAREFUL) {
+    spoil<true, D>(v, a.v_stride * 2, max(u.from, clear & ~(KEYS - 1)), min(row.end, u.to), o);
+  } else {
+    float most = 0.f;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) most = max3(most, __builtin_fabsf(o[e][i]), __builtin_fabsf(o[e][i + 1]));
+    int *stop = reinterpret_cast<int *>(lds + buffer * 2 * TILE);   // (the buffer that nothing reads or fills now)
+    if (lane == 0) stop[wave] = 0;
+    if (row.valid && !finite(most)) stop[wave] = 1;
+    tile_barrier();
+    if (stop[0] | stop[1] | stop[2] | stop[3]) return false;
+  }
   finish<true, D>(a, u, row, wave * 32 + n, o, w);
+  return true;
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
+  __shared__ __align__(16) char lds[4 * 64 * D * 2];         // K, V of two tiles
+  if (attend_unit<D, false>(a, blockIdx.x, threadIdx.x, lds)) return;
+  tile_barrier();                                            // every wave has seen that
+  int unit = blockIdx.x, t = threadIdx.x;                    // (as if others: else the first time keeps what the
+  asm volatile("" : "+s"(unit), "+v"(t));                    // second needs)
+  attend_unit<D, true>(a, unit, t, lds);
 }
 
 // Eight floats as three bf16 parts whose sum they are: two cut off (a mask, and the
@@ -452,7 +479,8 @@ __device__ __forceinline__ f32x16 product(const bf16x8 (&a)[3], const bf16x8 (&b
 // them for one, which takes three eighths of the time of the matrix
 // instructions for floats.  The workgroup splits a tile of 32 keys into LDS, each
 // thread its share, read into registers while the tile before was computed on.
-// V's values that are not finite count as 0 there and are noted (see spoil).
+// V's values that are not finite count as 0 there and are noted: spoil finds who sees
+// them.
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
   constexpr int KEYS = 32, PIECES = D / 8, ROW = D * 2, PART = KEYS * ROW, EACH = KEYS * PIECES / 256;
@@ -579,13 +607,8 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
   constexpr int TR = D / 4, ROWS = 256 / TR;
   constexpr int GROUPS = kPromptRows / ROWS;
   const int group = blockIdx.x % GROUPS;
-  int lo = 0, hi = a.seqs - 1;
   const int i = blockIdx.x / GROUPS;                         // a tile of a KV head, of sequences that have parts
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (i >= a.s[mid].join0) lo = mid; else hi = mid - 1;
-  }
-  const PromptSeq &s = a.s[lo];
+  const PromptSeq &s = a.s[seq_of<&PromptSeq::join0>(a, i)];
   const int tile = (i - s.join0) / a.Hkv, h = (i - s.join0) - tile * a.Hkv;
   const int first_unit = s.unit0 + tile * s.splits * a.Hkv + h;      // (tiles from the last one on, as in unit_of)
   const Unit u = unit_of(a, first_unit);
