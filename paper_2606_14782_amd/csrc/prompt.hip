@@ -672,15 +672,17 @@ struct StepTimes {
 };
 
 static StepTimes step_times(int head_dim, bool bf16) {
-  if (bf16) return head_dim == 128 ? StepTimes{1.5, 2.0, 1.05} : StepTimes{0.95, 1.2, 0.85};
-  return head_dim == 128 ? StepTimes{3.3, 4.5, 3.4} : StepTimes{1.47, 1.9, 1.4};
+  if (bf16) return head_dim == 128 ? StepTimes{1.17, 2.0, 1.0} : StepTimes{0.7, 0.95, 0.95};
+  return head_dim == 128 ? StepTimes{3.2, 5.1, 2.35} : StepTimes{1.4, 1.9, 1.0};
 }
 
 // A batch takes what its longest workgroup does, or what all of them do together; a
-// workgroup costs five steps besides its own, and parts, alike in length, end in
-// rounds of 512 (us, forecast and measured: 1K tokens of 28 heads 31.5 and 31.9;
-// 512 queries over 8K keys 199 and 195, in four parts 74 and 75, in five 116 and
-// 99, in eight 84 and 81).
+// workgroup costs seven steps besides its own, and parts, alike in length, end in
+// rounds of 512 (us, forecast and measured: 1K tokens of 28 heads 27 and 28; 512
+// queries over 8K keys 158 and 156, in four parts 78 and 75, in five 101 and 90, in
+// eight 92 and 83).
+constexpr double kUnitSteps = 7;
+
 static double forecast(const PromptArgs *a, const StepTimes &t, int keys_a_step, int chunk) {
   double steps = 0, units = 0, longest = 0;
   for (int i = 0; i < a->seqs; ++i) {
@@ -690,14 +692,14 @@ static double forecast(const PromptArgs *a, const StepTimes &t, int keys_a_step,
     units += n * (chunk ? std::max(1.0, std::min(seen / chunk + 0.5, std::ceil((double)s.keys / chunk))) : 1.0);
     longest = std::max(longest, (double)(chunk ? std::min(s.keys, chunk) : s.keys) / keys_a_step);
   }
-  double last = (longest + 5) * t.alone;
+  double last = (longest + kUnitSteps) * t.alone;
   if (chunk) {
     const double full = std::floor(units / 512), rest = units - 512 * full;
-    last = (longest + 5) * (full * t.shared + (rest > 256 ? t.shared : rest > 0 ? t.alone : 0));
+    last = (longest + kUnitSteps) * (full * t.shared + (rest > 256 ? t.shared : rest > 0 ? t.alone : 0));
   } else if (units > 256) {
-    last += (steps / units + 5) * (t.shared - t.alone);      // beside one of mean length
+    last += (steps / units + kUnitSteps) * (t.shared - t.alone);      // beside one of mean length
   }
-  return std::max(last, (steps + 5 * units) / 256 * t.all);
+  return std::max(last, (steps + kUnitSteps * units) / 256 * t.all);
 }
 
 PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
