@@ -679,7 +679,7 @@ static StepTimes step_times(int head_dim, bool bf16) {
 // A batch takes what its longest workgroup does, or what all of them do together; a
 // workgroup costs seven steps besides its own, and parts, alike in length, end in
 // rounds of 512 (us, forecast and measured: 1K tokens of 28 heads 27 and 28; 512
-// queries over 8K keys 158 and 156, in four parts 78 and 75, in five 101 and 90, in
+// queries over 8K keys 158 and 156, in four parts 78 and 75, in five 105 and 90, in
 // eight 92 and 83).
 constexpr double kUnitSteps = 7;
 
@@ -720,7 +720,8 @@ PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
   const int keys_a_step = bf16 ? 64 : 32;
   double best = forecast(a, times, keys_a_step, 0);
   int chunk = 0;
-  for (int parts = 2; parts <= 64 && longest > 64; parts += std::max(1, parts / 4)) {
+  // (Batches of 2^24 query rows fill the GPU; their join would pass a launch's threads.)
+  for (int parts = 2; parts <= 64 && longest > 64 && rows <= 1 << 24; parts += std::max(1, parts / 4)) {
     const int c = ((longest + parts - 1) / parts + 63) / 64 * 64;
     const double time = forecast(a, times, keys_a_step, c) + 5 + 0.15 * parts + 7e-5 * head_dim / 128 * rows * parts;
     if (time < best) {
