@@ -646,15 +646,17 @@ bacon_status bacon_rotate(const bacon_rotary *r, int64_t tokens, const int32_t *
  * the window's tokens (token N_b - W + w is entry w); entries whose token is not
  * a query of this call are left as they were, so that chunks fill them in turn.
  *
- * Logits, maxima, sums and outputs are held in 32 bits.  In bfloat16 a weight
+ * Logits, maxima, sums and outputs are held in 32 bits (|V| up to 2^88 passes no
+ * sum's range).  In bfloat16 a weight
  * enters the second product rounded to bfloat16 (2^-9 of itself at most, as much as
  * the output's own rounding, and independent from key to key).  A query one of
  * whose logits is NaN or +infinity, or whose logits are all -infinity, gives NaN;
- * where K or V of a key that is seen is not finite, so are its queries' outputs.
+ * so does, in float32, one that sees a K that is not finite.  Where V of a key
+ * that is seen is not finite, its queries' outputs of that dimension are not.
  * What lies in rows that no query sees reaches nothing.
  * d_work: scratch of bacon_prompt_work_bytes (0: may be NULL), 256-byte aligned,
- * of this call alone until its work is done.  The arrays of `batch` and
- * cu_queries are read during the call.  budgets are not read (may be NULL). */
+ * of this call alone until its work is done.  Outputs and work overlap nothing
+ * else of the call.  The arrays of `batch` and cu_queries are read during the call.  budgets are not read (may be NULL). */
 bacon_status bacon_prompt_attend(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries,
                                  const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride,
                                  const void *d_v, int64_t v_stride, void *d_out, float *d_lse, float *d_window_lse,

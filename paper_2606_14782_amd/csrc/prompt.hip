@@ -479,8 +479,8 @@ __device__ __forceinline__ f32x16 product(const bf16x8 (&a)[3], const bf16x8 (&b
 // them for one, which takes three eighths of the time of the matrix
 // instructions for floats.  The workgroup splits a tile of 32 keys into LDS, each
 // thread its share, read into registers while the tile before was computed on.
-// V's values that are not finite count as 0 there and are noted: spoil finds who sees
-// them.
+// In tiles that mask keys V's values that are not finite count as 0 and are noted:
+// spoil finds who sees them.
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
   constexpr int KEYS = 32, PIECES = D / 8, ROW = D * 2, PART = KEYS * ROW, EACH = KEYS * PIECES / 256;
@@ -528,6 +528,7 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
   const int far = __builtin_amdgcn_readfirstlane(
       min(u.to, u.row0 + wave * 32 >= u.rows ? 0
                                              : keys_seen(u.s, (min(u.row0 + wave * 32 + 32, u.rows) - 1) / a.G)));
+  const int all_clear = keys_seen(u.s, u.row0 / a.G);        // below this key none of the workgroup's waves masks one
   const float scale_log2 = a.scale * kLog2e;
   f32x16 o[D / 32];
   Weighed w;
@@ -541,6 +542,15 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
   for (int base = u.from; base < u.to; base += KEYS) {
     lds_barrier();                                           // the tile before has been read
     bool bad = false;
+    if (base + KEYS > all_clear)
+#pragma unroll
+      for (int i = 0; i < EACH; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!finite(vr[i][e >> 2][e & 3])) {
+            vr[i][e >> 2][e & 3] = 0.f;
+            bad = true;
+          }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const int at = i * 256 + t, r = at / PIECES, c = at % PIECES;
@@ -549,10 +559,6 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
       for (int e = 0; e < 8; ++e) {
         x[e] = kr[i][e >> 2][e & 3];
         y[e] = vr[i][e >> 2][e & 3];
-        if (!finite(y[e])) {
-          y[e] = 0.f;
-          bad = true;
-        }
       }
       bf16x8 xp[3], yp[3];
       split8(x, xp);
@@ -596,7 +602,7 @@ __global__ __launch_bounds__(256, 2) void k_prompt_fp32(PromptArgs a) {
     }
   }
   lds_barrier();
-  if (noted) spoil<false, D>(v, a.v_stride * 4, u.from, min(row.end, u.to), o);
+  if (noted) spoil<false, D>(v, a.v_stride * 4, max(u.from, all_clear & ~(KEYS - 1)), min(row.end, u.to), o);
   finish<false, D>(a, u, row, wave * 32 + n, o, w);
 }
 
@@ -705,13 +711,14 @@ static double forecast(const PromptArgs *a, const StepTimes &t, int keys_a_step,
 PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
   PromptPlan p{};
   int longest = 0;
-  int64_t rows = 0;
+  int64_t rows = 0, tiles = 0;
   for (int i = 0; i < a->seqs; ++i) {
     PromptSeq &s = a->s[i];
     const int64_t r = (int64_t)s.queries * a->G;
     s.tiles = (int)((r + kPromptRows - 1) / kPromptRows);
     longest = std::max(longest, s.keys);
     rows += r * a->Hkv;
+    tiles += (int64_t)s.tiles * a->Hkv;
   }
   // The parts that the longest keys are divided into: as many as make the forecast
   // least, with the joining launch's time: 5 us and what its parts' bytes take
@@ -720,8 +727,8 @@ PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
   const int keys_a_step = bf16 ? 64 : 32;
   double best = forecast(a, times, keys_a_step, 0);
   int chunk = 0;
-  // (Batches of 2^24 query rows fill the GPU; their join would pass a launch's threads.)
-  for (int parts = 2; parts <= 64 && longest > 64 && rows <= 1 << 24; parts += std::max(1, parts / 4)) {
+  // (2^20 tiles fill the GPU; their join, of 4096 threads each, would pass a launch's 2^32.)
+  for (int parts = 2; parts <= 64 && longest > 64 && tiles < 1 << 20; parts += std::max(1, parts / 4)) {
     const int c = ((longest + parts - 1) / parts + 63) / 64 * 64;
     const double time = forecast(a, times, keys_a_step, c) + 5 + 0.15 * parts + 7e-5 * head_dim / 128 * rows * parts;
     if (time < best) {

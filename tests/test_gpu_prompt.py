@@ -195,6 +195,28 @@ def test_keys_and_values_that_are_not_finite(dtype, d, lens, queries):
         assert torch.equal(out[rest], clean[rest])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("at", [5, 1700, 2955, 2990])
+@pytest.mark.parametrize("queries", [None, [3000 - 2900]])
+def test_values_that_are_not_finite_far_back(dtype, at, queries):
+    """Of a key in tiles that mask none, in a part of the keys, and in the last tile."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(8)
+    n, d, m = 3000, 128, 3000 if queries is None else queries[0]
+    q, k, v = (_rand(rng, t, h, d, dtype=dtype) for t, h in ((m, 2), (n, 1), (n, 1)))
+    call = lambda: bacon.bacon_prompt_attend(_shape(2, 1, d, 4, dtype), _batch([n]), q, k, v,  # noqa: E731
+                                             None if queries is None else _cu(queries), want_lse=True)[:2]
+    clean, clean_lse = call()
+    v[at, 0, 7] = float("inf")
+    out, lse = call()
+    first = max(m - (n - at), 0)                                # the first query that sees it
+    assert torch.equal(out[:first], clean[:first]) and torch.equal(lse, clean_lse)
+    assert not torch.isfinite(out[first:, :, 7]).any()
+    keep = [i for i in range(d) if i != 7]
+    assert torch.equal(out[first:][..., keep], clean[first:][..., keep])
+
+
 def test_views_strides_and_guards():
     """q, k, v as parts of one projection's output; outputs between guards."""
     import torch
