@@ -25,6 +25,7 @@ struct PromptArgs {
   unsigned group_magic;    // 2^32 / G, rounded up (0 where G is 1)
   float scale;             // 1 / sqrt(d)
   int seqs, units;
+  int sets;                // of four waves a workgroup (bf16), which take a unit's keys in turn
   int joined;              // tiles of KV heads whose parts are joined
   float2 *part_ml;         // [unit rows] maximum and sum of every part
   float *part_o;           // [unit rows, d]

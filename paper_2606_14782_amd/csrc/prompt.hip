@@ -4,7 +4,8 @@
 // r / G of head h G + r % G, so the G heads that share K and V share its tiles.
 // Each of its four waves holds 32 of them and sees every tile of keys, which
 // come through LDS, read directly from memory into one of two buffers while the
-// other is computed on.  Both products have the query rows along N:
+// other is computed on; or two sets of four waves take the tiles in turn and are
+// joined at the end.  Both products have the query rows along N:
 //
 //   S^T = K Q^T    lane (n = lane & 31, g = lane >> 5) holds, of row n, the logits
 //                  of keys 8 t + 4 g + i (t < 4, i < 4) of every 32
@@ -329,17 +330,20 @@ __device__ __forceinline__ void spoil(const char *v, int64_t stride_bytes, int f
 // A unit's outputs; false where one came out that is not finite, and nothing is
 // handed on.  That may be by a masked key's value (0 times it): CAREFUL counts such
 // values as 0 in tiles that mask keys, and finds what sees them.  (Looking for them
-// at once took 1.5 us of a masked tile's 3.)
-template <int D, bool CAREFUL>
+// at once took 1.5 us of a masked tile's 3.)  SETS of four waves take tiles in turn,
+// each through two buffers of its own.
+template <int D, int SETS, bool CAREFUL>
 __device__ __forceinline__ bool attend_unit(const PromptArgs &a, int unit, int t, char *lds) {
   constexpr int KEYS = 64, PIECES = D / 8, TILE = KEYS * D * 2, ROW = D * 2;
   const Unit u = unit_of(a, unit);
-  const int lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int lane = t & 63, set = SETS == 1 ? 0 : __builtin_amdgcn_readfirstlane(t >> 8);
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6 & 3);
   const int n = lane & 31, g = lane >> 5;
   const Row row = row_of(a, u, wave * 32 + n);
   const char *k = static_cast<const char *>(a.k) + ((int64_t)u.s.k0 * a.k_stride + u.h * D) * 2;
   const char *v = static_cast<const char *>(a.v) + ((int64_t)u.s.k0 * a.v_stride + u.h * D) * 2;
-  const unsigned lds_at = (unsigned)(uintptr_t)(LDS char *)lds;
+  char *own = lds + set * 4 * TILE;                          // this set's two buffers
+  const unsigned lds_at = (unsigned)(uintptr_t)(LDS char *)own;
   Share<KEYS, PIECES> ks, vs;
   ks.find(a.k_stride * 2, KEYS, wave, k_place<PIECES>);
   vs.find(a.v_stride * 2, KEYS, wave, v_place<PIECES>);
@@ -353,7 +357,7 @@ __device__ __forceinline__ bool attend_unit(const PromptArgs &a, int unit, int t
     vs.ask(v + base * a.v_stride * 2, to + TILE, wave);
   };
   bf16x8 q[D / 16];
-  if (u.from < u.to) ask(u.from, 0);
+  if (u.from + set * KEYS < u.to) ask(u.from + set * KEYS, 0);
   {
     const char *p = static_cast<const char *>(a.q) +
                     (((int64_t)u.s.q0 + row.query) * a.q_stride + (int64_t)row.head * D) * 2 + g * 16;
@@ -381,11 +385,12 @@ __device__ __forceinline__ bool attend_unit(const PromptArgs &a, int unit, int t
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
   int buffer = 0;
-  for (int base = u.from; base < u.to; base += KEYS, buffer ^= 1) {
+  for (int step = u.from; step < u.to; step += SETS * KEYS, buffer ^= 1) {
+    const int base = step + set * KEYS;
     tile_barrier();
-    if (base + KEYS < u.to) ask(base + KEYS, buffer ^ 1);
+    if (base + SETS * KEYS < u.to) ask(base + SETS * KEYS, buffer ^ 1);
     if (base >= far) continue;
-    const char *kt = lds + buffer * 2 * TILE, *vt = kt + TILE;
+    const char *kt = own + buffer * 2 * TILE, *vt = kt + TILE;
     f32x16 s[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -420,32 +425,64 @@ __device__ __forceinline__ bool attend_unit(const PromptArgs &a, int unit, int t
     else
       product([&](int j, int e) { return v_piece<ROW>(vt, v_at, j, e); });
   }
-  if constexpr (CAREFUL) {
-    spoil<true, D>(v, a.v_stride * 2, max(u.from, clear & ~(KEYS - 1)), min(row.end, u.to), o);
-  } else {
+  // (the buffer that nothing reads or fills now, and the one read last)
+  int *stop = reinterpret_cast<int *>(lds + buffer * 2 * TILE);
+  if constexpr (!CAREFUL) {
     float most = 0.f;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
       for (int i = 0; i < 16; i += 2) most = max3(most, __builtin_fabsf(o[e][i]), __builtin_fabsf(o[e][i + 1]));
-    int *stop = reinterpret_cast<int *>(lds + buffer * 2 * TILE);   // (the buffer that nothing reads or fills now)
-    if (lane == 0) stop[wave] = 0;
-    if (row.valid && !finite(most)) stop[wave] = 1;
+    const int at = set * 4 + wave;
+    if (lane == 0) stop[at] = 0;
+    if (row.valid && !finite(most)) stop[at] = 1;
     tile_barrier();
-    if (stop[0] | stop[1] | stop[2] | stop[3]) return false;
+    int any = 0;
+#pragma unroll
+    for (int i = 0; i < 4 * SETS; ++i) any |= stop[i];
+    if (any) return false;
   }
+  if constexpr (SETS == 2) {
+    if (CAREFUL) tile_barrier();
+    // the second set's rows, each lane's for the same lane of the first
+    f32x4 *to = reinterpret_cast<f32x4 *>(lds + 4 * TILE) + wave * (D / 8) * 64 + lane;
+    float2 *ml = reinterpret_cast<float2 *>(lds + (buffer ^ 1) * 2 * TILE) + wave * 64 + lane;
+    if (set == 1) {
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          to[(e * 4 + i) * 64] = f32x4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
+      *ml = make_float2(w.at, w.sum);
+    }
+    tile_barrier();
+    if (set == 1) return true;
+    const float2 x = *ml;
+    const float at = fmaxf(w.at, x.x), f = __builtin_amdgcn_exp2f(minus(w.at, at)), h = __builtin_amdgcn_exp2f(minus(x.x, at));
+    w.at = at;
+    w.sum = w.sum * f + x.y * h;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 y = to[(e * 4 + i) * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[e][4 * i + j] = o[e][4 * i + j] * f + y[j] * h;
+      }
+  }
+  if constexpr (CAREFUL) spoil<true, D>(v, a.v_stride * 2, max(u.from, clear & ~(KEYS - 1)), min(row.end, u.to), o);
   finish<true, D>(a, u, row, wave * 32 + n, o, w);
   return true;
 }
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void k_prompt_bf16(PromptArgs a) {
-  __shared__ __align__(16) char lds[4 * 64 * D * 2];         // K, V of two tiles
-  if (attend_unit<D, false>(a, blockIdx.x, threadIdx.x, lds)) return;
+template <int D, int SETS>
+__global__ __launch_bounds__(256 * SETS, 2) void k_prompt_bf16(PromptArgs a) {
+  __shared__ __align__(16) char lds[SETS * 4 * 64 * D * 2];  // K, V of two tiles a set
+  if (attend_unit<D, SETS, false>(a, blockIdx.x, threadIdx.x, lds)) return;
   tile_barrier();                                            // every wave has seen that
   int unit = blockIdx.x, t = threadIdx.x;                    // (as if others: else the first time keeps what the
   asm volatile("" : "+s"(unit), "+v"(t));                    // second needs)
-  attend_unit<D, true>(a, unit, t, lds);
+  attend_unit<D, SETS, true>(a, unit, t, lds);
 }
 
 // Eight floats as three bf16 parts whose sum they are: two cut off (a mask, and the
@@ -708,6 +745,25 @@ static double forecast(const PromptArgs *a, const StepTimes &t, int keys_a_step,
   return std::max(last, (steps + kUnitSteps * units) / 256 * t.all);
 }
 
+// The same with two sets of waves a workgroup and one part: a tile of a set costs half,
+// a workgroup's join three steps more, and a compute unit holds one.  It pays where
+// the longest rows are what the call waits for (us, one set and two: 1K tokens of 28
+// heads 28.8 and 26.3, 2K of 16 47.6 and 41.5, of 28 52.9 and 48.1, of 32 53.7 and
+// 52.1; not 256 tokens of 32, 12.7 and 13.9, nor four prompts of 4K, 572 and 657).
+static bool two_sets(const PromptArgs *a, int head_dim, double *time) {
+  double steps = 0, units = 0, longest = 0;
+  for (int i = 0; i < a->seqs; ++i) {
+    const PromptSeq &s = a->s[i];
+    const double n = (double)s.tiles * a->Hkv;
+    steps += n * 0.5 * (std::max(0, s.keys - s.queries) + s.keys) / 64;
+    units += n;
+    longest = std::max(longest, s.keys / 64.0);
+  }
+  if (!(units <= 256 ? longest >= 12 : units <= 512 && longest >= 20 && steps <= 0.6 * longest * units)) return false;
+  *time = std::max(longest + 10, (steps + 10 * units) / 256) * (head_dim == 128 ? 1.0 : 0.61);
+  return true;
+}
+
 PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
   PromptPlan p{};
   int longest = 0;
@@ -726,6 +782,7 @@ PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
   const StepTimes times = step_times(head_dim, bf16);
   const int keys_a_step = bf16 ? 64 : 32;
   double best = forecast(a, times, keys_a_step, 0);
+  a->sets = bf16 && two_sets(a, head_dim, &best) ? 2 : 1;
   int chunk = 0;
   // (2^20 tiles fill the GPU; their join, of 4096 threads each, would pass a launch's 2^32.)
   for (int parts = 2; parts <= 64 && longest > 64 && tiles < 1 << 20; parts += std::max(1, parts / 4)) {
@@ -734,6 +791,7 @@ PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
     if (time < best) {
       best = time;
       chunk = c;
+      a->sets = 1;
     }
     if (c == 64) break;
   }
@@ -759,27 +817,25 @@ PromptPlan prompt_plan(PromptArgs *a, int head_dim, bool bf16) {
   return p;
 }
 
-hipError_t launch_prompt(const PromptArgs &a, bool bf16, int head_dim, hipStream_t s) {
-  const dim3 grid((unsigned)a.units), threads(256);
-  if (bf16 && head_dim == 128)
-    hipLaunchKernelGGL((k_prompt_bf16<128>), grid, threads, 0, s, a);
+template <int D>
+static void launch(const PromptArgs &a, bool bf16, hipStream_t s) {
+  const dim3 grid((unsigned)a.units);
+  if (bf16 && a.sets == 2)
+    hipLaunchKernelGGL((k_prompt_bf16<D, 2>), grid, dim3(512), 0, s, a);
   else if (bf16)
-    hipLaunchKernelGGL((k_prompt_bf16<64>), grid, threads, 0, s, a);
-  else if (head_dim == 128)
-    hipLaunchKernelGGL((k_prompt_fp32<128>), grid, threads, 0, s, a);
+    hipLaunchKernelGGL((k_prompt_bf16<D, 1>), grid, dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_prompt_fp32<64>), grid, threads, 0, s, a);
-  if (a.joined) {
-    const dim3 join((unsigned)a.joined * (kPromptRows * head_dim / 4 / 256));
-    if (bf16 && head_dim == 128)
-      hipLaunchKernelGGL((k_prompt_join<true, 128>), join, threads, 0, s, a);
-    else if (bf16)
-      hipLaunchKernelGGL((k_prompt_join<true, 64>), join, threads, 0, s, a);
-    else if (head_dim == 128)
-      hipLaunchKernelGGL((k_prompt_join<false, 128>), join, threads, 0, s, a);
-    else
-      hipLaunchKernelGGL((k_prompt_join<false, 64>), join, threads, 0, s, a);
-  }
+    hipLaunchKernelGGL((k_prompt_fp32<D>), grid, dim3(256), 0, s, a);
+  if (!a.joined) return;
+  const dim3 join((unsigned)a.joined * (kPromptRows * D / 4 / 256));
+  if (bf16)
+    hipLaunchKernelGGL((k_prompt_join<true, D>), join, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_prompt_join<false, D>), join, dim3(256), 0, s, a);
+}
+
+hipError_t launch_prompt(const PromptArgs &a, bool bf16, int head_dim, hipStream_t s) {
+  head_dim == 128 ? launch<128>(a, bf16, s) : launch<64>(a, bf16, s);
   return hipGetLastError();
 }
 

@@ -115,6 +115,22 @@ def test_divided_keys(dtype, lens, queries):
     _run(np.random.default_rng(len(lens)), 4, 2, 128, dtype, lens, queries, W=16)
 
 
+@pytest.mark.parametrize("scale", [1.0, 30.0])
+@pytest.mark.parametrize("hq,hkv,d,lens,queries", [
+    (28, 4, 128, [1000], None), (32, 8, 64, [1500, 70, 0, 33], None), (14, 2, 64, [2077], None),
+    (28, 4, 128, [1601, 40], [700, 50]), (16, 16, 128, [2050], None)])
+def test_long_rows_on_an_emptier_gpu(hq, hkv, d, lens, queries, scale):
+    """Where the longest rows are what a call waits for and nothing is divided: odd
+    and even numbers of tiles, rows of one tile, sequences of none."""
+    from paper_2606_14782_amd import bacon
+    import ctypes as C
+    cuq = None if queries is None else _cu(queries)
+    need = bacon.lib().bacon_prompt_work_bytes(C.byref(_shape(hq, hkv, d, 16, "bf16")), C.byref(_batch(lens).c),
+                                               None if cuq is None else cuq.ctypes.data)
+    assert need == 0
+    _run(np.random.default_rng(d), hq, hkv, d, "bf16", lens, queries, W=16, scale=scale, heads=[0, hq // 2, hq - 1])
+
+
 def test_many_units():
     """More workgroups than the GPU holds at once: nothing divided."""
     _run(np.random.default_rng(3), 64, 8, 64, "bf16", [700] * 12, heads=[0, 13, 63])
@@ -197,22 +213,23 @@ def test_keys_and_values_that_are_not_finite(dtype, d, lens, queries):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("at", [5, 1700, 2955, 2990])
-@pytest.mark.parametrize("queries", [None, [3000 - 2900]])
-def test_values_that_are_not_finite_far_back(dtype, at, queries):
+@pytest.mark.parametrize("hq,queries", [(2, None), (2, [3000 - 2900]), (14, None)])
+def test_values_that_are_not_finite_far_back(dtype, at, hq, queries):
     """Of a key in tiles that mask none, in a part of the keys, and in the last tile."""
     import torch
     from paper_2606_14782_amd import bacon
     rng = np.random.default_rng(8)
     n, d, m = 3000, 128, 3000 if queries is None else queries[0]
-    q, k, v = (_rand(rng, t, h, d, dtype=dtype) for t, h in ((m, 2), (n, 1), (n, 1)))
-    call = lambda: bacon.bacon_prompt_attend(_shape(2, 1, d, 4, dtype), _batch([n]), q, k, v,  # noqa: E731
+    q, k, v = (_rand(rng, t, h, d, dtype=dtype) for t, h in ((m, hq), (n, hq // 2), (n, hq // 2)))
+    call = lambda: bacon.bacon_prompt_attend(_shape(hq, hq // 2, d, 4, dtype), _batch([n]), q, k, v,  # noqa: E731
                                              None if queries is None else _cu(queries), want_lse=True)[:2]
     clean, clean_lse = call()
-    v[at, 0, 7] = float("inf")
+    v[at, -1, 7] = float("inf")
     out, lse = call()
     first = max(m - (n - at), 0)                                # the first query that sees it
     assert torch.equal(out[:first], clean[:first]) and torch.equal(lse, clean_lse)
-    assert not torch.isfinite(out[first:, :, 7]).any()
+    assert torch.equal(out[:, :-2], clean[:, :-2])
+    assert not torch.isfinite(out[first:, -2:, 7]).any()
     keep = [i for i in range(d) if i != 7]
     assert torch.equal(out[first:][..., keep], clean[first:][..., keep])
 
