@@ -491,10 +491,10 @@ class _Given:
 
     def rows(self, t, name, heads, head_dim):
         """Tokens and token distance of [.., heads, head_dim]."""
-        shape, strides = t.shape, t.stride()
-        if (len(shape) == 3 and strides[2] == 1 and strides[1] == head_dim and shape[1] == heads and shape[2] == head_dim
-                and shape[0] > 1 and t.dtype == self.dtype and t.device == self.device):
-            return shape[0], strides[0]
+        if t.dim() == 3 and t.dtype == self.dtype and t.device == self.device:      # the usual, without loops
+            (n, h, d), (step, run, one) = t.shape, t.stride()
+            if h == heads and d == head_dim and run == d and one == 1 and n:
+                return n, step if n > 1 else h * d
         at = _tokens_at(t, heads, head_dim) if t.dtype == self.dtype and t.device == self.device else None
         if at is None or at[1] is None:
             raise BaconError(ERR_INVALID, f"{name} must be {self.dtype} [.., {heads}, {head_dim}] on {self.device}, a "
@@ -576,9 +576,10 @@ def bacon_rotate(rotary: Rotary, positions, q=None, k=None, q_norm=None, k_norm=
     first = q if q is not None else k
     if first is None:
         raise BaconError(ERR_INVALID, "q and k are None")
-    g, c, lead, d = _Given(first, rotary.torch_dtype), rotary.c, first.shape[:-2], rotary.head_dim
+    g, lead, d = _Given(first, rotary.torch_dtype), first.shape[:-2], rotary.head_dim
     qp = kp = qo = ko = None
     qs = ks = qos = kos = n = 0
+    same = True
     if q is not None:
         n, qs = g.rows(q, "q", rotary.num_q_heads, d)
         if q_out is None:
@@ -586,20 +587,23 @@ def bacon_rotate(rotary: Rotary, positions, q=None, k=None, q_norm=None, k_norm=
             qos = rotary.num_q_heads * d
         else:
             qos = g.rows(q_out, "q_out", rotary.num_q_heads, d)[1]
+            same = q_out.shape[:-2] == lead
         qp, qo = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise BaconError(ERR_INVALID, "q_out without q")
     if k is not None:
         n, ks = g.rows(k, "k", rotary.num_kv_heads, d)
+        same = same and (k is first or k.shape[:-2] == lead)
         if k_out is None:
             k_out = g.like(k)
             kos = rotary.num_kv_heads * d
         else:
             kos = g.rows(k_out, "k_out", rotary.num_kv_heads, d)[1]
+            same = same and k_out.shape[:-2] == lead
         kp, ko = k.data_ptr(), k_out.data_ptr()
     elif k_out is not None:
         raise BaconError(ERR_INVALID, "k_out without k")
-    if q is not None and q_out.shape[:-2] != lead or k is not None and (k.shape[:-2] != lead or k_out.shape[:-2] != lead):
+    if not same:
         raise BaconError(ERR_INVALID, f"q, k and their outputs do not all have the tokens {tuple(lead)}")
     pos = g.whole(positions, "positions", (3, *lead) if rotary.sectioned else lead, g.torch.int32)
     g.call(rotary._rotate, rotary._c, n, pos, qp, qs, kp, ks, None if q_norm is None else g.whole(q_norm, "q_norm", (d,)),
