@@ -613,7 +613,8 @@ void bacon_default_rotary(bacon_rotary *r);
  * that bacon_rotate uses; host work. */
 bacon_status bacon_rotary_frequencies(const bacon_rotary *r, double *frequencies, double *magnitude);
 
-/* Turns q and k of `tokens` tokens (0: nothing to do; at most 2^25).  d_q [tokens, Hq, d], its tokens q_stride
+/* Turns q and k of `tokens` tokens (0: nothing to do; at most 2^25).  d_q
+ * [tokens, Hq, d], its tokens q_stride
  * elements apart (>= Hq d, a multiple of 16 bytes; a view of a fused projection's
  * output will do), to d_q_out, q_out_stride apart; k likewise.  q or k may be
  * NULL (then its output is too); an output may be its input (the same pointer
@@ -647,12 +648,12 @@ bacon_status bacon_rotate(const bacon_rotary *r, int64_t tokens, const int32_t *
  * a query of this call are left as they were, so that chunks fill them in turn.
  *
  * Logits, maxima, sums and outputs are held in 32 bits (|V| up to 2^88 passes no
- * sum's range).  In bfloat16 a weight
- * enters the second product rounded to bfloat16 (2^-9 of itself at most, as much as
- * the output's own rounding, and independent from key to key).  A query one of
- * whose logits is NaN or +infinity, or whose logits are all -infinity, gives NaN;
- * so does, in float32, one that sees a K that is not finite.  Where V of a key
- * that is seen is not finite, its queries' outputs of that dimension are not.
+ * sum's range).  In bfloat16 a weight enters the second product rounded to bfloat16
+ * (2^-8 of itself at most, as much as the output's own rounding, and independent
+ * from key to key).  A query one of whose logits is NaN or +infinity, or whose logits
+ * are all -infinity, gives NaN; so does, in float32, one that sees a K that is not
+ * finite.  Where V of a key that is seen is not finite, its queries' outputs of that
+ * dimension are not.
  * What lies in rows that no query sees reaches nothing.
  * d_work: scratch of bacon_prompt_work_bytes (0: may be NULL), 256-byte aligned,
  * of this call alone until its work is done.  Outputs and work overlap nothing

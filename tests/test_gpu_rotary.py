@@ -272,3 +272,29 @@ def test_binding_refuses():
         args.update(kw)
         with pytest.raises(bacon.BaconError):
             bacon.bacon_rotate(rot, **args)
+
+
+def test_one_token_of_any_view():
+    """A decoded token's heads in a projection's output, with leading dimensions, in
+    place, and refused where they do not lie together or the tokens differ."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(12)
+    rot = _rotary(4, 2, 64, "bf16")
+    both = _rand(rng, 5, 8, 64)
+    p = torch.tensor([70000], dtype=torch.int32, device="cuda")
+    q, k = both[3:4, :4], both[3:4, 4:6]
+    wq, wk = bacon.bacon_rotate(rot, p, q.contiguous(), k.contiguous())
+    a, b = bacon.bacon_rotate(rot, p, q, k)
+    assert torch.equal(a, wq) and torch.equal(b, wk) and a.is_contiguous()
+    a, b = bacon.bacon_rotate(rot, p[None], q[None], k[None])
+    assert torch.equal(a, wq[None]) and torch.equal(b, wk[None])
+    with pytest.raises(bacon.BaconError):
+        bacon.bacon_rotate(rot, p, both[3:4, ::2], k)
+    with pytest.raises(bacon.BaconError):
+        bacon.bacon_rotate(rot, p, q, both[:2, 4:6])
+    with pytest.raises(bacon.BaconError):
+        bacon.bacon_rotate(rot, p, q, k, k_out=torch.empty_like(both[:2, 4:6]))
+    rest = both[:, 6:].clone()
+    bacon.bacon_rotate(rot, p, q, k, q_out=q, k_out=k)
+    assert torch.equal(both[3:4, :4], wq) and torch.equal(both[3:4, 4:6], wk) and torch.equal(both[:, 6:], rest)
