@@ -645,7 +645,8 @@ bacon_status bacon_rotate(const bacon_rotary *r, int64_t tokens, const int32_t *
  * [cu_queries[batch], Hq, d]; d_lse (optional) [cu_queries[batch], Hq] float32;
  * d_window_lse (optional) [batch, Hq, W] float32: the lse of the queries that are
  * the window's tokens (token N_b - W + w is entry w); entries whose token is not
- * a query of this call are left as they were, so that chunks fill them in turn.
+ * a query of this call are left as they were.  N_b grows from chunk to chunk, and the
+ * window with it: chunks fill one buffer in turn through bacon_prompt_attend_chunk.
  *
  * Logits, maxima, sums and outputs are held in 32 bits (|V| up to 2^88 passes no
  * sum's range).  In bfloat16 a weight enters the second product rounded to bfloat16
@@ -663,6 +664,19 @@ bacon_status bacon_prompt_attend(const bacon_shape *shape, const bacon_batch *ba
                                  const void *d_v, int64_t v_stride, void *d_out, float *d_lse, float *d_window_lse,
                                  void *d_work, size_t work_bytes, void *stream);
 size_t bacon_prompt_work_bytes(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries);
+
+/* The same for prompts that come in chunks, with one d_window_lse for all of a
+ * prompt's calls.  window_ends (host array [batch], read during the call): the
+ * tokens E_b >= N_b that sequence b will have when its last chunk has come.  Token E_b -
+ * W + w is entry w; each call writes the entries of its own queries and leaves the
+ * others, so that after the last chunk, of whatever sizes they were, all W are there
+ * (of E_b < W the last E_b), as from one call over the whole prompt.  A chunk that
+ * ends before the window writes none; a call repeated writes the same.  NULL: E_b =
+ * N_b, as in bacon_prompt_attend.  Its scratch is bacon_prompt_work_bytes. */
+bacon_status bacon_prompt_attend_chunk(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries,
+                                       const int32_t *window_ends, const void *d_q, int64_t q_stride, const void *d_k,
+                                       int64_t k_stride, const void *d_v, int64_t v_stride, void *d_out, float *d_lse,
+                                       float *d_window_lse, void *d_work, size_t work_bytes, void *stream);
 
 const char *bacon_status_string(bacon_status s);
 const char *bacon_last_error(void);

@@ -32,7 +32,7 @@ ENTRY_POINTS = [
     "bacon_cache_attend", "bacon_cache_work_bytes", "bacon_cache_step", "bacon_cache_advance",
     "bacon_cache_errors",
     "bacon_default_rotary", "bacon_rotary_frequencies", "bacon_rotate",
-    "bacon_prompt_attend", "bacon_prompt_work_bytes",
+    "bacon_prompt_attend", "bacon_prompt_attend_chunk", "bacon_prompt_work_bytes",
 ]
 
 
@@ -166,9 +166,11 @@ def lib() -> C.CDLL:
         L.bacon_rotary_frequencies.argtypes = [rot, vp, vp]
         L.bacon_rotate.argtypes = [rot, i64, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp]
         L.bacon_prompt_attend.argtypes = [C.POINTER(Shape), cap, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, sz, vp]
+        L.bacon_prompt_attend_chunk.argtypes = [C.POINTER(Shape), cap, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp,
+                                                sz, vp]
         L.bacon_prompt_work_bytes.argtypes = [C.POINTER(Shape), cap, vp]
         L.bacon_prompt_work_bytes.restype = sz
-        for name in ("rotary_frequencies", "rotate", "prompt_attend"):
+        for name in ("rotary_frequencies", "rotate", "prompt_attend", "prompt_attend_chunk"):
             getattr(L, "bacon_" + name).restype = C.c_int
         for name in ("layout", "init", "free", "clear", "tables", "store", "load", "append", "attend",
                      "step", "advance"):
@@ -612,13 +614,15 @@ def bacon_rotate(rotary: Rotary, positions, q=None, k=None, q_norm=None, k_norm=
 
 
 def bacon_prompt_attend(shape: Shape, batch: BatchLayout, q, k, v, queries=None, want_lse=False,
-                        want_window_lse=False, out=None, lse=None, window_lse=None, work=None):
+                        want_window_lse=False, out=None, lse=None, window_lse=None, work=None, window_ends=None):
     """Causal attention of a ragged batch of prompts: q [Tq, Hq, d] over k, v [T,
     Hkv, d] (views of one projection's output will do).  queries: the cumulative
     numbers of queries [batch + 1] where they are the prompts' last tokens only.
     Returns (out [Tq, Hq, d], lse [Tq, Hq] or None, window_lse [batch, Hq, W] or
     None); entries of window_lse whose token is no query stay (NaN, where it is
-    made here)."""
+    made here).  window_ends [batch]: the tokens that prompts which come in chunks
+    will have, so that their chunks fill one window_lse in turn; None: a window is of
+    the call's own last tokens."""
     hq, hkv, d, W = shape.num_q_heads, shape.num_kv_heads, shape.head_dim, shape.window
     g = _Given(q, None)
     torch, L = g.torch, lib()
@@ -630,6 +634,12 @@ def bacon_prompt_attend(shape: Shape, batch: BatchLayout, q, k, v, queries=None,
             raise BaconError(ERR_INVALID, f"queries has shape {cuq.shape}, {batch.cu.shape} expected")
         cup = cuq.ctypes.data
     n, total, seqs = int(cuq[-1]), int(batch.cu[-1]), len(batch.cu) - 1
+    endp = None
+    if window_ends is not None:
+        ends = np.ascontiguousarray(window_ends, dtype=np.int32)
+        if ends.shape != (seqs,):
+            raise BaconError(ERR_INVALID, f"window_ends has shape {ends.shape}, {(seqs,)} expected")
+        endp = ends.ctypes.data
     qn, qs = g.rows(q, "q", hq, d)
     kn, ks = g.rows(k, "k", hkv, d)
     vn, vs = g.rows(v, "v", hkv, d)
@@ -652,7 +662,7 @@ def bacon_prompt_attend(shape: Shape, batch: BatchLayout, q, k, v, queries=None,
     if need and work is None:
         work = q.new_empty(need, dtype=torch.uint8)
     workp = g.whole(work, "work", None, torch.uint8)
-    g.call(L.bacon_prompt_attend, sp, bp, cup, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, outp, lsep, winp,
+    g.call(L.bacon_prompt_attend_chunk, sp, bp, cup, endp, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, outp, lsep, winp,
            workp, 0 if work is None else work.numel())
     return out, lse, window_lse
 

@@ -14,6 +14,7 @@ struct PromptSeq {
   int k0, keys, q0, queries;
   int unit0, tiles, splits, index;
   int join0;               // tiles of KV heads before it that are joined
+  int window0;             // its first query's entry of the window (below 0: that query has none)
 };
 
 struct PromptArgs {

@@ -175,7 +175,7 @@ __device__ __forceinline__ void finish(const PromptArgs &a, const Unit &u, const
   if (g == 0) {
     const float lse = none ? -INFINITY : (w.at + __log2f(l)) * kLn2;
     if (a.lse) a.lse[token * a.Hq + row.head] = lse;
-    const int at_window = a.W - u.s.queries + row.query;
+    const int at_window = u.s.window0 + row.query;
     if (a.window && at_window >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + at_window] = lse;
   }
 }
@@ -701,7 +701,7 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
   if (dim == 0) {
     const float lse = none ? -INFINITY : (most + __log2f(sum)) * kLn2;
     if (a.lse) a.lse[token * a.Hq + row.head] = lse;
-    const int place = a.W - u.s.queries + row.query;
+    const int place = u.s.window0 + row.query;
     if (a.window && place >= 0) a.window[((int64_t)u.s.index * a.Hq + row.head) * a.W + place] = lse;
   }
 }

@@ -2,6 +2,7 @@
 // checks, the division of the work and launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/bacon.h"
@@ -54,9 +55,10 @@ bacon_status check_cu(const bacon_shape *s, const int32_t *cu, int batch, const 
   return BACON_OK;
 }
 
-// The batch's sequences that have queries, divided.
-bacon_status check_batch(const bacon_shape *s, const bacon_batch *bt, const int32_t *cu_queries, PromptArgs *a,
-                         PromptPlan *plan) {
+// The batch's sequences that have queries, divided.  window_ends: tokens of each prompt
+// at its end, whose last W the window is of (NULL: its keys).
+bacon_status check_batch(const bacon_shape *s, const bacon_batch *bt, const int32_t *cu_queries,
+                         const int32_t *window_ends, PromptArgs *a, PromptPlan *plan) {
   TRY(check_shape(s));
   if (!bt) return fail(BACON_ERR_INVALID, "batch is NULL");
   if (bt->batch < 1 || bt->batch > s->max_batch)
@@ -72,16 +74,21 @@ bacon_status check_batch(const bacon_shape *s, const bacon_batch *bt, const int3
   a->group_magic = a->G == 1 ? 0 : (unsigned)((0x100000000ull + a->G - 1) / a->G);
   a->scale = (float)(1.0 / std::sqrt((double)s->head_dim));
   for (int b = 0; b < bt->batch; ++b) {
-    const int queries = cuq[b + 1] - cuq[b];
+    const int queries = cuq[b + 1] - cuq[b], keys = bt->cu_seqlens[b + 1] - bt->cu_seqlens[b];
+    if (window_ends && window_ends[b] < keys)
+      return fail(BACON_ERR_INVALID, "sequence %d has %d keys, its window ends at token %d", b, keys, window_ends[b]);
     if (queries == 0) continue;
     if ((int64_t)queries * a->G > kMaxTokens)
       return fail(BACON_ERR_UNSUPPORTED, "%d queries of %d heads per KV head are too many", queries, a->G);
     PromptSeq &q = a->s[a->seqs++];
     q.k0 = bt->cu_seqlens[b];
-    q.keys = bt->cu_seqlens[b + 1] - bt->cu_seqlens[b];
+    q.keys = keys;
     q.q0 = cuq[b];
     q.queries = queries;
     q.index = b;
+    // (queries are at most 2^30: none of them has an entry where this is below)
+    const int64_t to_come = window_ends ? (int64_t)window_ends[b] - keys : 0;
+    q.window0 = (int)std::max<int64_t>((int64_t)a->W - queries - to_come, -kMaxTokens);
   }
   *plan = prompt_plan(a, s->head_dim, s->dtype == BACON_BF16);
   if (a->units > kMaxUnits) return fail(BACON_ERR_UNSUPPORTED, "the batch's queries are too many for one call");
@@ -121,16 +128,16 @@ extern "C" {
 size_t bacon_prompt_work_bytes(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries) {
   PromptArgs a{};
   PromptPlan p{};
-  return check_batch(shape, batch, cu_queries, &a, &p) == BACON_OK ? p.bytes : 0;
+  return check_batch(shape, batch, cu_queries, nullptr, &a, &p) == BACON_OK ? p.bytes : 0;
 }
 
-bacon_status bacon_prompt_attend(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries,
-                                 const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride,
-                                 const void *d_v, int64_t v_stride, void *d_out, float *d_lse, float *d_window_lse,
-                                 void *d_work, size_t work_bytes, void *stream) {
+bacon_status bacon_prompt_attend_chunk(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries,
+                                       const int32_t *window_ends, const void *d_q, int64_t q_stride, const void *d_k,
+                                       int64_t k_stride, const void *d_v, int64_t v_stride, void *d_out, float *d_lse,
+                                       float *d_window_lse, void *d_work, size_t work_bytes, void *stream) {
   PromptArgs a{};
   PromptPlan p{};
-  TRY(check_batch(shape, batch, cu_queries, &a, &p));
+  TRY(check_batch(shape, batch, cu_queries, window_ends, &a, &p));
   if (a.seqs == 0) return BACON_OK;
   TRY(check_rows(shape, d_q, q_stride, a.Hq, "q"));
   TRY(check_ptr(d_out, "out", 16));
@@ -160,6 +167,14 @@ bacon_status bacon_prompt_attend(const bacon_shape *shape, const bacon_batch *ba
   a.part_o = reinterpret_cast<float *>(static_cast<char *>(d_work) + p.ml_bytes);
   const hipError_t e = launch_prompt(a, shape->dtype == BACON_BF16, shape->head_dim, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? BACON_OK : fail(BACON_ERR_HIP, "prompt_attend: %s", hipGetErrorString(e));
+}
+
+bacon_status bacon_prompt_attend(const bacon_shape *shape, const bacon_batch *batch, const int32_t *cu_queries,
+                                 const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride,
+                                 const void *d_v, int64_t v_stride, void *d_out, float *d_lse, float *d_window_lse,
+                                 void *d_work, size_t work_bytes, void *stream) {
+  return bacon_prompt_attend_chunk(shape, batch, cu_queries, nullptr, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_out,
+                                   d_lse, d_window_lse, d_work, work_bytes, stream);
 }
 
 }  // extern "C"

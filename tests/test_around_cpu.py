@@ -265,3 +265,20 @@ def test_formats_that_are_none_refused(fmt):
 def test_a_shape_without_a_format_is_in_8_bits():
     s = bacon.CacheShape(3, 8, 2, 128, 32, 32, 4, 10, 200, bacon.BF16)
     assert s.format == bacon.CACHE_E4M3
+
+
+def _chunk(ends, **kw):
+    s, b, e = _shape(), _batch([50, 60]), np.asarray(ends, np.int32)
+    a = dict(cuq=[0, 10, 20], q=FAKE)
+    a.update(kw)
+    q = np.asarray(a["cuq"], np.int32)
+    return bacon.lib().bacon_prompt_attend_chunk(C.byref(s), C.byref(b.c), q.ctypes.data, e.ctypes.data, a["q"], 1024, FAKE,
+                                                 256, FAKE, 256, FAKE, FAKE, FAKE, FAKE, 1 << 40, None)
+
+
+def test_window_ends_before_the_keys_refused():
+    for ends in ([49, 60], [50, 59], [0, 0], [-1, 60], [50, -2 ** 31]):
+        _refused(_chunk(ends), INV)
+        _refused(_chunk(ends, cuq=[0, 0, 0]), INV)              # (also of a sequence without queries)
+    _refused(_chunk([50, 2 ** 31 - 1], q=None), INV)            # the other checks are bacon_prompt_attend's
+    assert _chunk([50, 2 ** 31 - 1], cuq=[0, 0, 0]) == bacon.OK

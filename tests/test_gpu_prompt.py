@@ -363,3 +363,119 @@ def test_binding_refuses():
     with pytest.raises(bacon.BaconError):
         bacon.bacon_prompt_attend(shape, long, q, k, k, [0, 1], work=torch.zeros(256, dtype=torch.uint8, device="cuda"))
     bacon.bacon_prompt_attend(shape, _batch([0, 0]), q[:0], k[:0], k[:0])     # nothing to do
+
+
+CHUNKED = [
+    ("bf16", 4, 2, 64, 32, [220], [[200], [20]]),
+    ("bf16", 4, 2, 64, 32, [220], [[100], [95], [1], [24]]),
+    ("fp32", 6, 2, 128, 8, [130, 9], [[129, 4], [1, 0], [0, 5]]),
+    ("fp32", 4, 4, 64, 16, [40, 10], [[25, 3], [14, 6], [1, 1]]),              # a prompt shorter than the window
+    ("bf16", 4, 2, 128, 16, [5003, 700], [[4990, 690], [9, 1], [1, 0], [3, 9]]),  # keys divided
+    ("fp32", 4, 2, 128, 16, [5003], [[4990], [9], [1], [3]]),
+    ("bf16", 28, 4, 128, 32, [1601], [[1590], [11]]),                           # two sets of waves, then divided keys
+]
+
+
+def _chunks(rng, dtype, hq, hkv, d, W, lens):
+    """A function of a call's chunk of every prompt, and the prompts themselves."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    q, k, v = ([_rand(rng, n, h, d, dtype=dtype) for n in lens] for h in (hq, hkv, hkv))
+    shape = _shape(hq, hkv, d, W, dtype)
+
+    def call(at, sizes, window, ends):
+        to = [a + m for a, m in zip(at, sizes)]
+        parts = [torch.cat([x[:e] for x, e in zip(t, to)]) for t in (k, v)]
+        rows = torch.cat([x[a:e] for x, a, e in zip(q, at, to)])
+        return bacon.bacon_prompt_attend(shape, _batch(to), rows, *parts, _cu(sizes), window_lse=window,
+                                         window_ends=ends)[0]
+
+    return call, q, k
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,W,lens,chunks", CHUNKED)
+def test_one_window_for_all_chunks(dtype, hq, hkv, d, W, lens, chunks):
+    """Chunks of any sizes, the last ones shorter than the window, leave in one buffer
+    what a call over the whole prompts leaves there; a call repeated changes nothing."""
+    import torch
+    rng = np.random.default_rng(W + d)
+    call, q, k = _chunks(rng, dtype, hq, hkv, d, W, lens)
+    window = torch.full((len(lens), hq, W), MARK, device="cuda")
+    at = [0] * len(lens)
+    for sizes in chunks:
+        call(at, sizes, window, lens)
+        at = [a + m for a, m in zip(at, sizes)]
+        now = window.clone()
+        call([a - m for a, m in zip(at, sizes)], sizes, window, np.array(lens))
+        assert torch.equal(now, window)
+        for b, n in enumerate(lens):                            # filled up to the tokens so far, and no further
+            w = min(max(at[b] - (n - W), max(0, W - n)), W)
+            assert (window[b, :, w:] == MARK).all()
+    assert at == lens
+    got = _np(window)
+    for b, n in enumerate(lens):
+        m = min(n, W)
+        assert np.all(got[b, :, :W - m] == MARK)
+        qn, kn = _np(q[b]), _np(k[b])
+        for h in range(hq):
+            key = kn[:, h * hkv // hq]
+            _, s, _, tol = A.attend(qn[n - m:, h], key, key, np.arange(n - m + 1, n + 1), dtype)
+            err = np.abs(got[b, h, W - m:] - s)
+            assert np.all(err <= tol), (b, h, float((err / tol).max()))
+
+
+def test_window_of_a_chunk_that_ends_before_it():
+    """Windows that are still to come, the furthest among them, and none named."""
+    import torch
+    call, _, _ = _chunks(np.random.default_rng(3), "bf16", 4, 2, 64, 16, [90])
+    window = torch.full((1, 4, 16), MARK, device="cuda")
+    for end in (106, 200, 2 ** 31 - 1):
+        out = call([0], [90], window, [end])
+        assert (window == MARK).all()
+    assert torch.equal(call([0], [90], window, [105]), out)
+    assert (window[..., 1:] == MARK).all() and (window[..., 0] != MARK).all()
+    whole = torch.full((1, 4, 16), MARK, device="cuda")
+    assert torch.equal(call([0], [90], whole, None), out)
+    named = torch.full((1, 4, 16), MARK, device="cuda")
+    call([0], [90], named, [90])
+    assert torch.equal(whole, named) and torch.equal(window[..., 0], whole[..., -1])
+
+
+def test_captured_chunks_fill_one_window():
+    """The chunks' calls in one graph, replayed on other inputs between eager work."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(4)
+    hq, hkv, d, W, n = 4, 2, 64, 32, 220
+    shape = _shape(hq, hkv, d, W, "bf16")
+    inputs = [[_rand(rng, n, h, d) for h in (hq, hkv, hkv)] for _ in range(3)]
+    window = torch.full((1, hq, W), MARK, device="cuda")
+
+    def chunks(q, k, v, window):
+        for a, e in ((0, 200), (200, 219), (219, 220)):
+            bacon.bacon_prompt_attend(shape, _batch([e]), q[a:e], k[:e], v[:e], [0, e - a], window_lse=window, window_ends=[n])
+
+    x = [t.clone() for t in inputs[0]]
+    chunks(*x, window)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        chunks(*x, window)
+    for i in (1, 2, 0, 1):
+        want = torch.full((1, hq, W), MARK, device="cuda")
+        chunks(*inputs[i], want)
+        for t, y in zip(x, inputs[i]):
+            t.copy_(y)
+        window.fill_(MARK)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(window, want) and not (window == MARK).any()
+
+
+def test_binding_refuses_window_ends():
+    import torch
+    from paper_2606_14782_amd import bacon
+    q, k = (torch.zeros(12, h, 64, dtype=torch.bfloat16, device="cuda") for h in (4, 2))
+    for ends in ([5], [5, 7, 9], [4, 7], [5, 6], [[5, 7]], 12):
+        with pytest.raises(bacon.BaconError):
+            bacon.bacon_prompt_attend(_shape(4, 2, 64, 8, "bf16"), _batch([5, 7]), q, k, k, window_ends=ends)
+    bacon.bacon_prompt_attend(_shape(4, 2, 64, 8, "bf16"), _batch([5, 7]), q, k, k, window_ends=[5, 9])
