@@ -46,6 +46,8 @@ class Layer:
         self.ctx = bacon.Context(1, hq, hkv, d, W, B, T, dtype, bacon.default_params(pool_kernel=5))
         self.window = torch.empty(B, hq, W, device="cuda")
         self.out = bacon.bacon_prompt_attend(self.ctx.shape, self.batch, q, k, v, window_lse=self.window)[0]
+        if chunk is not None:
+            self.window = self.window_by_chunks(chunk, q, k, v)
         rows = np.concatenate([np.arange(self.cu[i + 1] - W, self.cu[i + 1]) for i in range(B)])
         self.q_win = q[torch.from_numpy(rows).cuda()].contiguous()
         self.q, self.k, self.v = q, k, v.contiguous()
@@ -67,6 +69,23 @@ class Layer:
                 at += budgets[b]
                 p = self.cu[b] + np.array(kept + list(range(lens[b] - W, lens[b])))
                 self.rows[b].append([A.held(kn[p, h]), A.held(vn[p, h])])
+
+    def window_by_chunks(self, chunks, q, k, v):
+        """One buffer through the prompts' chunks, each a number of every prompt's next tokens."""
+        import torch
+        from paper_2606_14782_amd import bacon
+        window = torch.full_like(self.window, float("nan"))
+        at = [0] * len(self.lens)
+        for sizes in chunks:
+            to = [a + m for a, m in zip(at, sizes)]
+            rows = torch.cat([q[c + a:c + e] for c, a, e in zip(self.cu, at, to)])
+            keys, values = (torch.cat([x[c:c + e] for c, e in zip(self.cu, to)]) for x in (k, v))
+            batch = bacon.BatchLayout(np.concatenate([[0], np.cumsum(to)]), [1] * len(to))
+            bacon.bacon_prompt_attend(self.ctx.shape, batch, rows, keys, values, np.concatenate([[0], np.cumsum(sizes)]),
+                                      window_lse=window, window_ends=self.lens)
+            at = to
+        assert at == list(self.lens)
+        return window
 
     def tensor(self, *shape):
         import torch
@@ -185,3 +204,14 @@ def test_a_pool_beyond_32_bits_of_bytes():
     for h in range(4):
         o, s, tol, stol = A.attend_held(R.attend, _np(q)[0, 0, h], *want, "bf16")
         assert np.all(np.abs(_np(out)[0, 0, h] - o) <= tol) and abs(float(lse[0, 0, h]) - s) <= stol
+
+
+@pytest.mark.parametrize("case,chunk", [
+    (CASES[0], [[200, 997, 60], [95, 2, 0], [4, 0, 5], [1, 1, 0]]), (CASES[1], [[193, 89], [7, 1]]),
+    (CASES[2], [[64], [635], [1]])])
+def test_prompt_in_chunks_to_decoding(case, chunk, monkeypatch):
+    """The last chunks shorter than the window, one of a single token: the window's
+    normalisers, the kept sets and the decoding as of whole prompts."""
+    whole = Layer
+    monkeypatch.setitem(globals(), "Layer", lambda *a, **kw: whole(*a, chunk=chunk, **kw))
+    test_prompt_to_decoding(*case)
