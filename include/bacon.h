@@ -575,7 +575,8 @@ int32_t bacon_cache_errors(bacon_cache *cache);
  * the first row, the next sections[1] by the second, the others by the third.
  *
  * d_q_norm, d_k_norm (each optional, [d] of the dtype): heads are first
- * normalised, x <- x / sqrt(mean x^2 + norm_eps) * weight. */
+ * normalised, x <- x / sqrt(mean x^2 + norm_eps) * weight, whatever finite values they
+ * hold (a head of zeros and a norm_eps of 0 give NaN). */
 typedef enum { BACON_ROTARY_HALF = 0, BACON_ROTARY_PAIRS = 1 } bacon_rotary_layout;
 typedef enum {
   BACON_ROTARY_PLAIN = 0,

@@ -8,6 +8,9 @@ namespace bacon {
 
 constexpr int kRotaryMaxHeads = 4096;
 constexpr int kRotaryMaxPairs = 64;
+// What a head's values are multiplied by where their squares pass a float's range, or
+// come so low that they lose bits.
+constexpr float kNormLarge = 0x1p-72f, kNormSmall = 0x1p100f;
 constexpr int kRotaryMaxTokens = 1 << 25;     // of a call: a launch holds fewer than 2^32 threads
 
 // Heads of one side (q or k): [tokens, heads, d], tokens `stride` elements apart.
@@ -26,6 +29,7 @@ struct RotateArgs {
   int pairs;               // rotary_dim / 2
   int row1, row2;          // pairs from row1 on turn by the second row, from row2 on by the third
   float magnitude, eps;
+  float eps_large, eps_small;      // eps beside the squares of values times kNormLarge, kNormSmall
   int per_wave;            // head groups a wave takes of its token (set by the launch, as the next)
   int parts;               // waves of a token
   double turns[kRotaryMaxPairs];   // of a pair, a position

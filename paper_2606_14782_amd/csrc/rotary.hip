@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "rotary.h"
 
@@ -136,7 +137,24 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
         for (int e = 0; e < 16; ++e) sum += x[e] * x[e];
 #pragma unroll
         for (int m = 1; m < LH; m <<= 1) sum += __shfl_xor(sum, m);
-        const float f = 1.f / sqrtf(sum * (1.f / D) + a.eps);
+        float f = 1.f / sqrtf(sum * (1.f / D) + a.eps);
+        // Squares past 2^128 (the largest value is then 2^60 or more), or a sum below 2^-80,
+        // of which squares under 2^-126 may be a part: the same of values times a power of
+        // two, which brings the largest to 2^-12 .. 2^56, or below 2^60.  (The lanes of a
+        // head hold the same sum.)
+        if (__builtin_expect(!(sum < INFINITY) || sum + a.eps < 0x1p-80f, 0)) {
+          const bool large = !(sum < INFINITY);
+          const float by = large ? kNormLarge : kNormSmall;
+          sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            x[e] *= by;
+            sum += x[e] * x[e];
+          }
+#pragma unroll
+          for (int m = 1; m < LH; m <<= 1) sum += __shfl_xor(sum, m);
+          f = 1.f / sqrtf(sum * (1.f / D) + (large ? a.eps_large : a.eps_small));
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = x[e] * f * w[e];
       }

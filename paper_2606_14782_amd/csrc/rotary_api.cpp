@@ -173,6 +173,8 @@ bacon_status bacon_rotate(const bacon_rotary *r, int64_t tokens, const int32_t *
   a.row2 = rows ? r->sections[0] + r->sections[1] : a.pairs;
   a.magnitude = (float)frequencies_of(r, f);
   a.eps = (float)r->norm_eps;
+  a.eps_large = (float)(r->norm_eps * kNormLarge * kNormLarge);
+  a.eps_small = (float)std::min(r->norm_eps * kNormSmall * kNormSmall, 3e38);
   for (int i = 0; i < a.pairs; ++i) a.turns[i] = f[i] / kTwoPi;
   const hipError_t e = launch_rotate(a, r->dtype == BACON_BF16, r->head_dim, r->layout == BACON_ROTARY_HALF,
                                      static_cast<hipStream_t>(stream));

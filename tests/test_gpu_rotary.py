@@ -298,3 +298,48 @@ def test_one_token_of_any_view():
     rest = both[:, 6:].clone()
     bacon.bacon_rotate(rot, p, q, k, q_out=q, k_out=k)
     assert torch.equal(both[3:4, :4], wq) and torch.equal(both[3:4, 4:6], wk) and torch.equal(both[:, 6:], rest)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("d,r", [(128, 128), (64, 20)])
+@pytest.mark.parametrize("eps", [0.0, 1e-60, 1e-30, 1e-6, 1e30])
+def test_normalised_heads_of_any_magnitude(dtype, layout, d, r, eps):
+    """Heads whose squares pass a float's range on either side, beside ordinary ones
+    of the same token and wave, and with an eps that counts for some of them only."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(14)
+    e = [0, 40, 58, 61, 64, 70, 100, 124, -30, -39, -41, -50, -63, -75, -100, -120]
+    x = rng.uniform(0.5, 2, (len(e), 5, d)) * rng.choice([-1.0, 1.0], (len(e), 5, d))
+    x[:, 1::2] *= 2.0 ** np.array(e)[:, None, None]             # (heads 0, 2, 4 stay as they are)
+    x[3, 1, ::2] = 0
+    x[6, 1, 5] *= 2.0 ** 20                                     # one value makes the sum
+    t = torch.from_numpy(x.astype(np.float32)).cuda()
+    t = t.bfloat16() if dtype == "bf16" else t
+    w = torch.from_numpy(rng.uniform(0.5, 2, d).astype(np.float32)).cuda().to(t.dtype)
+    pos = rng.integers(0, 5000, len(e))
+    if eps == 1e30:                                             # outputs of the small ones are no normal floats
+        t[8:, 1::2] = 0
+    f, m = A.frequencies(r, 10000.0)
+    got = bacon.bacon_rotate(_rotary(5, 1, d, dtype, r, layout, norm_eps=eps), _positions(pos), t, None, w)[0]
+    assert torch.isfinite(got).all()
+    _check(got, t, pos, f, m, layout, dtype, None, w, eps)
+
+
+def test_normalised_heads_that_are_not_finite():
+    """They are NaN where a value or the root is, and no head beside them changes."""
+    import torch
+    from paper_2606_14782_amd import bacon
+    rng = np.random.default_rng(15)
+    rot, pos = _rotary(4, 1, 64, "fp32", 32), _positions(np.arange(6))
+    x, w = _rand(rng, 6, 4, 64, dtype="fp32"), torch.ones(64, device="cuda")
+    want = bacon.bacon_rotate(rot, pos, x, None, w)[0]
+    y = x.clone()
+    y[1, 2, 40] = float("nan")
+    y[4, 0, 41] = float("inf")
+    got = bacon.bacon_rotate(rot, pos, y, None, w)[0]
+    assert got[1, 2].isnan().all() and got[4, 0, 41].isnan() and (got[4, 0, 42:] == 0).all()
+    same = torch.ones(6, 4, dtype=torch.bool, device="cuda")
+    same[1, 2] = same[4, 0] = False
+    assert torch.equal(got[same], want[same])
