@@ -601,7 +601,7 @@ typedef struct {
   double beta_slow;
   double magnitude;          /* 0: as above                                  */
   double norm_eps;           /* >= 0                                         */
-  const double *frequencies; /* GIVEN: [rotary_dim / 2], host memory         */
+  const double *frequencies; /* [rotary_dim / 2], host memory; of GIVEN alone */
   bacon_dtype dtype;
 } bacon_rotary;
 

@@ -534,7 +534,7 @@ class Rotary:
     """A bacon_rotary: how a model's queries and keys turn with their positions.
 
     sections: three numbers of pairs for three rows of positions (None: one row);
-    frequencies: radians a token of every pair (with scaling ROTARY_GIVEN)."""
+    frequencies: radians a token of every pair, with scaling ROTARY_GIVEN (else refused)."""
 
     def __init__(self, num_q_heads, num_kv_heads, head_dim, dtype, rotary_dim=None, layout=ROTARY_HALF, sections=None,
                  base=10000.0, scaling=ROTARY_PLAIN, factor=1.0, trained_tokens=0, beta_fast=32.0, beta_slow=1.0,
@@ -557,6 +557,8 @@ class Rotary:
         c.dtype = BF16 if self.torch_dtype == torch.bfloat16 else FP32
         self._given = None
         if frequencies is not None:
+            if scaling != ROTARY_GIVEN:
+                raise BaconError(ERR_INVALID, "frequencies are given, scaling is not ROTARY_GIVEN")
             self._given = np.ascontiguousarray(frequencies, dtype=np.float64)
             if self._given.shape != (c.rotary_dim // 2,):
                 raise BaconError(ERR_INVALID, f"{self._given.shape} frequencies for {c.rotary_dim // 2} pairs")

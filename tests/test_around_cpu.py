@@ -148,6 +148,16 @@ def test_binding_refuses_without_a_gpu():
         bacon.bacon_rotate(r, None)
 
 
+@pytest.mark.parametrize("scaling", [None, bacon.ROTARY_PLAIN, bacon.ROTARY_LINEAR, bacon.ROTARY_NTK, bacon.ROTARY_YARN])
+def test_frequencies_that_no_scaling_uses_refused(scaling):
+    """A table is what turns the pairs, or the call ends: it is never dropped."""
+    f = np.full(32, 0.5)
+    kw = {} if scaling is None else dict(scaling=scaling, trained_tokens=4096)
+    with pytest.raises(bacon.BaconError):
+        bacon.Rotary(4, 2, 64, "bf16", frequencies=f, **kw)
+    assert (bacon.Rotary(4, 2, 64, "bf16", scaling=bacon.ROTARY_GIVEN, frequencies=f).frequencies == 0.5).all()
+
+
 # ---------------------------------------------------------------- prompt
 
 def _shape(**kw):
