@@ -280,12 +280,16 @@ struct Share {
 
   // Asks for it, directly into LDS (a wave's 64 pieces one after the other).  The
   // compiler does not see these: it would wait for them before it reads the other
-  // buffer.  tile_barrier waits.  (Nothing else here uses m0.)
+  // buffer.  tile_barrier waits.  (m0 is the compiler's to set where an instruction of its
+  // own reads it: it has to know that this does.  It warns of any such register.)
   __device__ __forceinline__ void ask(const char *tile, unsigned to, int wave) const {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                   :: "s"(to + (wave * kEach + i) * 1024), "v"(at[i]), "s"(tile) : "memory");
+                   :: "s"(to + (wave * kEach + i) * 1024), "v"(at[i]), "s"(tile) : "m0", "memory");
+#pragma clang diagnostic pop
   }
 };
 
