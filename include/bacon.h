@@ -410,6 +410,10 @@ int32_t bacon_profile_read(bacon_ctx *ctx, bacon_kernel_time *out, int32_t max);
 /* What a cache holds its K and V in. */
 typedef enum { BACON_CACHE_E4M3 = 0, BACON_CACHE_E2M1 = 1 } bacon_cache_format;
 
+/* Clear it before its fields are set ({0}).  `format` lies where the struct had four bytes
+ * of padding before there were formats: its size and the other fields are as they were,
+ * and a caller built without the field gets E4M3 where that padding is 0 -- other bytes
+ * there are refused, or 1 taken for E2M1. */
 typedef struct {
   int32_t num_layers;
   int32_t num_q_heads;

@@ -292,3 +292,21 @@ def test_window_ends_before_the_keys_refused():
         _refused(_chunk(ends, cuq=[0, 0, 0]), INV)              # (also of a sequence without queries)
     _refused(_chunk([50, 2 ** 31 - 1], q=None), INV)            # the other checks are bacon_prompt_attend's
     assert _chunk([50, 2 ** 31 - 1], cuq=[0, 0, 0]) == bacon.OK
+
+
+def test_the_format_lies_in_former_padding():
+    """Callers built without the field: the same size, every other field in its place."""
+    before = [(n, t) for n, t in bacon.CacheShape._fields_ if n != "format"]
+
+    class Old(C.Structure):
+        _fields_ = before
+
+    assert C.sizeof(Old) == C.sizeof(bacon.CacheShape) == 48
+    for n, _ in before:
+        assert getattr(Old, n).offset == getattr(bacon.CacheShape, n).offset, n
+    assert bacon.CacheShape.format.offset == Old.dtype.offset + 4
+    old, a, b = Old(3, 8, 2, 128, 32, 32, 4, 10, 200, bacon.BF16), bacon.CacheOffsets(), bacon.CacheOffsets()
+    L = bacon.lib()
+    assert L.bacon_cache_layout(C.cast(C.byref(old), C.POINTER(bacon.CacheShape)), C.byref(a)) == bacon.OK
+    assert L.bacon_cache_layout(C.byref(_cache_shape(format=bacon.CACHE_E4M3)), C.byref(b)) == bacon.OK
+    assert a.total == b.total and a.codes == b.codes
