@@ -565,7 +565,10 @@ int32_t bacon_cache_errors(bacon_cache *cache);
  *   YARN    f_i = (1 - g) w_i / s + g w_i, g = (n - beta_slow) / (beta_fast -
  *           beta_slow) held to [0, 1], n = trained_tokens w_i / (2 pi) the turns
  *           that the pair made in training; m = 0.1 ln s + 1 (Peng et al. 2023,
- *           "YaRN: Efficient Context Window Extension of Large Language Models")
+ *           "YaRN: Efficient Context Window Extension of Large Language Models").
+ *           Programs that let g run over the pair's number between two rounded
+ *           borders, instead of over its turns, give the pairs between them other
+ *           frequencies: a model served that way takes GIVEN, with its magnitude
  *   GIVEN   f_i = frequencies[i] (within +-1e6), m = 1
  * magnitude > 0 replaces m.
  *
