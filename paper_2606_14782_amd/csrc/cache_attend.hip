@@ -708,6 +708,8 @@ hipError_t attend(const CacheStepArgs &a, hipStream_t s) {
   // unit holds two workgroups of four waves), one of 400 rows 13.6 and 13.3.  Attends
   // gain nothing (four sequences over 8K rows, 28 query rows, 15.7 and 14.6, eight
   // over 16K 47.9 and 48.9; one query row, 64 over 300 to 993 rows, 22.8 and 17.2).
+  // (These were measured in e4m3.  In e2m1, with eight and with four: the step of 256
+  // pairs 18.3 and 18.9, four attends over 8K rows 19.0 and 14.8.)
   const bool late = a.k && NT == 2 && a.chunk > 256 && units <= 256;
   const int waves = late && max_waves(BF16, D, NT) == 8 ? 8 : 4;
   if (hipError_t e = allow_lds<k_cache_attend<FMT, BF16, D, NT>>(attend_lds<BF16, D, NT>(waves))) return e;
@@ -729,6 +731,9 @@ CachePlan cache_plan(int pairs, int q_rows, int head_dim, int max_tokens) {
   // go down to a tile a part (over 1K rows 7.3 us, in parts of 256 8.1, whole
   // 8.9), with more than 16 query rows, whose workgroups are more already, to
   // 256 rows (three over 2K rows, 56 query rows: 18.0 us, in parts of 128 21.8).
+  // (In e4m3.  In e2m1: 32K rows in 256, 128 and 512 14.0, 18.8, 14.3 us; 512 rows whole and
+  // in parts 6.9, 7.3; 768 8.2, 7.2; 1K by 64, by 256 and whole 7.4, 7.9, 9.6; 56 query rows
+  // over 2K 12.1, in parts of 128 13.4.)
   const int64_t want = (256 + pairs - 1) / pairs;
   const int64_t by_rows = max_tokens <= 768 ? 1 : max_tokens / (q_rows > 16 ? 256 : 64);
   p.splits = (int)std::min(want, by_rows);
@@ -754,8 +759,10 @@ hipError_t launch_cache_attend(CacheStepArgs a, bool bf16, int head_dim, hipStre
   // (64/8, eight tokens) 25.3 and 20.4, eight over 16K (32 query rows) 56.1 and
   // 48.9; but 64 over 300 to 993 rows (28 query rows) 15.4 and 16.1, one over 64 rows
   // 5.5 and 7.0.  fp32, whose parts fill the registers: five tokens of four
-  // sequences 13.1 and 14.8.  A step of 17 to 32 query rows keeps them in the one
-  // workgroup that appends: two would not see each other's rows.
+  // sequences 13.1 and 14.8.  (In e4m3.  In e2m1: three of 40K to 70K rows, where 32 are
+  // slower, 56.5 and 59.4; 23.1 and 20.7; 50.7 and 43.8; 14.8 and 14.9; fp32 13.5 and
+  // 15.3.)  A step of 17 to 32 query rows keeps them in the one workgroup that
+  // appends: two would not see each other's rows.
   const bool shared = bf16 && a.chunk > 256 && (R > 32 || a.chunk > 1024);
   const bool one = R <= 16 || !(a.k || shared);
   a.groups = (R + (one ? 15 : 31)) / (one ? 16 : 32);
