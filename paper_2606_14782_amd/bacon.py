@@ -664,8 +664,8 @@ def bacon_prompt_attend(shape: Shape, batch: BatchLayout, q, k, v, queries=None,
     if need and work is None:
         work = q.new_empty(need, dtype=torch.uint8)
     workp = g.whole(work, "work", None, torch.uint8)
-    g.call(L.bacon_prompt_attend_chunk, sp, bp, cup, endp, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, outp, lsep, winp,
-           workp, 0 if work is None else work.numel())
+    g.call(L.bacon_prompt_attend_chunk, sp, bp, cup, endp, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, outp, lsep,
+           winp, workp, 0 if work is None else work.numel())
     return out, lse, window_lse
 
 
